@@ -294,7 +294,7 @@ def _plain_reserve(st, first, last, keep):
     refs.index_add_(0, src, torch.full_like(src, -1, dtype=torch.int32))
     refs[new] = 1
     table[got] = new.to(torch.int32)
-    bad = (j * page < last) & ((table < 0) | (shared & ~got))
+    bad = need & ~got
     lead = torch.where(bad, j, table.shape[1]).amin(1)
     return torch.minimum(last[:, 0].clamp(min=0), lead * page).to(torch.int32)
 
@@ -444,8 +444,6 @@ def _exact_pages(case, st):
                             refs[p] -= 1
                     else:
                         lead = min(lead, j * page)
-                elif j * page < hi and p < 0:
-                    lead = min(lead, j * page)
             granted.append(min(lead, len(table[b]) * page))
         return granted
 
