@@ -231,6 +231,140 @@ sd2_status sd2_train_loss(sd2_handle_t h, const int32_t* tokens, const int32_t* 
                           int32_t rows_per_chunk, float* out_kl, float* out_loss, void* scratch,
                           size_t scratch_bytes);
 
+/*
+ * Paged K/V caches.
+ *
+ * A page holds page_size consecutive positions of one sequence, in every array of the cache.  The
+ * table names the pages of each sequence in the order of its positions; refs counts for every page the
+ * table entries that name it, so that sequences with a common beginning can share its pages.  All of it
+ * is the caller's device memory: start with refs 0 and table entries -1.  sd2_pages_reserve gives a
+ * sequence the pages it is about to write (and copies those it shares), sd2_pages_fork lets it go on from
+ * another one's, sd2_pages_trim takes pages back, sd2_pages_compact moves the pages in use together;
+ * sd2_paged_append writes rows, sd2_paged_attn reads them.  A table entry outside 0 .. n_pages - 1 names
+ * no page: its positions are neither read nor written.
+ *
+ * These calls belong to no handle.  Each is asynchronous on hip_stream (NULL: the default stream) of
+ * the current device, which the memory has to be on; calls on one cache have to be ordered (one stream, or
+ * events between them), calls on different caches need not be, as long as they have workspaces of their
+ * own.  They may be captured into a graph; a replay reads the device arrays anew, while host values (lists of
+ * sequences, sizes) are those of the capture.  Workspaces need no initialisation, are 256-byte
+ * aligned, and are used by the call's own kernels only.  Arguments are checked before anything is enqueued;
+ * what device arrays hold (lengths, offsets, table entries) cannot be, and is brought into range by the
+ * kernels, as stated with each call.  No pair of buffers of a call may overlap unless stated.
+ */
+#define SD2_PAGE_ARRAYS 8     /* arrays of a cache at most */
+#define SD2_PAGED_MAX_SEQS 4096
+
+/* One array of a cache: page p is blocks * page_size rows of row_bytes bytes, page after page.  A block
+ * (a layer and KV head, say) is the page's positions in order. */
+typedef struct {
+    void* data;         /* device, 16-byte aligned */
+    int32_t blocks;     /* 1..65536 */
+    int32_t row_bytes;  /* a multiple of 16, up to 65536 */
+} sd2_page_array;
+
+typedef struct {
+    int32_t page_size;  /* positions per page: 16, 32, 64, 128, 256, 512 or 1024 */
+    int32_t n_pages;    /* 1..2^24 */
+    int32_t max_seqs;   /* 1..SD2_PAGED_MAX_SEQS */
+    int32_t max_pages;  /* entries of a sequence; max_pages * page_size below 2^31 */
+    int32_t* table;     /* device [max_seqs][max_pages] */
+    int32_t* refs;      /* device [n_pages] */
+    int32_t n_arrays;   /* 1..SD2_PAGE_ARRAYS */
+    sd2_page_array arrays[SD2_PAGE_ARRAYS];
+} sd2_pages;
+
+/* Bytes of workspace that sd2_pages_reserve and sd2_pages_compact need (0: invalid). */
+size_t sd2_pages_workspace_bytes(const sd2_pages* pages);
+
+/*
+ * Make positions first[b] .. last[b] - 1 of the sequences b = 0 .. nseq - 1 writable (device int32
+ * [nseq] each; first[b] >= last[b]: nothing for this one).  Of the table entries that hold these positions,
+ *  - one that names no page gets a free page (refs 0), and
+ *  - one whose page is shared (refs above 1 when the call begins) gets a free page too, to which the rows
+ *    of the positions below keep[b] are copied (keep NULL: below first[b]); the shared page loses this
+ *    reference.  Sequences that share a page and both write to it get a copy each.
+ * Free pages are given in ascending order to the entries in the order of (sequence, position).  granted (device int32
+ * [nseq], or NULL) receives last[b], or the position where the first page begins that the pool could not
+ * give or that lies behind the table's last entry.  Entries left without a page stay as they were.
+ * Negative positions count as 0.
+ */
+sd2_status sd2_pages_reserve(const sd2_pages* pages, int32_t nseq, const int32_t* first, const int32_t* last,
+                             const int32_t* keep, int32_t* granted, void* workspace, size_t workspace_bytes,
+                             void* hip_stream);
+
+/*
+ * For each i the sequence dst[i] gives up its pages and takes those of src[i], shared (HOST int32 [n]
+ * each, sequences in 0 .. max_seqs - 1; no dst twice, and none that is also a src:
+ * SD2_ERR_INVALID_ARG).  No row is copied: see sd2_pages_reserve.
+ */
+sd2_status sd2_pages_fork(const sd2_pages* pages, int32_t n, const int32_t* src, const int32_t* dst, void* hip_stream);
+
+/*
+ * Sequences b = 0 .. nseq - 1 keep the pages of their first lens[b] positions (device int32 [nseq])
+ * and give up the others; lens[b] = 0 frees a sequence, a negative one leaves it as it is.
+ */
+sd2_status sd2_pages_trim(const sd2_pages* pages, int32_t nseq, const int32_t* lens, void* hip_stream);
+
+/*
+ * Move the pages in use (refs above 0) to 0 .. live - 1: those behind, in ascending order, into the
+ * free ones before, in ascending order, with their rows, references and table entries.  live (device int32
+ * [1], or NULL) receives their number.
+ */
+sd2_status sd2_pages_compact(const sd2_pages* pages, int32_t* live, void* workspace, size_t workspace_bytes,
+                             void* hip_stream);
+
+/* One layer of a paged cache for sd2_paged_append and sd2_paged_attn: the row of page p, KV head h and
+ * slot s starts at element p * page_stride + (h * page_size + s) * head_dim of k and of v. */
+typedef struct {
+    void *k, *v;           /* device, 16-byte aligned */
+    int64_t page_stride;   /* elements, at least n_kv_heads * page_size * head_dim, whole 16-byte units */
+    int32_t dtype;         /* sd2_dtype of k, v and of the rows of a call */
+    int32_t page_size;     /* as sd2_pages */
+    int32_t n_pages;       /* as sd2_pages */
+    int32_t n_kv_heads;    /* 1..1024 */
+    int32_t head_dim;      /* 32, 64 or 128 */
+    int32_t max_pages;     /* as sd2_pages */
+    const int32_t* table;  /* device [nseq][max_pages] */
+} sd2_paged_kv;
+
+/* The rows that a call brings, packed: sequence b = 0 .. nseq - 1 has the rows row_off[b] ..
+ * row_off[b + 1] - 1 (ascending; or max_rows rows each, when row_off is NULL), and they are the last ones
+ * of its lens[b] positions: row i of n is position lens[b] - n + i.  Offsets are brought into 0 ..
+ * total_rows, rows of a sequence beyond max_rows and rows that belong to no sequence are left alone. */
+typedef struct {
+    int32_t nseq;            /* 0..SD2_PAGED_MAX_SEQS */
+    int32_t max_rows;        /* of one sequence, at least 1 */
+    int32_t total_rows;      /* of all; nseq * max_rows when row_off is NULL */
+    const int32_t* row_off;  /* device [nseq + 1], or NULL */
+    const int32_t* lens;     /* device [nseq] */
+} sd2_paged_rows;
+
+/* Rows of k and v (device [total_rows][n_kv_heads][head_dim], k_stride and v_stride elements from one row
+ * to the next, whole 16-byte units) into the pages of their positions.  Rows without a page, or at a
+ * negative position, are dropped. */
+sd2_status sd2_paged_append(const sd2_paged_kv* kv, const sd2_paged_rows* rows, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, void* hip_stream);
+
+/*
+ * Causal grouped-query attention of the rows over their sequences' pages: row at position p, head h:
+ *   out = sum_j softmax_j(scale * q . k_j) v_j   over the positions j <= p that have a page,
+ * KV head h / (n_heads / n_kv_heads); zeros when there is none (a negative position, no page).
+ * q, out: device [total_rows][n_heads][head_dim], q_stride and out_stride elements from one row to the next
+ * (whole 16-byte units); n_heads a multiple of n_kv_heads, up to 1024.  bf16: scores, softmax and
+ * sums in fp32, the softmax's weights rounded to bf16 for their product with v; fp32: fp32 throughout.
+ * Memory behind a sequence's last position, and pages it does not name, are not read, or do not count,
+ * whatever they hold.  A non-finite value of v may reach the rows of its sequence in this call that
+ * lie before it as well as those behind.
+ * max_len: the largest length expected, 1..max_pages * page_size (it decides how the work is split; a longer
+ * sequence is computed all the same).
+ */
+size_t sd2_paged_attn_workspace_bytes(const sd2_paged_kv* kv, const sd2_paged_rows* rows, int32_t n_heads,
+                                      int32_t max_len);
+sd2_status sd2_paged_attn(const sd2_paged_kv* kv, const sd2_paged_rows* rows, const void* q, int64_t q_stride,
+                          void* out, int64_t out_stride, int32_t n_heads, float scale, int32_t max_len,
+                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Destroy a handle (NULL is a no-op).  Does not free caller memory. */
 sd2_status sd2_destroy(sd2_handle_t h);
 

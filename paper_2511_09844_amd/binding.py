@@ -20,7 +20,9 @@ DBG_LOGITS_V, DBG_LOGITS_D, DBG_STEER, DBG_OWN_DRAFTS, DBG_OWN_N, DBG_OWN_Y, DBG
 
 EXPORTS = ["sd2_workspace_bytes", "sd2_create", "sd2_create_noalloc", "sd2_create_mlp", "sd2_train_loss",
            "sd2_train_loss_scratch_bytes", "sd2_prefill", "sd2_round", "sd2_round_forced", "sd2_destroy",
-           "sd2_status_string", "sd2_last_error", "sd2_debug_read", "sd2_profile", "sd2_profile_read"]
+           "sd2_status_string", "sd2_last_error", "sd2_debug_read", "sd2_profile", "sd2_profile_read",
+           "sd2_pages_workspace_bytes", "sd2_pages_reserve", "sd2_pages_fork", "sd2_pages_trim", "sd2_pages_compact",
+           "sd2_paged_append", "sd2_paged_attn_workspace_bytes", "sd2_paged_attn"]
 PROF_GEMV, PROF_ATTN, PROF_SAMPLER, PROF_OTHER, PROF_PROGRAM = 1, 2, 3, 4, 5
 
 
@@ -47,6 +49,30 @@ STEER_INPUT, STEER_MLP, STEER_MLP_OUT, STEER_NONE, STEER_MLP_COND = 0, 1, 2, 3, 
 class MlpSteering(ctypes.Structure):
     _fields_ = [("w_s", P), ("w_hml", P), ("ln_gain", P), ("ln_bias", P), ("ln_eps", ctypes.c_float),
                 ("w_cf", P), ("w_cu", P)]
+
+
+PAGE_ARRAYS, PAGED_MAX_SEQS = 8, 4096
+
+
+class PageArray(ctypes.Structure):
+    _fields_ = [("data", P), ("blocks", ctypes.c_int32), ("row_bytes", ctypes.c_int32)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_seqs", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("table", P), ("refs", P), ("n_arrays", ctypes.c_int32),
+                ("arrays", PageArray * PAGE_ARRAYS)]
+
+
+class PagedKv(ctypes.Structure):
+    _fields_ = [("k", P), ("v", P), ("page_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", P)]
+
+
+class PagedRows(ctypes.Structure):
+    _fields_ = [("nseq", ctypes.c_int32), ("max_rows", ctypes.c_int32), ("total_rows", ctypes.c_int32),
+                ("row_off", P), ("lens", P)]
 
 
 _lib = None
@@ -93,6 +119,24 @@ def load():
         lib.sd2_profile_read.argtypes = [P, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32),
                                          ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
         lib.sd2_profile_read.restype = ctypes.c_int32
+        i32, i64, pages, kv, rows = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(Pages), ctypes.POINTER(PagedKv), \
+            ctypes.POINTER(PagedRows)
+        lib.sd2_pages_workspace_bytes.argtypes = [pages]
+        lib.sd2_pages_workspace_bytes.restype = ctypes.c_size_t
+        lib.sd2_pages_reserve.argtypes = [pages, i32, P, P, P, P, P, ctypes.c_size_t, P]
+        lib.sd2_pages_reserve.restype = i32
+        lib.sd2_pages_fork.argtypes = [pages, i32, P, P, P]
+        lib.sd2_pages_fork.restype = i32
+        lib.sd2_pages_trim.argtypes = [pages, i32, P, P]
+        lib.sd2_pages_trim.restype = i32
+        lib.sd2_pages_compact.argtypes = [pages, P, P, ctypes.c_size_t, P]
+        lib.sd2_pages_compact.restype = i32
+        lib.sd2_paged_append.argtypes = [kv, rows, P, i64, P, i64, P]
+        lib.sd2_paged_append.restype = i32
+        lib.sd2_paged_attn_workspace_bytes.argtypes = [kv, rows, i32, i32]
+        lib.sd2_paged_attn_workspace_bytes.restype = ctypes.c_size_t
+        lib.sd2_paged_attn.argtypes = [kv, rows, P, i64, P, i64, i32, ctypes.c_float, i32, P, ctypes.c_size_t, P]
+        lib.sd2_paged_attn.restype = i32
         _lib = lib
     return _lib
 

@@ -1,0 +1,510 @@
+"""Paged K/V caches on the GPU against plain float64 attention and a list model of the pages.
+
+Every cache here holds NaN (or infinities) behind its sequences' last positions and in every page that no
+sequence names, its pages lie in no order, and tolerances are those of attend_bound."""
+import random
+
+import pytest
+import torch
+
+from paged_ref import PageModel, attend64, attend_bound, make_cache, rows_of
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def check(cache, q, lens, rows, packed, layer=0, scale=None, out=None, **kw):
+    ln, off = rows_of(lens, rows, packed)
+    got = cache.attend(q, ln, layer=layer, row_off=off, scale=scale, out=out, **kw)
+    ref, absv, spread = attend64(cache, q, lens, rows, layer, scale)
+    bound = attend_bound(ref, absv, spread, cache.dtype, max(lens + [1]), cache.head_dim)
+    err = (got.double() - ref).abs()
+    assert torch.isfinite(got).all()
+    worst = float((err / bound).max()) if err.numel() else 0.0
+    assert worst <= 1.0, f"error {float(err.max())} is {worst} of the bound"
+    return got
+
+
+def queries(n, heads, hd, dtype, seed=1, std=1.0):
+    return (torch.randn(n, heads, hd, generator=torch.Generator().manual_seed(seed)) * std).to(dtype).cuda()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("h,hkv,hd", [(1, 1, 32), (6, 2, 64), (8, 1, 128), (17, 1, 64), (12, 12, 32)])
+def test_one_token(dtype, page, h, hkv, hd):
+    # one token, the ends of tiles and pages, an empty sequence, a few thousand
+    lens = [1, 0, 15, 16, 17, 31, 33, 63, 64, 65, 127, 257, 1000, 2311]
+    cache = make_cache(lens, dtype, hkv, hd, page)
+    check(cache, queries(len(lens), h, hd, dtype), lens, [1] * len(lens), False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("h,hkv,hd", [(4, 4, 64), (8, 2, 128), (3, 1, 32), (16, 2, 64)])
+@pytest.mark.parametrize("rows", [2, 5, 9, 16, 17, 33])
+def test_blocks_of_rows(dtype, h, hkv, hd, rows):
+    # lengths from fewer positions than rows (the first rows then have none) to several spans
+    lens = [0, 1, rows - 1, rows, rows + 1, 48, 300, 1029]
+    cache = make_cache(lens, dtype, hkv, hd, 32)
+    check(cache, queries(rows * len(lens), h, hd, dtype), lens, [rows] * len(lens), False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("h,hkv,hd,page", [(4, 4, 64, 16), (8, 2, 128, 64), (3, 1, 32, 32), (12, 4, 64, 128)])
+def test_packed_prompts(dtype, h, hkv, hd, page):
+    lens = [1, 0, 700, 16, 129, 64, 63, 255, 2, 33]
+    cache = make_cache(lens, dtype, hkv, hd, page)
+    check(cache, queries(sum(lens), h, hd, dtype), lens, lens, True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_chunks_over_what_is_cached(dtype):
+    lens, rows = [900, 77, 40, 0, 512, 1, 333], [100, 77, 0, 0, 1, 1, 200]
+    cache = make_cache(lens, dtype, 2, 128, 64, layers=3, extra_entries=4)
+    q = queries(sum(rows), 8, 128, dtype)
+    for layer in (0, 2):
+        check(cache, q, lens, rows, True, layer=layer, max_rows=200, max_len=900)
+        check(cache, q, lens, rows, True, layer=layer)  # no hints
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 70], ids=["one", "many"])
+def test_missing_pages_do_not_count(dtype, rows):
+    lens = [400, 333, 200, 90]
+    cache = make_cache(lens, dtype, 2, 64, 32)
+    cache.table[0, 3] = -1
+    cache.table[1, 0] = cache.n_pages        # no such page
+    cache.table[1, 10] = -2 ** 31
+    cache.table[2, :] = -1                   # a sequence without any: zeros
+    cache.table[3, 0] = 2 ** 31 - 1
+    got = check(cache, queries(rows * 4, 4, 64, dtype), lens, [rows] * 4, False)
+    assert (got[2 * rows: 3 * rows] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("std", [0.0, 30.0], ids=["equal", "peaked"])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_scores_all_equal_or_far_apart(dtype, std, rows):
+    lens = [517, 64]
+    cache = make_cache(lens, dtype, 2, 64, 16, stale=float("inf"))
+    check(cache, queries(rows * 2, 4, 64, dtype, std=std), lens, [rows] * 2, False)
+    check(cache, queries(rows * 2, 4, 64, dtype), lens, [rows] * 2, False, scale=-0.5)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 3, 150])
+def test_rows_apart_and_rows_of_no_sequence(dtype, rows):
+    lens = [rows + 170, rows + 5]
+    n = 2 * rows
+    cache = make_cache(lens, dtype, 2, 64, 16)
+    wide = queries(n + 7, 12, 64, dtype)  # Q | K | V of a projection, q its first 8 heads
+    q = wide[:, :8]
+    out = torch.full((n + 7, 10, 64), 3.0, dtype=dtype, device="cuda")
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    off = torch.tensor([2, 2 + rows, 2 + n], dtype=torch.int32, device="cuda")
+    cache.attend(q, ln, row_off=off, max_rows=rows, out=out[:, 1:9])
+    ref, absv, spread = attend64(cache, q[2: 2 + n], lens, [rows, rows])
+    bound = attend_bound(ref, absv, spread, dtype, max(lens), 64)
+    assert ((out[2: 2 + n, 1:9].double() - ref).abs() <= bound).all()
+    out[2: 2 + n, 1:9] = 3.0
+    assert (out == 3.0).all(), "something else was written"
+
+
+def test_offsets_out_of_range_stay_inside():
+    lens = [60, 70, 80]
+    cache = make_cache(lens, BF16, 2, 64, 16)
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    q = queries(12, 4, 64, BF16)
+    out = torch.full_like(q, 3.0)
+    off = torch.tensor([-5, 4, 2 ** 30, 7], dtype=torch.int32, device="cuda")  # rows 0-3, 4-11, none
+    cache.attend(q, ln, row_off=off, max_rows=8, out=out)
+    ref, absv, spread = attend64(cache, q, lens, [4, 8, 0])
+    assert ((out.double() - ref).abs() <= attend_bound(ref, absv, spread, BF16, 80, 64)).all()
+    off = torch.tensor([4, 4, 9, 12], dtype=torch.int32, device="cuda")  # more rows than max_rows: the first of them
+    out.fill_(3.0)
+    cache.attend(q, ln, row_off=off, max_rows=2, out=out)
+    assert (out[:4] == 3.0).all() and (out[6:9] == 3.0).all() and (out[11] == 3.0).all()
+
+
+@pytest.mark.parametrize("rows", [1, 20, 200])
+def test_far_pages_of_a_large_pool(rows):
+    # element offsets beyond 2^32
+    from paper_2511_09844_amd.paged import PagedCache
+    page, hkv, hd, n_pages = 256, 4, 128, 36000  # 4.7e9 elements
+    k = torch.empty(n_pages, 1, hkv, page, hd, dtype=BF16, device="cuda")
+    v = torch.empty_like(k)
+    lens = [700, 513]
+    table = torch.full((2, 4), -1, dtype=torch.int32)
+    table[0, :3] = torch.tensor([n_pages - 1, 3, n_pages - 5])
+    table[1, :3] = torch.tensor([n_pages // 2, n_pages - 2, 0])
+    refs = torch.zeros(n_pages, dtype=torch.int32)
+    cache = PagedCache(k, v, table.cuda(), refs.cuda())
+    used = table[table >= 0].long().cuda()
+    for pool in (k, v):
+        pool[used] = torch.randn(len(used), 1, hkv, page, hd, device="cuda").to(BF16)
+    new = [queries(2 * rows, hkv, hd, BF16, seed=s) for s in (2, 3)]
+    ln, _ = rows_of(lens, [rows] * 2, False)
+    cache.append(*new, ln)
+    for b, n in enumerate(lens):
+        for i in range(rows):
+            j = n - rows + i
+            for x, pool in zip(new, (k, v)):
+                assert torch.equal(pool[table[b, j // page].item(), 0, :, j % page], x[b * rows + i])
+    check(cache, queries(2 * rows, 8, hd, BF16), lens, [rows] * 2, False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("hd,hkv", [(32, 3), (64, 1), (128, 8)])
+def test_append(dtype, hd, hkv):
+    lens, rows = [1, 0, 300, 17, 64, 5, 40], [1, 0, 300, 3, 64, 8, 2]  # (sequence 5 brings more rows than positions)
+    cache = make_cache(lens, dtype, hkv, hd, 16, layers=2)
+    cache.table[6, 2] = -1
+    cache.table[2, 4] = cache.n_pages + 7
+    wide = queries(sum(rows), 2 * hkv + 1, hd, dtype)  # k and v as parts of wider rows
+    k, v = wide[:, 1: 1 + hkv], wide[:, 1 + hkv:]
+    want = [cache.k.clone(), cache.v.clone()]
+    table = cache.table.tolist()
+    at = 0
+    for b, (n, r) in enumerate(zip(lens, rows)):
+        for i in range(r):
+            j = n - r + i
+            if j >= 0 and 0 <= table[b][j // 16] < cache.n_pages:
+                want[0][table[b][j // 16], 1, :, j % 16] = k[at + i]
+                want[1][table[b][j // 16], 1, :, j % 16] = v[at + i]
+        at += r
+    ln, off = rows_of(lens, rows, True)
+    cache.append(k, v, ln, layer=1, row_off=off, max_rows=max(rows))
+    for got, ref in zip((cache.k, cache.v), want):
+        assert torch.equal(got.view(torch.int16 if dtype == BF16 else torch.int32), ref.view(torch.int16 if dtype == BF16 else torch.int32))
+
+
+def test_refusals_of_the_binding():
+    from paper_2511_09844_amd.binding import Sd2Error
+    cache = make_cache([40, 50], BF16, 2, 64, 16, layers=2)
+    ln = torch.tensor([40, 50], dtype=torch.int32, device="cuda")
+    q = queries(2, 4, 64, BF16)
+    bad = [lambda: cache.attend(q.float(), ln), lambda: cache.attend(q.cpu(), ln), lambda: cache.attend(q[:, :3], ln),
+           lambda: cache.attend(q[..., :32], ln), lambda: cache.attend(q, ln.long()), lambda: cache.attend(q, ln.cpu()),
+           lambda: cache.attend(q, ln, layer=2), lambda: cache.attend(q, ln, layer=-1), lambda: cache.attend(q, ln, out=q),
+           lambda: cache.attend(q, ln, out=q[:1]), lambda: cache.attend(q, ln, max_len=0), lambda: cache.attend(q, ln, max_rows=2),
+           lambda: cache.attend(q, ln, max_len=10 ** 6), lambda: cache.attend(q, ln, row_off=ln),
+           lambda: cache.attend(torch.cat([q, q[:1]]), ln), lambda: cache.attend(q.transpose(1, 2).contiguous().transpose(1, 2), ln),
+           lambda: cache.attend(q, torch.zeros(3, dtype=torch.int32, device="cuda")),
+           lambda: cache.attend(q, ln, scale=float("nan")), lambda: cache.attend(torch.empty(2, 0, 64, dtype=BF16, device="cuda"), ln),
+           lambda: cache.append(q[:, :2], q, ln), lambda: cache.append(q, q, ln), lambda: cache.append(q[:, :2], q[:1, :2], ln),
+           lambda: cache.reserve(ln, ln[:1]), lambda: cache.reserve(ln, ln.long()), lambda: cache.trim(ln.cpu()),
+           lambda: cache.trim(torch.zeros(3, dtype=torch.int32, device="cuda")), lambda: cache.fork([0], [0]),
+           lambda: cache.fork([0], [5]), lambda: cache.fork([0, 1], [1])]
+    for i, call in enumerate(bad):
+        with pytest.raises(Sd2Error):
+            call()
+            print("not refused:", i)
+    from paper_2511_09844_amd.paged import PagedCache
+    with pytest.raises(Sd2Error):
+        PagedCache(cache.k, cache.v.float(), cache.table, cache.refs)
+    with pytest.raises(Sd2Error):
+        PagedCache(cache.k, cache.v, cache.table, cache.refs[:-1])
+    with pytest.raises(Sd2Error):
+        PagedCache.empty(4, 24, 1, 1, 64, 1, 1)
+    # nothing to do is no error
+    cache.fork([], [])
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert cache.attend(q[:0], none).shape == (0, 4, 64) and cache.reserve(none, none).numel() == 0
+    cache.append(q[:0, :2], q[:0, :2], none)
+    cache.trim(none)
+
+
+# ---- pages ---------------------------------------------------------------------------------------------
+
+class Tagged:
+    """A small cache and its list model, every slot of the cache holding the model's tag."""
+
+    def __init__(self, n_pages, page, seqs, entries, dtype=F32, layers=2, hkv=3, hd=32):
+        from paper_2511_09844_amd.paged import PagedCache
+        self.cache = PagedCache.empty(n_pages, page, layers, hkv, hd, seqs, entries, dtype)
+        self.model = PageModel(n_pages, page, seqs, entries)
+        self.cache.k.zero_()
+        self.cache.v.zero_()
+        self.tag = 0
+
+    def dev(self, v):
+        return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+    def write(self, b, lo, hi):
+        """Tag positions lo .. hi - 1 of sequence b."""
+        for j in range(lo, hi):
+            p = self.model.table[b][j // self.model.page]
+            if p >= 0:
+                self.tag += 1
+                self.model.tags[p][j % self.model.page] = self.tag
+                self.cache.k[p, :, :, j % self.model.page] = self.tag
+                self.cache.v[p, :, :, j % self.model.page] = -self.tag
+
+    def check(self):
+        assert self.cache.table.tolist() == self.model.table
+        assert self.cache.refs.tolist() == self.model.refs
+        k, v = self.cache.k.cpu(), self.cache.v.cpu()
+        for row in self.model.table:
+            for p in row:
+                if p >= 0:
+                    for s, t in enumerate(self.model.tags[p]):
+                        if t is not None:
+                            assert (k[p, :, :, s] == t).all() and (v[p, :, :, s] == -t).all(), (p, s, t)
+
+    def reserve(self, first, last, keep=None):
+        got = self.cache.reserve(self.dev(first), self.dev(last), None if keep is None else self.dev(keep))
+        want = self.model.reserve(first, last, keep)
+        assert got.tolist() == want
+        return want
+
+    def fork(self, src, dst):
+        self.cache.fork(src, dst)
+        self.model.fork(src, dst)
+
+    def trim(self, lens):
+        self.cache.trim(self.dev(lens))
+        self.model.trim(lens)
+
+    def compact(self):
+        assert self.cache.compact().tolist() == [self.model.compact()]
+
+
+def test_pages_given_shared_copied_taken_back_and_moved():
+    t = Tagged(12, 16, 4, 5)
+    assert t.reserve([0, 0], [33, 16]) == [33, 16]
+    t.write(0, 0, 33)
+    t.write(1, 0, 16)
+    t.check()
+    t.fork([0, 0], [2, 3])
+    t.check()
+    # sequence 2 writes on in the shared last page, sequence 3 begins a page of its own
+    assert t.reserve([0, 16, 33, 48], [0, 20, 40, 50]) == [0, 20, 40, 50]
+    t.check()
+    t.write(2, 33, 40)
+    t.check()
+    t.trim([0, -1, 32, -1])
+    t.check()
+    t.compact()
+    t.check()
+    t.compact()  # nothing left to move
+    t.check()
+    # everything free again
+    t.trim([0, 0, 0, 0])
+    t.check()
+    assert t.cache.refs.sum() == 0
+    t.compact()
+    t.check()
+
+
+def test_a_pool_that_runs_out_and_a_table_that_ends():
+    t = Tagged(5, 16, 3, 4)
+    assert t.reserve([0, 0, 0], [40, 40, 10]) == [40, 32, 0]  # 3 + 2 pages, none left
+    t.check()
+    t.write(0, 0, 40)
+    t.fork([0], [2])
+    assert t.reserve([0, 0, 30], [0, 0, 48]) == [0, 0, 16]    # shared, and no page for a copy
+    t.check()
+    t.trim([-1, 0, -1])
+    assert t.reserve([0, 0, 30], [0, 0, 48]) == [0, 0, 48]
+    t.check()
+    t.trim([0, 0, 0])
+    assert t.reserve([0, -7, 70], [1000, -3, 80]) == [64, 0, 64]  # four entries; behind them
+    t.check()
+    assert t.reserve([0], [64]) == [64]                       # there already
+    t.check()
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_random_histories(seed):
+    rng = random.Random(seed)
+    page, seqs, entries = rng.choice([16, 32]), rng.choice([2, 5, 9]), rng.choice([3, 8])
+    t = Tagged(rng.choice([6, 20, 60]), page, seqs, entries)
+    lens = [0] * seqs
+    for _ in range(25):
+        op = rng.choice(["reserve", "reserve", "reserve", "fork", "trim", "compact"])
+        if op == "reserve":
+            n = rng.randint(1, seqs)
+            last = [min(lens[b] + rng.choice([0, 1, 5, page, 2 * page]), entries * page) for b in range(n)]
+            got = t.reserve(lens[:n], last)
+            for b in range(n):
+                if got[b] > lens[b]:
+                    t.write(b, lens[b], got[b])
+                    lens[b] = got[b]
+        elif op == "fork":
+            order = rng.sample(range(seqs), seqs)
+            m = rng.randint(1, max(1, seqs // 2))
+            dst, src = order[:m], [rng.choice(order[m:]) for _ in range(m)]
+            t.fork(src, dst)
+            for s, d in zip(src, dst):
+                lens[d] = lens[s]
+        elif op == "trim":
+            keep = [rng.choice([-1, 0, rng.randint(0, lens[b])]) for b in range(seqs)]
+            t.trim(keep)
+            lens = [n if kp < 0 else min(n, kp) for n, kp in zip(lens, keep)]
+        else:
+            t.compact()
+        t.check()
+
+
+@pytest.mark.parametrize("n_pages", [1, 4095, 4096, 4097, 20001])
+def test_pools_of_many_pages(n_pages):
+    t = Tagged(n_pages, 16, 3, 2 * n_pages, layers=1, hkv=1)
+    most = n_pages * 16
+    t.reserve([0], [most // 2])
+    t.reserve([0, 0], [0, most])
+    assert t.cache.table.tolist() == t.model.table and t.cache.refs.tolist() == t.model.refs
+    t.trim([0, -1, -1])
+    t.compact()
+    assert t.cache.table.tolist() == t.model.table and t.cache.refs.tolist() == t.model.refs
+
+
+def test_many_sequences_at_once():
+    t = Tagged(3000, 16, 1100, 4, layers=1, hkv=1)
+    first = [0] * 1100
+    last = [(7 * b) % 60 for b in range(1100)]
+    t.reserve(first, last)
+    t.fork(list(range(100)) * 5, list(range(100, 600)))
+    t.reserve(last, [n + 9 for n in last])
+    t.trim([-1 if b % 3 else 0 for b in range(1100)])
+    t.compact()
+    assert t.cache.table.tolist() == t.model.table and t.cache.refs.tolist() == t.model.refs
+
+
+def test_entries_that_name_no_page_are_left_alone():
+    t = Tagged(8, 16, 2, 4)
+    t.reserve([0, 0], [40, 20])
+    t.write(0, 0, 40)
+    t.cache.table[1, 2] = 77
+    t.cache.table[1, 3] = -9
+    table = t.cache.table.clone()
+    t.trim([32, -1])
+    t.compact()
+    assert t.cache.table[1, 2:].tolist() == [77, -9] and t.cache.table[0].tolist()[:2] == table[0].tolist()[:2]
+    t.cache.fork([1], [0])
+    assert t.cache.table[0].tolist() == t.cache.table[1].tolist()
+    assert t.cache.refs.tolist()[:5].count(2) == 2 and int(t.cache.refs.sum()) == 4
+
+
+# ---- together, as a serving loop uses them ------------------------------------------------------------------
+
+class Serve:
+    """A few layers of append and attend over a cache, beside dense float64 caches."""
+
+    def __init__(self, dtype, h, hkv, hd, page, layers, seqs, entries, n_pages):
+        from paper_2511_09844_amd.paged import PagedCache
+        self.cache = PagedCache.empty(n_pages, page, layers, hkv, hd, seqs, entries, dtype)
+        self.dtype, self.h, self.hkv, self.hd, self.layers = dtype, h, hkv, hd, layers
+        self.dense = [[[] for _ in range(seqs)] for _ in range(layers)]
+        self.gen = torch.Generator("cuda").manual_seed(5)
+
+    def randn(self, *shape):
+        return torch.randn(shape, generator=self.gen, device="cuda").to(self.dtype)
+
+    def step(self, lens, rows, packed=True):
+        """rows[b] new positions of every sequence, up to lens[b]; every layer checked."""
+        ln, off = rows_of(lens, rows, packed)
+        first = torch.tensor([n - r for n, r in zip(lens, rows)], dtype=torch.int32, device="cuda")
+        assert self.cache.reserve(first, ln).tolist() == lens
+        total = sum(rows)
+        for layer in range(self.layers):
+            qkv = self.randn(total, self.h + 2 * self.hkv, self.hd)
+            q, k, v = qkv[:, : self.h], qkv[:, self.h: self.h + self.hkv], qkv[:, self.h + self.hkv:]
+            self.cache.append(k, v, ln, layer=layer, row_off=off, max_rows=max(rows))
+            got = self.cache.attend(q, ln, layer=layer, row_off=off, max_rows=max(rows))
+            at = 0
+            for b, r in enumerate(rows):
+                self.dense[layer][b] = self.dense[layer][b] + [(k[at + i].double(), v[at + i].double()) for i in range(r)]
+                at += r
+            ref, absv, spread = attend64(self.cache, q, lens, rows, layer)
+            assert ((got.double() - ref).abs() <= attend_bound(ref, absv, spread, self.dtype, max(lens), self.hd)).all()
+            for b, n in enumerate(lens):
+                entries = self.cache.table[b].tolist()
+                for j in range(0, n, 7):
+                    p, s = entries[j // self.cache.page_size], j % self.cache.page_size
+                    assert torch.equal(self.cache.k[p, layer, :, s].double(), self.dense[layer][b][j][0])
+                    assert torch.equal(self.cache.v[p, layer, :, s].double(), self.dense[layer][b][j][1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_serving_loop(dtype):
+    s = Serve(dtype, 8, 2, 64, 16, 2, 4, 12, 40)
+    s.step([50, 0, 21, 0], [50, 0, 21, 0])        # two prompts arrive
+    s.step([51, 0, 22, 0], [1, 0, 1, 0])
+    s.cache.fork([0, 0], [1, 3])                  # two more samples of the first
+    for layer in s.dense:
+        layer[1], layer[3] = list(layer[0]), list(layer[0])
+    s.step([52, 52, 23, 52], [1, 1, 1, 1], packed=False)
+    s.step([57, 57, 28, 57], [5, 5, 5, 5], packed=False)  # speculative blocks, rolled back to what was taken
+    taken = [54, 53, 28, 56]
+    s.cache.trim(torch.tensor(taken, dtype=torch.int32, device="cuda"))
+    for layer in s.dense:
+        for b, n in enumerate(taken):
+            layer[b] = layer[b][:n]
+    s.step([n + 1 for n in taken], [1] * 4, packed=False)
+    s.cache.trim(torch.tensor([0, -1, -1, -1], dtype=torch.int32, device="cuda"))  # the first one is done
+    for layer in s.dense:
+        layer[0] = []
+    s.cache.compact()
+    s.step([90, 55, 30, 58], [90, 1, 1, 1])       # a new prompt beside decoding sequences
+
+
+def _capture(fn):
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        fn()
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = fn()
+    return graph, out
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_captured_steps_follow_the_lengths(dtype):
+    """reserve, append and attend captured once and replayed while the lengths grow, eager work between."""
+    lens = [100, 37, 250]
+    cache = make_cache(lens, dtype, 2, 64, 16, extra_entries=4, spare=12)
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    first = ln - 1
+    q, k, v = queries(3, 8, 64, dtype, 7), queries(3, 2, 64, dtype, 8), queries(3, 2, 64, dtype, 9)
+    fixed = cache.max_pages * cache.page_size
+
+    def step():
+        granted = cache.reserve(first, ln)
+        cache.append(k, v, ln)
+        return granted, cache.attend(q, ln, max_len=fixed)
+
+    graph, (granted, out) = _capture(step)
+    for i in range(1, 30):
+        ln.add_(1)
+        first.add_(1)
+        for t, seed in ((q, 10), (k, 11), (v, 12)):
+            t.copy_(queries(3, t.shape[1], 64, dtype, 100 * i + seed))
+        graph.replay()
+        now = [n + i for n in lens]
+        assert granted.tolist() == now
+        ref, absv, spread = attend64(cache, q, now, [1, 1, 1])
+        assert ((out.double() - ref).abs() <= attend_bound(ref, absv, spread, dtype, max(now), 64)).all()
+        again = cache.attend(q, ln, max_len=fixed)
+        assert torch.equal(again, out), "a replay and an eager call differ"
+        torch.cuda.synchronize()
+
+
+def test_two_streams_at_once():
+    """Calls on two caches from two streams, none waiting for the other."""
+    lens = [3000, 1500, 700]
+    caches = [make_cache(lens, BF16, 2, 128, 64, seed=s) for s in (0, 1)]
+    qs = [queries(3, 8, 128, BF16, s) for s in (3, 4)]
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    want = [c.attend(q, ln) for c, q in zip(caches, qs)]
+    streams = [torch.cuda.Stream() for _ in caches]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(50):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(caches[i].attend(qs[i], ln))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(g, want[i]) for g in got[i])
