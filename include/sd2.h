@@ -267,7 +267,7 @@ typedef struct {
     int32_t page_size;  /* positions per page: 16, 32, 64, 128, 256, 512 or 1024 */
     int32_t n_pages;    /* 1..2^24 */
     int32_t max_seqs;   /* 1..SD2_PAGED_MAX_SEQS */
-    int32_t max_pages;  /* entries of a sequence; max_pages * page_size below 2^31 */
+    int32_t max_pages;  /* entries of a sequence; max_pages * page_size at most 2^30 */
     int32_t* table;     /* device [max_seqs][max_pages] */
     int32_t* refs;      /* device [n_pages] */
     int32_t n_arrays;   /* 1..SD2_PAGE_ARRAYS */

@@ -1,5 +1,24 @@
 // Causal grouped-query attention over a paged K/V cache.
+//
+// For few rows per sequence (decoding, speculative blocks): k_pdecode.  A query vector is a (row, head)
+// pair; those of one sequence and KV head read the same keys, so they are the 16 columns of a matrix
+// instruction (NT times 16 of them per wave), and both products are computed transposed,
+//   S^T = K Q^T   (16 keys x 16 query vectors)
+//   O^T += V^T P^T (16 columns of v x 16 query vectors, HD / 16 of them),
+// with the contraction index of the second one numbered as the result of the first lies in the
+// registers: lane group g holds keys 4 g + r of every 16.  So a lane holds one query vector's scores,
+// its running maximum and its part of the sums, the softmax needs one exchange over the four lane groups
+// per block of keys, and neither the weights nor K and V go through LDS: a lane loads rows of K and V
+// straight from the pages as operands.  bf16 V needs its columns' values of eight keys in one
+// register set: a lane loads HD / 16 neighbouring columns of its eight keys and permutes bytes.
+//
+// A page is looked up once per 16 keys (pages are multiples of 16 positions) and all lanes' loads of
+// those keys go through one buffer descriptor, whose size says how many of the 16 rows exist: rows behind
+// the last position and pages that are missing read as zeros, whatever lies there, and nothing
+// outside a page is ever addressed.
 #include <math.h>
+
+#include <algorithm>
 
 #include "device_common.h"
 #include "paged.h"
@@ -7,73 +26,459 @@
 
 namespace sd2 {
 
-template <typename T>
-__device__ __forceinline__ void paged_put1(const PagedAttnArgs& a, int row, int c, float v);
-template <>
-__device__ __forceinline__ void paged_put1<float>(const PagedAttnArgs& a, int row, int c, float v) {
-    if (a.planes) pg_put1(a.planes, a.Mp, row, c, v);
-    else ((float*)a.out)[row * a.out_stride + c] = v;
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Maximum and sum over the four 16-lane groups of a wave (lanes l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float col_max(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-template <>
-__device__ __forceinline__ void paged_put1<uint16_t>(const PagedAttnArgs& a, int row, int c, float v) {
-    const __bf16 h = (__bf16)v;
-    ((uint16_t*)a.out)[row * a.out_stride + c] = __builtin_bit_cast(uint16_t, h);
+__device__ __forceinline__ float col_sum(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// One wave per row and head, a key at a time.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_paged_attn(PagedAttnArgs a) {
-    constexpr int E = (HD + 63) / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row = blockIdx.x;
-    const int b = paged_seq(a.r, row);
-    int n;
-    const int r0 = paged_rows(a.r, b, n);
-    if (row < r0 || row >= r0 + n) return;
-    const int pos = paged_len(a.r, b, r0, n) - n + (row - r0);
-    const int G = a.H / a.c.Hkv;
-    for (int h = wave; h < a.H; h += 4) {
-        const int kvh = h / G;
-        float q[E], o[E], m = -INFINITY, l = 0.f;
-        for (int e = 0; e < E; ++e) {
-            const int d = lane + 64 * e;
-            q[e] = d < HD ? load_scalar<T>((const T*)a.q, row * a.q_stride + h * HD + d) * a.scale : 0.f;
-            o[e] = 0.f;
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
+    const f2 v = {x, y};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
+}
+
+// n neighbouring output values of a row (n columns from c, a multiple of n).
+template <typename T, int N>
+__device__ __forceinline__ void put(const PagedAttnArgs& a, int row, int c, const float* v) {
+    if constexpr (sizeof(T) == 2) {
+        uint16_t* p = (uint16_t*)a.out + row * a.out_stride + c;
+        if constexpr (N % 8 == 0) {
+#pragma unroll
+            for (int i = 0; i < N; i += 8)
+                *(u4*)(p + i) = u4{pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3]), pack_bf16(v[i + 4], v[i + 5]),
+                                   pack_bf16(v[i + 6], v[i + 7])};
+        } else {
+            static_assert(N == 4);
+            *(u2*)p = u2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
         }
-        for (int j = 0; j <= pos; ++j) {
-            const int p = paged_page(a.c, b, j >> a.c.shift);
-            if (p < 0) continue;
-            const int64_t at = p * a.c.page_stride + (((int64_t)kvh << a.c.shift) + (j & ((1 << a.c.shift) - 1))) * HD;
-            float s = 0.f;
-            for (int e = 0; e < E; ++e) {
-                const int d = lane + 64 * e;
-                if (d < HD) s += q[e] * load_scalar<T>((const T*)a.c.k, at + d);
-            }
-            s = wave_sum(s);
-            const float mn = fmaxf(m, s), w = expf(s - mn), f = m == -INFINITY ? 0.f : expf(m - mn);
-            m = mn;
-            l = l * f + w;
-            for (int e = 0; e < E; ++e) {
-                const int d = lane + 64 * e;
-                if (d < HD) o[e] = o[e] * f + w * load_scalar<T>((const T*)a.c.v, at + d);
-            }
-        }
-        for (int e = 0; e < E; ++e) {
-            const int d = lane + 64 * e;
-            if (d < HD) paged_put1<T>(a, row, h * HD + d, l > 0.f ? o[e] / l : 0.f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const float4 x = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+            if (a.planes) pg_put4(a.planes, a.Mp, row, c + i, x);
+            else *(float4*)((float*)a.out + row * a.out_stride + c + i) = x;
         }
     }
 }
 
-size_t paged_attn_bytes(const PagedView&, const PagedRows&, int, bool, int64_t) { return 256; }
+// The keys a workgroup of k_pdecode takes at a time, 16 or 32 per wave.
+template <typename T>
+constexpr int kBlockKeys = sizeof(T) == 2 ? 32 : 16;
+constexpr int kDecodeWaves = 4;
 
-hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t, void*, size_t, hipEvent_t, hipEvent_t) {
+struct DecodeArgs {
+    PagedAttnArgs a;
+    int ncg;         // groups of 16 NT query vectors of a sequence and KV head, at most
+    int nspan;       // workgroups that share a group's keys
+    float* part;     // partials: [group][span][16 NT][HD] sums, then [group][span][16 NT] (maximum, sum)
+    int64_t ml;      // floats of the first
+};
+
+// Keys of a span, and spans that have keys, of a sequence of n positions.
+template <typename T>
+__device__ __forceinline__ int span_keys(int n, int nspan, int& live) {
+    constexpr int step = kDecodeWaves * kBlockKeys<T>;
+    const int keys = max(((n + nspan - 1) / nspan + step - 1) / step * step, step);
+    live = (n + keys - 1) / keys;
+    return keys;
+}
+
+// One block of keys in registers, as loaded.
+template <typename T, int HD>
+struct Block {
+    static constexpr bool H = sizeof(T) == 2;
+    static constexpr int TK = H ? 2 : 1;              // tiles of 16 keys
+    static constexpr int NK = H ? HD / 32 : HD / 16;  // 16-byte loads of a row of K per lane
+    static constexpr int VW = H ? HD / 16 : HD / 16 < 4 ? HD / 16 : 4;  // neighbouring columns of V per lane
+    static constexpr int VU = HD / 16 / VW;
+    static constexpr int VD = VW * sizeof(T) / 4;     // dwords of them
+    typedef uint32_t vv __attribute__((ext_vector_type(VD)));
+    u4 k[TK][NK];
+    vv v[TK * 4][VU];
+};
+
+template <typename T, int HD>
+__device__ __forceinline__ void load_block(Block<T, HD>& x, const PagedView& c, int kvh, const int* page, int k0, int end,
+                                           int lane) {
+    using B = Block<T, HD>;
+    constexpr int RB = HD * sizeof(T);
+    const int n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < B::TK; ++t) {
+        const int key = k0 + 16 * t;
+        const int rows = page[t] < 0 ? 0 : max(min(end - key, 16), 0);
+        const int64_t at = (int64_t)max(page[t], 0) * c.page_stride + (((int64_t)kvh << c.shift) + (key & ((1 << c.shift) - 1))) * HD;
+        const auto rk = __builtin_amdgcn_make_buffer_rsrc((T*)c.k + at, 0, rows * RB, 0x00020000);
+        const auto rv = __builtin_amdgcn_make_buffer_rsrc((T*)c.v + at, 0, rows * RB, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < B::NK; ++i)
+            x.k[t][i] = __builtin_amdgcn_raw_buffer_load_b128(rk, n * RB + 16 * g + 64 * i, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int u = 0; u < B::VU; ++u) {
+                const int off = (4 * g + r) * RB + (u * 16 + n) * B::VW * (int)sizeof(T);
+                if constexpr (B::VD == 4) x.v[4 * t + r][u] = __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0);
+                else if constexpr (B::VD == 2) x.v[4 * t + r][u] = __builtin_amdgcn_raw_buffer_load_b64(rv, off, 0, 0);
+                else x.v[4 * t + r][u] = __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0);
+            }
+    }
+}
+
+template <typename T, int HD, int NT>
+struct Acc {
+    f4 o[NT][HD / 16];
+    float m[NT], l[NT];
+};
+
+template <typename T, int HD, int NT>
+__device__ __forceinline__ void block_step(const Block<T, HD>& x, const u4 (&q)[NT][Block<T, HD>::NK], Acc<T, HD, NT>& acc,
+                                           const int* page, int k0, const int (&pos)[NT], bool whole, float scale, int lane) {
+    using B = Block<T, HD>;
+    const int g = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        f4 s[B::TK];
+#pragma unroll
+        for (int t = 0; t < B::TK; ++t) {
+            s[t] = f4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (B::H) {
+#pragma unroll
+                for (int i = 0; i < B::NK; ++i)
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, x.k[t][i]),
+                                                                   __builtin_bit_cast(b8, q[j][i]), s[t], 0, 0, 0);
+            } else {
+                f4 s1 = s[t];  // two chains
+#pragma unroll
+                for (int i = 0; i < B::NK; ++i) {
+                    const f4 kk = __builtin_bit_cast(f4, x.k[t][i]), qq = __builtin_bit_cast(f4, q[j][i]);
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[e], qq[e], s[t], 0, 0, 0);
+                        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[e + 1], qq[e + 1], s1, 0, 0, 0);
+                    }
+                }
+                s[t] += s1;
+            }
+            s[t] *= scale;
+            if (!whole)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[t][r] = page[t] >= 0 && k0 + 16 * t + 4 * g + r <= pos[j] ? s[t][r] : -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < B::TK; ++t) mx = fmaxf(mx, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
+        mx = fmaxf(acc.m[j], col_max(mx));
+        // (nothing readable yet: the maximum is -inf, and every weight 0)
+        const float base = mx == -INFINITY ? 0.f : mx;
+        if (__any(mx != acc.m[j])) {
+            const float f = __builtin_amdgcn_exp2f(acc.m[j] - base);
+            acc.l[j] *= f;
+#pragma unroll
+            for (int i = 0; i < HD / 16; ++i) acc.o[j][i] *= f;
+            acc.m[j] = mx;
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < B::TK; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[t][r] = __builtin_amdgcn_exp2f(s[t][r] - base);
+                sum += s[t][r];
+            }
+        acc.l[j] += sum;
+        if constexpr (B::H) {
+            // the weights as bf16, the type of the matrix instruction that v enters as it is: half a step of
+            // 2^-8 each, as much as the output's own rounding
+            const b8 p = __builtin_bit_cast(b8, u4{pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]),
+                                                   pack_bf16(s[1][0], s[1][1]), pack_bf16(s[1][2], s[1][3])});
+#pragma unroll
+            for (int i = 0; i < HD / 16; ++i) {
+                u4 w;
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    w[d] = __builtin_amdgcn_perm(x.v[2 * d + 1][0][i / 2], x.v[2 * d][0][i / 2], i % 2 ? 0x07060302 : 0x05040100);
+                acc.o[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, w), p, acc.o[j][i], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int u = 0; u < B::VU; ++u)
+#pragma unroll
+                    for (int e = 0; e < B::VW; ++e)
+                        acc.o[j][u * B::VW + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[r][u][e]), s[0][r],
+                                                                                     acc.o[j][u * B::VW + e], 0, 0, 0);
+        }
+    }
+}
+
+// Query vector v of a sequence and KV head: row v / G of the sequence, head kvh * G + v % G.
+template <typename T, int HD, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_pdecode(DecodeArgs d) {
+    using B = Block<T, HD>;
+    constexpr int QV = 16 * NT, BK = kBlockKeys<T>;
+    __shared__ __attribute__((aligned(16))) f4 os[2][NT * (HD / 16)][64];
+    __shared__ float ms[kDecodeWaves][QV][2];
+    const PagedAttnArgs& a = d.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, g = lane >> 4;
+    // groups of one sequence and KV head that read the same keys lie on one XCD (workgroups go round
+    // them in turn)
+    const int units = a.r.nseq * a.c.Hkv * d.nspan, units8 = (units + 7) / 8 * 8;
+    const int cg = blockIdx.x / units8, unit = blockIdx.x % units8;
+    if (unit >= units) return;
+    const int span = unit % d.nspan, kvh = unit / d.nspan % a.c.Hkv, b = unit / d.nspan / a.c.Hkv;
+    const int G = a.H / a.c.Hkv;
+    int nrows;
+    const int r0 = paged_rows(a.r, b, nrows);
+    const int nqv = nrows * G, v0 = cg * QV;
+    if (v0 >= nqv) return;
+    const int len = paged_len(a.r, b, r0, nrows);
+    // positions that some row of this group reads
+    const int last = len - nrows + min(v0 + QV - 1, nqv - 1) / G;
+    const int end = min(last + 1, (int64_t)a.c.max_pages << a.c.shift);
+    int live;
+    const int keys = span_keys<T>(max(end, 0), d.nspan, live);
+    const int64_t group = ((int64_t)b * a.c.Hkv + kvh) * d.ncg + cg;
+    if (span >= max(live, 1)) return;
+    const int kb = span * keys, ke = min(end, kb + keys);
+    u4 q[NT][B::NK];
+    int pos[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int v = v0 + 16 * j + n, row = min(v, nqv - 1) / G, h = kvh * G + min(v, nqv - 1) % G;
+        pos[j] = len - nrows + row;
+        const T* p = (const T*)a.q + (r0 + row) * a.q_stride + h * HD + g * (16 / (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < B::NK; ++i) q[j][i] = *(const u4*)(p + i * (64 / (int)sizeof(T)));
+    }
+    const int first = len - nrows + v0 / G;  // of the group's rows
+    const float scale = a.scale * kLog2e;
+    Acc<T, HD, NT> acc;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        acc.m[j] = -INFINITY;
+        acc.l[j] = 0.f;
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) acc.o[j][i] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+    auto look = [&](int k0, int (&page)[B::TK]) {
+#pragma unroll
+        for (int t = 0; t < B::TK; ++t)
+            page[t] = k0 + 16 * t < ke ? __builtin_amdgcn_readfirstlane(paged_page(a.c, b, (k0 + 16 * t) >> a.c.shift)) : -1;
+    };
+    constexpr int step = kDecodeWaves * BK;
+    int k0 = kb + wave * BK;
+    Block<T, HD> x[2];
+    int page[3][B::TK];
+    look(k0, page[0]);
+    look(k0 + step, page[1]);
+    load_block<T, HD>(x[0], a.c, kvh, page[0], k0, ke, lane);
+    for (; k0 < ke; k0 += 2 * step) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int k = k0 + i * step;
+            if (k >= ke) break;
+            look(k + 2 * step, page[2]);
+            load_block<T, HD>(x[1 - i], a.c, kvh, page[1], k + step, ke, lane);
+            bool whole = k + BK - 1 <= min(first, ke - 1);
+#pragma unroll
+            for (int t = 0; t < B::TK; ++t) whole &= page[0][t] >= 0;
+            block_step<T, HD, NT>(x[i], q, acc, page[0], k, pos, whole, scale, lane);
+#pragma unroll
+            for (int t = 0; t < B::TK; ++t) {
+                page[0][t] = page[1][t];
+                page[1][t] = page[2][t];
+            }
+        }
+    }
+    // the waves' parts on one maximum, then added
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        acc.l[j] = col_sum(acc.l[j]);
+        if (g == 0) {
+            ms[wave][16 * j + n][0] = acc.m[j];
+            ms[wave][16 * j + n][1] = acc.l[j];
+        }
+    }
+    __syncthreads();
+    float mt[NT], lt[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kDecodeWaves; ++w) m = fmaxf(m, ms[w][16 * j + n][0]);
+        mt[j] = m;
+        const float base = m == -INFINITY ? 0.f : m;
+        lt[j] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kDecodeWaves; ++w) lt[j] += ms[w][16 * j + n][1] * __builtin_amdgcn_exp2f(ms[w][16 * j + n][0] - base);
+        const float f = __builtin_amdgcn_exp2f(acc.m[j] - base);
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) acc.o[j][i] *= f;
+    }
+#pragma unroll
+    for (int half = 2; half > 0; half /= 2) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < HD / 16; ++i) os[wave - half][j * (HD / 16) + i][lane] = acc.o[j][i];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < HD / 16; ++i) acc.o[j][i] += os[wave][j * (HD / 16) + i][lane];
+        __syncthreads();
+    }
+    if (wave) return;
+    // a lane holds, of query vector n, columns (16 u + 4 g + r) VW + e for r < 4, e < VW
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int v = v0 + 16 * j + n;
+        const float inv = d.nspan > 1 ? 1.f : lt[j] > 0.f ? 1.f / lt[j] : 0.f;
+#pragma unroll
+        for (int u = 0; u < B::VU; ++u) {
+            float y[4 * B::VW];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < B::VW; ++e) y[r * B::VW + e] = acc.o[j][u * B::VW + e][r] * inv;
+            const int c = (16 * u + 4 * g) * B::VW;
+            if (d.nspan > 1) {
+                float* p = d.part + ((group * d.nspan + span) * QV + 16 * j + n) * HD + c;
+#pragma unroll
+                for (int i = 0; i < 4 * B::VW; i += 4) *(f4*)(p + i) = f4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+            } else if (v < nqv) {
+                put<T, 4 * B::VW>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
+            }
+        }
+        if (d.nspan > 1 && g == 0) {
+            float* p = d.part + d.ml + ((group * d.nspan + span) * QV + 16 * j + n) * 2;
+            *(f2*)p = f2{mt[j], lt[j]};
+        }
+    }
+}
+
+// The spans of a group joined: a thread per query vector and 4 columns.
+template <typename T, int HD, int NT>
+__global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
+    constexpr int QV = 16 * NT, PER = 256 / (HD / 4);
+    const PagedAttnArgs& a = d.a;
+    const int nb = (QV + PER - 1) / PER;
+    const int64_t group = blockIdx.x / nb;
+    const int i = blockIdx.x % nb * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4;
+    const int cg = group % d.ncg, kvh = group / d.ncg % a.c.Hkv, b = group / d.ncg / a.c.Hkv, G = a.H / a.c.Hkv;
+    int nrows;
+    const int r0 = paged_rows(a.r, b, nrows);
+    const int nqv = nrows * G, v0 = cg * QV, v = v0 + i;
+    if (i >= QV || v >= nqv) return;
+    const int len = paged_len(a.r, b, r0, nrows);
+    const int end = min(len - nrows + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift);
+    int live;
+    span_keys<T>(max(end, 0), d.nspan, live);
+    live = max(live, 1);
+    const float* po = d.part + (group * d.nspan * QV + i) * HD + c;
+    const float* pm = d.part + d.ml + (group * d.nspan * QV + i) * 2;
+    float m = -INFINITY, l = 0.f;
+    f4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < live; s0 += 8) {
+        f2 ml[8];
+        f4 x[8];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const int64_t k = (int64_t)min(s0 + s, live - 1) * QV;
+            ml[s] = *(const f2*)(pm + k * 2);
+            x[s] = *(const f4*)(po + k * HD);
+        }
+        float mn = m;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) mn = fmaxf(mn, ml[s][0]);
+        const float base = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m - base);
+        l *= f;
+        o *= f;
+        m = mn;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float w = s0 + s < live ? __builtin_amdgcn_exp2f(ml[s][0] - base) : 0.f;
+            l += w * ml[s][1];
+            o += w * x[s];
+        }
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    put<T, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
+}
+
+struct DecodePlan {
+    int nt, ncg, nspan;
+    int64_t groups, ml;  // floats of the sums
+};
+
+DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
+    DecodePlan p;
+    const int qv = std::min<int64_t>((int64_t)r.max_rows * (H / c.Hkv), 1 << 20);
+    p.nt = qv <= 16 ? 1 : 2;
+    p.ncg = (qv + 16 * p.nt - 1) / (16 * p.nt);
+    p.groups = (int64_t)std::max(r.nseq, 1) * c.Hkv * p.ncg;
+    const int64_t step = kDecodeWaves * (bf16 ? 32 : 16), most = std::min<int64_t>((max_len + step - 1) / step, 128);
+    p.nspan = (int)std::max<int64_t>(1, std::min<int64_t>(most, (1024 + p.groups - 1) / p.groups));
+    p.ml = p.groups * p.nspan * 16 * p.nt * c.hd;
+    return p;
+}
+
+template <typename T, int HD, int NT>
+hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p, float* ws) {
+    const DecodeArgs d{a, p.ncg, p.nspan, ws, p.ml};
+    const int64_t units8 = ((int64_t)a.r.nseq * a.c.Hkv * p.nspan + 7) / 8 * 8;
+    if (units8 * p.ncg > INT32_MAX) return hipErrorInvalidValue;
+    const hipError_t err = launch(k_pdecode<T, HD, NT>, dim3((unsigned)(units8 * p.ncg)), dim3(256), s, d);
+    if (err != hipSuccess || p.nspan == 1) return err;
+    constexpr int per = 256 / (HD / 4), nb = (16 * NT + per - 1) / per;
+    return launch(k_pjoin<T, HD, NT>, dim3((unsigned)(p.groups * nb)), dim3(256), s, d);
+}
+
+template <typename T, int HD>
+hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws) {
+    const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len);
+    return p.nt == 1 ? run_decode<T, HD, 1>(s, a, p, ws) : run_decode<T, HD, 2>(s, a, p, ws);
+}
+
+}  // namespace
+
+size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
+    const DecodePlan p = decode_plan(c, r, H, bf16, max_len);
+    return p.nspan == 1 ? 256 : (size_t)(p.ml + p.groups * p.nspan * 16 * p.nt * 2) * 4;
+}
+
+hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t, hipEvent_t,
+                      hipEvent_t) {
     if (!a.r.total_rows || !a.r.nseq) return hipSuccess;
-    const dim3 grid(a.r.total_rows), block(256);
     switch (a.c.hd) {
-        case 32: return launch(bf16 ? k_paged_attn<uint16_t, 32> : k_paged_attn<float, 32>, grid, block, s, a);
-        case 64: return launch(bf16 ? k_paged_attn<uint16_t, 64> : k_paged_attn<float, 64>, grid, block, s, a);
-        case 128: return launch(bf16 ? k_paged_attn<uint16_t, 128> : k_paged_attn<float, 128>, grid, block, s, a);
+        case 32: return bf16 ? decode<uint16_t, 32>(s, a, max_len, (float*)ws) : decode<float, 32>(s, a, max_len, (float*)ws);
+        case 64: return bf16 ? decode<uint16_t, 64>(s, a, max_len, (float*)ws) : decode<float, 64>(s, a, max_len, (float*)ws);
+        case 128: return bf16 ? decode<uint16_t, 128>(s, a, max_len, (float*)ws) : decode<float, 128>(s, a, max_len, (float*)ws);
         default: return hipErrorInvalidValue;
     }
 }

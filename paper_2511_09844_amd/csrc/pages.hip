@@ -338,7 +338,7 @@ hipError_t copy_listed(hipStream_t s, const sd2_pages& p, const PageList& l, boo
 
 bool pages_ok(const sd2_pages* p) {
     if (!p || shift_of(p->page_size) < 0 || p->n_pages < 1 || p->n_pages > 1 << 24 || p->max_seqs < 1 ||
-        p->max_seqs > SD2_PAGED_MAX_SEQS || p->max_pages < 1 || (int64_t)p->max_pages * p->page_size > INT32_MAX ||
+        p->max_seqs > SD2_PAGED_MAX_SEQS || p->max_pages < 1 || (int64_t)p->max_pages * p->page_size > 1 << 30 ||
         !aligned(p->table, 4) || !aligned(p->refs, 4) || p->n_arrays < 1 || p->n_arrays > SD2_PAGE_ARRAYS)
         return false;
     for (int i = 0; i < p->n_arrays; ++i) {
@@ -417,7 +417,7 @@ bool view_of(const sd2_paged_kv* kv, PagedView* c, int* size) {
     const int shift = shift_of(kv->page_size);
     if (shift < 0 || kv->n_pages < 1 || kv->n_pages > 1 << 24 || kv->n_kv_heads < 1 || kv->n_kv_heads > 1024 ||
         (kv->head_dim != 32 && kv->head_dim != 64 && kv->head_dim != 128) || kv->max_pages < 1 ||
-        (int64_t)kv->max_pages * kv->page_size > INT32_MAX || !aligned(kv->k, 16) || !aligned(kv->v, 16) ||
+        (int64_t)kv->max_pages * kv->page_size > 1 << 30 || !aligned(kv->k, 16) || !aligned(kv->v, 16) ||
         !aligned(kv->table, 4))
         return false;
     if (kv->page_stride < (int64_t)kv->n_kv_heads * kv->page_size * kv->head_dim || kv->page_stride % (16 / *size) ||

@@ -119,6 +119,8 @@ def test_attn_and_append_arguments_refused():
     assert attn(lib, c, none, q=None, out=None) == 0
     assert lib.sd2_paged_append(ctypes.byref(c), ctypes.byref(none), None, 0, None, 0, None) == 0
     assert attn(lib, c, rows(total_rows=0, row_off=AT)) == 0
+    for r in (none, rows(total_rows=0, row_off=AT), rows(nseq=0, total_rows=0, row_off=AT, max_rows=2 ** 31 - 1)):
+        assert lib.sd2_paged_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(r), 8, 64) > 0
 
 
 def test_paged_struct_layouts_match_the_header(tmp_path):
