@@ -180,6 +180,28 @@ sd2_status sd2_create_mlp(const sd2_config* cfg, const sd2_weights* verifier, co
                           void* hip_stream, sd2_handle_t* out);
 
 /*
+ * Create a handle whose K/V caches lie in pages (see "Paged K/V caches" below): instead of max_seq_len
+ * rows for each of max_batch sequences the workspace holds n_pages pages, each of page_size positions in every
+ * layer of both models.  Sequences take pages as they grow and give them up when they finish;
+ * sd2_fork lets sequences share a common beginning, sd2_release frees one, sd2_compact moves the
+ * pages in use together.  cfg->steering must be SD2_STEER_INPUT or SD2_STEER_NONE; rounds run one kernel per
+ * operation; everything else is as sd2_create, with sd2_create_paged_bytes for sd2_workspace_bytes.
+ * sd2_prefill returns SD2_ERR_CAPACITY when batch * ceil((max_prompt - 1) / page_size) exceeds n_pages.
+ * A sequence that the pool cannot give the pages of a round sits it out: its out_counts entry is 0, its
+ * state is kept (SD2_DBG_STATE: done = 2), and it goes on in a later round that finds pages, which finished
+ * sequences have left; when none can go on, the caller has to release one.  sd2_train_loss returns
+ * SD2_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    int32_t page_size;  /* 16, 32, 64, 128, 256, 512 or 1024 */
+    int32_t n_pages;    /* 1..2^24 */
+} sd2_paging;
+size_t sd2_create_paged_bytes(const sd2_config* cfg, const sd2_paging* paging);
+sd2_status sd2_create_paged(const sd2_config* cfg, const sd2_weights* verifier, const sd2_weights* drafter,
+                            const void* w_steer, const sd2_paging* paging, void* workspace, size_t workspace_bytes,
+                            void* hip_stream, sd2_handle_t* out);
+
+/*
  * Prefill `batch` sequences (1..max_batch) with their prompts.
  * tokens: device int32 [batch][max_prompt], row b holding lens[b] prompt ids in [0, vocab);
  * lens: device int32 [batch], each in [1, max_prompt]; max_prompt: host bound on lens.
@@ -200,6 +222,20 @@ sd2_status sd2_prefill(sd2_handle_t h, int32_t batch, const int32_t* tokens, con
  * Returns SD2_ERR_STATE before sd2_prefill.
  */
 sd2_status sd2_round(sd2_handle_t h, int32_t* out_tokens, int32_t* out_counts);
+
+/*
+ * Calls on a running generation of a paged handle (SD2_ERR_UNSUPPORTED on any other, SD2_ERR_STATE
+ * before sd2_prefill), between rounds.
+ * sd2_fork: `count` further sequences go on from sequence seq (0 .. number of sequences - 1) as it is now,
+ *   sharing its pages until they write to them; they are the next count sequences, in the rounds'
+ *   outputs too (SD2_ERR_CAPACITY beyond max_batch).  They draw random numbers of their own.
+ * sd2_release: sequence seq is finished now and gives up its pages; its number stays taken.
+ * sd2_compact: the pages in use are moved to the front of the pool; live (device int32 [1], or NULL)
+ *   receives their number.
+ */
+sd2_status sd2_fork(sd2_handle_t h, int32_t seq, int32_t count);
+sd2_status sd2_release(sd2_handle_t h, int32_t seq);
+sd2_status sd2_compact(sd2_handle_t h, int32_t* live);
 
 /*
  * Test hook: like sd2_round, but the trajectory follows caller-supplied decisions.
@@ -381,7 +417,8 @@ const char* sd2_last_error(sd2_handle_t h);
 #define SD2_DBG_OWN_DRAFTS 4  /* int32 [batch][k]: drafts the library drew itself last round */
 #define SD2_DBG_OWN_N 5       /* int32 [batch]: accepted count the library computed itself */
 #define SD2_DBG_OWN_Y 6       /* int32 [batch]: final token the library drew itself */
-#define SD2_DBG_STATE 7       /* int32 [batch][5]: t, len_verifier, len_drafter, produced, done */
+#define SD2_DBG_STATE 7       /* int32 [batch][5]: t, len_verifier, len_drafter, produced, done (2: without pages
+                                 in the last round) */
 #define SD2_DBG_HIST 8        /* int32 [batch][max_seq_len]: committed tokens */
 #define SD2_DBG_HIDDEN_V 9    /* float [batch][k+1][d_verifier]: last verify pass's final-norm hidden states */
 #define SD2_DBG_PATH 10       /* int32 [2]: round execution path (0: one kernel per operation, 1: one persistent
@@ -398,6 +435,9 @@ const char* sd2_last_error(sd2_handle_t h);
 #define SD2_DBG_NONFINITE 13  /* int32 [1]: 1 if a verifier or drafter logit of a round since the last read of
                                  this selector was a NaN or an infinity (every logit the round's decisions use
                                  is checked as the sampler reads it), else 0; the read clears it */
+
+#define SD2_DBG_REFS 14       /* int32 [n_pages]: table entries that name each page; SD2_ERR_STATE without pages */
+#define SD2_DBG_TABLE 15      /* int32 [max_batch][ceil(max_seq_len / page_size)]: the page table (-1: none) */
 
 /* Copy a debug buffer of the last round into host memory dst (bytes must match). */
 sd2_status sd2_debug_read(sd2_handle_t h, int32_t what, void* dst_host, size_t bytes);

@@ -16,13 +16,14 @@ P = ctypes.c_void_p
 SD2_OK = 0
 STATUS = {0: "ok", -1: "invalid argument", -2: "capacity", -3: "state", -4: "hip error", -5: "unsupported"}
 DBG_LOGITS_V, DBG_LOGITS_D, DBG_STEER, DBG_OWN_DRAFTS, DBG_OWN_N, DBG_OWN_Y, DBG_STATE, DBG_HIST, DBG_HIDDEN_V, DBG_PATH, \
-    DBG_TRACE, DBG_UBIAS, DBG_NONFINITE = range(1, 14)
+    DBG_TRACE, DBG_UBIAS, DBG_NONFINITE, DBG_REFS, DBG_TABLE = range(1, 16)
 
 EXPORTS = ["sd2_workspace_bytes", "sd2_create", "sd2_create_noalloc", "sd2_create_mlp", "sd2_train_loss",
            "sd2_train_loss_scratch_bytes", "sd2_prefill", "sd2_round", "sd2_round_forced", "sd2_destroy",
            "sd2_status_string", "sd2_last_error", "sd2_debug_read", "sd2_profile", "sd2_profile_read",
            "sd2_pages_workspace_bytes", "sd2_pages_reserve", "sd2_pages_fork", "sd2_pages_trim", "sd2_pages_compact",
-           "sd2_paged_append", "sd2_paged_attn_workspace_bytes", "sd2_paged_attn"]
+           "sd2_paged_append", "sd2_paged_attn_workspace_bytes", "sd2_paged_attn", "sd2_create_paged_bytes",
+           "sd2_create_paged", "sd2_fork", "sd2_release", "sd2_compact"]
 PROF_GEMV, PROF_ATTN, PROF_SAMPLER, PROF_OTHER, PROF_PROGRAM = 1, 2, 3, 4, 5
 
 
@@ -49,6 +50,10 @@ STEER_INPUT, STEER_MLP, STEER_MLP_OUT, STEER_NONE, STEER_MLP_COND = 0, 1, 2, 3, 
 class MlpSteering(ctypes.Structure):
     _fields_ = [("w_s", P), ("w_hml", P), ("ln_gain", P), ("ln_bias", P), ("ln_eps", ctypes.c_float),
                 ("w_cf", P), ("w_cu", P)]
+
+
+class Paging(ctypes.Structure):
+    _fields_ = [("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32)]
 
 
 PAGE_ARRAYS, PAGED_MAX_SEQS = 8, 4096
@@ -137,6 +142,17 @@ def load():
         lib.sd2_paged_attn_workspace_bytes.restype = ctypes.c_size_t
         lib.sd2_paged_attn.argtypes = [kv, rows, P, i64, P, i64, i32, ctypes.c_float, i32, P, ctypes.c_size_t, P]
         lib.sd2_paged_attn.restype = i32
+        lib.sd2_create_paged_bytes.argtypes = [ctypes.POINTER(Config), ctypes.POINTER(Paging)]
+        lib.sd2_create_paged_bytes.restype = ctypes.c_size_t
+        lib.sd2_create_paged.argtypes = [ctypes.POINTER(Config), ctypes.POINTER(Weights), ctypes.POINTER(Weights), P,
+                                         ctypes.POINTER(Paging), P, ctypes.c_size_t, P, ctypes.POINTER(P)]
+        lib.sd2_create_paged.restype = i32
+        lib.sd2_fork.argtypes = [P, i32, i32]
+        lib.sd2_fork.restype = i32
+        lib.sd2_release.argtypes = [P, i32]
+        lib.sd2_release.restype = i32
+        lib.sd2_compact.argtypes = [P, P]
+        lib.sd2_compact.restype = i32
         _lib = lib
     return _lib
 
@@ -201,10 +217,11 @@ class Engine:
 
     With `mlp` (a dict of device tensors w_s, w_hml, ln_gain, ln_bias and a float ln_eps) the
     handle is created by sd2_create_mlp (cfg.steering STEER_MLP or STEER_MLP_OUT) and `w_steer` is
-    unused; with cfg.steering STEER_NONE (the unsteered drafter) `w_steer` may be None."""
+    unused; with cfg.steering STEER_NONE (the unsteered drafter) `w_steer` may be None.  With `paging`
+    = (page_size, n_pages) its caches lie in pages (sd2_create_paged)."""
 
     def __init__(self, cfg: Config, verifier: DeviceModel, drafter: DeviceModel, w_steer: torch.Tensor,
-                 stream=None, device="cuda", mlp=None, noalloc=False):
+                 stream=None, device="cuda", mlp=None, noalloc=False, paging=None):
         lib = load()
         self.lib = lib
         self.cfg = cfg
@@ -212,7 +229,12 @@ class Engine:
         self.w_steer = w_steer
         self.mlp = mlp
         self.stream = stream if stream is not None else torch.cuda.current_stream()
-        nbytes = lib.sd2_workspace_bytes(ctypes.byref(cfg))
+        self.paging = None if paging is None else Paging(*paging)
+        if paging is None:
+            nbytes = lib.sd2_workspace_bytes(ctypes.byref(cfg))
+        else:
+            assert mlp is None and not noalloc
+            nbytes = lib.sd2_create_paged_bytes(ctypes.byref(cfg), ctypes.byref(self.paging))
         if nbytes == 0:
             raise Sd2Error("invalid configuration")
         self.h = P()
@@ -228,7 +250,12 @@ class Engine:
             self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
             base = self.workspace.data_ptr()
             off = (-base) % 256
-            if mlp is None:
+            if paging is not None:
+                rc = lib.sd2_create_paged(ctypes.byref(cfg), ctypes.byref(verifier.w), ctypes.byref(drafter.w), ws_ptr,
+                                          ctypes.byref(self.paging), base + off, nbytes, self.stream.cuda_stream,
+                                          ctypes.byref(self.h))
+                check(rc, None, "sd2_create_paged")
+            elif mlp is None:
                 rc = lib.sd2_create(ctypes.byref(cfg), ctypes.byref(verifier.w), ctypes.byref(drafter.w), ws_ptr,
                                     base + off, nbytes, self.stream.cuda_stream, ctypes.byref(self.h))
                 check(rc, None, "sd2_create")
@@ -278,6 +305,22 @@ class Engine:
         check(rc, self.h, "sd2_round")
         return self.out_tokens[: self.batch], self.out_counts[: self.batch]
 
+    def fork(self, seq: int, count: int = 1):
+        """Paged handles: `count` further sequences go on from sequence seq, as the next ones."""
+        check(self.lib.sd2_fork(self.h, seq, count), self.h, "sd2_fork")
+        self.batch += count
+
+    def release(self, seq: int):
+        """Paged handles: sequence seq is finished and gives up its pages."""
+        check(self.lib.sd2_release(self.h, seq), self.h, "sd2_release")
+
+    def compact(self) -> torch.Tensor:
+        """Paged handles: the pages in use are moved together; returns their number (device int32 [1])."""
+        live = torch.zeros(1, dtype=torch.int32, device=self.out_counts.device)
+        self._live = live
+        check(self.lib.sd2_compact(self.h, live.data_ptr()), self.h, "sd2_compact")
+        return live
+
     def train_loss(self, tokens: torch.Tensor, deltas: torch.Tensor, rows_per_chunk: int = 512):
         """Training-objective forward (sd2_train_loss) over one device token sequence and its
         offsets: returns (mean KL over targets 1..n-1, per-target KL as numpy [n]).  The handle's
@@ -307,6 +350,9 @@ class Engine:
             DBG_OWN_Y: ((B,), np.int32), DBG_STATE: ((B, 5), np.int32),
             DBG_HIST: ((B, self.cfg.max_seq_len), np.int32), DBG_HIDDEN_V: ((B, k + 1, dV), np.float32),
             DBG_PATH: ((2,), np.int32), DBG_TRACE: ((33, 1024), np.int64), DBG_NONFINITE: ((1,), np.int32),
+            DBG_REFS: ((self.paging.n_pages if self.paging else 0,), np.int32),
+            DBG_TABLE: ((self.cfg.max_batch, -(-self.cfg.max_seq_len // self.paging.page_size) if self.paging else 0),
+                        np.int32),
             DBG_UBIAS: (((B, self.cfg.drafter.n_layers, self.cfg.drafter.d_ff) if self.cfg.steering == STEER_MLP
                          else (B, self.cfg.drafter.n_layers, self.cfg.cond_rank)
                          if self.cfg.steering == STEER_MLP_COND else (B, self.cfg.drafter.d_model)), np.float32),

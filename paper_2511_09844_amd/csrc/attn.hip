@@ -636,6 +636,21 @@ static void launch_pattn(Engine& e, hipStream_t s, AttnArgs a) {
 
 void launch_attn(Engine& e, hipStream_t s, ModelDev& m, int layer, int rows, int rps, const float* q, int q_stride) {
     const sd2_dims& dm = m.dm;
+    if (e.paged) {
+        PagedAttnArgs p{};
+        p.c = paged_view(e.pages, e.ws.pg_table, m, layer);
+        p.r = PagedRows{rows / rps, rps, rows, e.live_off, nullptr, e.ws.row_pos};
+        p.q = q; p.q_stride = q_stride; p.out = e.ws.attn; p.out_stride = dm.n_heads * m.hd;
+        p.planes = e.ws.planes ? (uint16_t*)e.ws.attn : nullptr;
+        p.Mp = pg_rows(rows);
+        p.H = dm.n_heads;
+        p.scale = 1.0f / sqrtf((float)m.hd);
+        prof_begin(&e, kProfAttn, 0.0);
+        const hipError_t err = paged_attn(s, p, false, e.cap, e.ws.attn_part, e.ws.attn_part_n * sizeof(float));
+        prof_end(&e);
+        if (err != hipSuccess) e.launch_err = err;
+        return;
+    }
     AttnArgs a{};
     a.q = q; a.q_stride = q_stride; a.kc = m.kc; a.vc = m.vc; a.out = e.ws.attn;
     a.planes = e.ws.planes ? (uint16_t*)e.ws.attn : nullptr;

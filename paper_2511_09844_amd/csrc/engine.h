@@ -5,6 +5,7 @@
 
 #include "../../include/sd2.h"
 #include "mk.h"
+#include "paged.h"
 
 namespace sd2 {
 
@@ -24,7 +25,7 @@ struct ModelDev {
     const void* final_norm;
     const void* lm_head;
     // workspace-resident
-    float* kc;                        // K cache [layer][batch][kv_head][cap][hd]
+    float* kc;                        // K cache [layer][batch][kv_head][cap][hd]; paged: [page][layer][kv_head][slot][hd]
     float* vc;                        // V cache, same layout
     float* rope_cos;                  // [cap][hd/2]
     float* rope_sin;
@@ -101,6 +102,11 @@ struct Workspace {
                             // bias: the g parts V_l^g g, L_D x R)
     float* cond_h;          // conditional bias: [2 max_batch][R] hidden layer of the drafter rows
     float* cond_b;          // conditional bias: [2 max_batch][F_D] one layer's bias of the drafter rows
+    // paged caches (sd2_create_paged; else null)
+    int32_t *pg_table, *pg_refs;  // [max_batch][max_pages], [n_pages]
+    int32_t *pg_first, *pg_last, *pg_granted, *pg_trim;  // [max_batch] arguments of the page calls
+    int32_t* steer_out;     // [max_batch] row that a sequence's steering goes to: its own, or -1 (keep the old one)
+    void* pg_ws;
 };
 
 // Per-launch timing entries (HIP events recorded on the engine's stream).
@@ -142,6 +148,8 @@ struct Engine {
     bool prof_on;
     int prof_n;
     ProfEntry* prof;
+    bool paged;             // caches in pages (one kernel per operation)
+    sd2_pages pages;        // both models' caches: a page holds the positions of every layer of both
     MkState mk;  // persistent round-program path (used when active)
     bool static_slot;   // created by sd2_create_noalloc: workspace and this object are static
     int static_device;  // its device
@@ -164,8 +172,24 @@ void prof_commit(Engine* e);
 // as far as the total stays within the static size, and small_part_room() at least, by which the
 // set of configurations that fit is fixed; the plans split K as far as they have room.
 enum WsForm { kWsFull, kWsSmall };
+// paging (or null): caches in pages, which *pages is made for.
 size_t carve(const sd2_config& c, char* base, Workspace* ws, ModelDev* mv, ModelDev* md, int* maxm,
-             MkState* mk = nullptr, WsForm form = kWsFull);
+             MkState* mk = nullptr, WsForm form = kWsFull, const sd2_paging* paging = nullptr, sd2_pages* pages = nullptr);
+// Layer `layer` of a model's paged caches.
+inline PagedView paged_view(const sd2_pages& p, const int32_t* table, const ModelDev& m, int layer) {
+    PagedView v{};
+    const int64_t per = (int64_t)m.dm.n_kv_heads * p.page_size * m.hd;
+    v.k = m.kc + layer * per;
+    v.v = m.vc + layer * per;
+    v.page_stride = m.dm.n_layers * per;
+    v.n_pages = p.n_pages;
+    v.shift = __builtin_ctz(p.page_size);
+    v.Hkv = m.dm.n_kv_heads;
+    v.hd = m.hd;
+    v.table = table;
+    v.max_pages = p.max_pages;
+    return v;
+}
 
 // ---- launchers (kernels.hip) ----
 void launch_rope_table(hipStream_t s, ModelDev& m, int cap);
@@ -183,7 +207,9 @@ void launch_layer(hipStream_t s, Engine& e, ModelDev& m, int layer, int rows, in
 void launch_cond_bias(hipStream_t s, Engine& e, int layer, int rows);
 // Final-norm LM head of `rows` residual rows into Y[out_map[r]] (bf16 path via the projection kernel).
 void launch_lm_head(Engine& e, ModelDev& m, int rows, float* Y, const int32_t* out_map);
-void launch_steer(Engine& e, const float* X, const float* ss, const int32_t* in_map, int rows);
+// out_map (null: the row itself) maps rows to sequences.
+void launch_steer(Engine& e, const float* X, const float* ss, const int32_t* in_map, int rows,
+                  const int32_t* out_map = nullptr);
 // MLP steering: copy the verifier residual rows after `layer` to the tap slots taken there.
 void launch_tap_copy(hipStream_t s, Engine& e, int layer, int rows);
 // Prefill: keep the tap rows at position len-2 of every sequence (slots taken after `layer`).
@@ -216,6 +242,7 @@ struct WsCall {
     const float *rcos, *rsin;
     float *qout, *kc, *vc;
     int cap, max_batch, layer;
+    PagedView paged;         // table not null: the caches lie in pages (kc, vc unused)
     const int32_t* m_live;   // rows that hold data, of M (on the device; null: all of them)
     const uint16_t* planes;  // X as planes, times the gain (else made from X)
     uint16_t* yplanes;       // planes of the output (see PgArgs), with the gain ygamma
@@ -250,6 +277,13 @@ void launch_prefill_finish(hipStream_t s, Engine& e, int batch, const int32_t* p
 void launch_rmsnorm_rows(hipStream_t s, const float* X, int rows, int d, const void* gamma, bool bf16, float eps,
                          float* Y);
 void launch_set_flag(hipStream_t s, int32_t* flag, int v);
+// Paged caches: pages of the prompts; pages of the positions that the next round writes (a sequence that
+// the pool cannot give them sits the round out); a sequence's state copied to those behind it; one given up.
+hipError_t launch_prefill_pages(hipStream_t s, Engine& e, int batch, const int32_t* prompt_len, int max_prompt);
+hipError_t launch_round_pages(hipStream_t s, Engine& e);
+hipError_t launch_fork(hipStream_t s, Engine& e, int seq, int count);
+hipError_t launch_release(hipStream_t s, Engine& e, int seq);
+void launch_init_pages(hipStream_t s, Engine& e);
 
 // Training-objective forward (sd2_train_loss): buffers carved from the caller's scratch.
 struct LossScratch {

@@ -117,6 +117,14 @@ WsForm ws_form(const sd2_config& c) {
                : kWsFull;
 }
 
+// A paged handle's workspace has no other form that it would have to agree with.
+WsForm paged_form(const sd2_config& c) { return c.dtype == SD2_F32 ? kWsSmall : kWsFull; }
+
+bool paging_ok(const sd2_paging* p) {
+    if (!p || p->n_pages < 1 || p->n_pages > 1 << 24) return false;
+    return p->page_size >= 16 && p->page_size <= 1024 && (p->page_size & (p->page_size - 1)) == 0;
+}
+
 int max_rows(const sd2_config& c, int prefill) {
     int B = c.max_batch;
     return std::max(std::max(B * (c.k + 1), 2 * B), prefill);
@@ -133,7 +141,7 @@ void model_dims(ModelDev* m, const sd2_dims& d) {
 namespace sd2 {
 
 size_t carve(const sd2_config& c, char* base, Workspace* ws, ModelDev* mv, ModelDev* md, int* maxm_out,
-             MkState* mk, WsForm form) {
+             MkState* mk, WsForm form, const sd2_paging* paging, sd2_pages* pages) {
     Carver cv{base};
     int B = c.max_batch, k = c.k, cap = c.max_seq_len, V = c.verifier.vocab;
     int maxm = max_rows(c, form == kWsFull ? kPrefillRows : kPrefillRowsSmall);
@@ -172,7 +180,7 @@ size_t carve(const sd2_config& c, char* base, Workspace* ws, ModelDev* mv, Model
     w.hidden_dbg = cv.take<float>((size_t)B * (k + 1) * c.verifier.d_model);
     w.part = cv.take<VPart>((size_t)B * (2 * k + 1) * kVocabChunks);
     static_assert(kVocabChunks * sizeof(VPart) >= 2 * sizeof(int32_t), "B + 1 offsets fit the sampler's partials");
-    if (planes) w.row_off = (int32_t*)w.part;
+    if (planes || paging) w.row_off = (int32_t*)w.part;
     w.lse_v = cv.take<float>((size_t)B * (k + 1));
     w.lse_d = cv.take<float>((size_t)B * k);
     w.argmax_v = cv.take<int32_t>((size_t)B * (k + 1));
@@ -290,7 +298,8 @@ size_t carve(const sd2_config& c, char* base, Workspace* ws, ModelDev* mv, Model
     for (int i = 0; i < 2; ++i) {
         ModelDev* m = ms[i];
         const sd2_dims& d = m->dm;
-        size_t kv = (size_t)d.n_layers * B * d.n_kv_heads * cap * m->hd;
+        const size_t rows = paging ? (size_t)paging->n_pages * paging->page_size : (size_t)B * cap;
+        size_t kv = (size_t)d.n_layers * d.n_kv_heads * rows * m->hd;
         m->kc = cv.take<float>(kv);
         m->vc = cv.take<float>(kv);
         m->rope_cos = cv.take<float>((size_t)cap * (m->hd / 2));
@@ -298,10 +307,31 @@ size_t carve(const sd2_config& c, char* base, Workspace* ws, ModelDev* mv, Model
         m->x = cv.take<float>((size_t)maxm * d.d_model);
         m->ss = cv.take<float>((size_t)maxm * (d.d_model / 16));
     }
+    if (paging) {
+        sd2_pages p{};
+        p.page_size = paging->page_size;
+        p.n_pages = paging->n_pages;
+        p.max_seqs = B;
+        p.max_pages = (cap + p.page_size - 1) / p.page_size;
+        w.pg_table = p.table = cv.take<int32_t>((size_t)B * p.max_pages);
+        w.pg_refs = p.refs = cv.take<int32_t>(p.n_pages);
+        w.pg_first = cv.take<int32_t>(B);
+        w.pg_last = cv.take<int32_t>(B);
+        w.pg_granted = cv.take<int32_t>(B);
+        w.pg_trim = cv.take<int32_t>(B);
+        w.steer_out = cv.take<int32_t>(B);
+        p.n_arrays = 4;
+        for (int i = 0; i < 4; ++i) {
+            const ModelDev* m = ms[i / 2];
+            p.arrays[i] = sd2_page_array{i % 2 ? m->vc : m->kc, m->dm.n_layers * m->dm.n_kv_heads, m->hd * (int32_t)sizeof(float)};
+        }
+        w.pg_ws = cv.take<char>(pages_bytes(p));
+        if (pages) *pages = p;
+    }
     // persistent round-program path: phase lists, activation arena, barrier and hand-off state
     {
         MkState st{};
-        st.max_batch = mk_max_batch(c);
+        st.max_batch = paging ? 0 : mk_max_batch(c);
         if (st.max_batch > 0) {
             st.prog_cap = mk_phase_count(c);
             st.prog = cv.take<MkPhase>((size_t)st.prog_cap);
@@ -388,6 +418,10 @@ sd2_status check_launch(Engine* e, const char* where) {
 void enqueue_round(Engine& e, int32_t* out_tokens, int32_t* out_counts) {
     hipStream_t s = e.stream;
     e.prof_n = 0;
+    if (e.paged) {
+        const hipError_t err = launch_round_pages(s, e);
+        if (err != hipSuccess) { e.launch_err = err; return; }
+    }
     int B = e.batch, k = e.cfg.k;
     if (e.mk.active) {
         // one persistent launch per drafter step and one for the verifier block
@@ -435,7 +469,7 @@ void enqueue_round(Engine& e, int32_t* out_tokens, int32_t* out_counts) {
         const float* src[3] = {e.ws.taps, e.ws.taps + slot, e.ws.taps + 2 * slot};
         launch_mlp_steer(e, src, e.ws.steer_map, B);
     } else if (e.w_steer) {
-        launch_steer(e, e.mv.x, e.mv.ss, e.ws.steer_map, B);
+        launch_steer(e, e.mv.x, e.mv.ss, e.ws.steer_map, B, e.paged ? e.ws.steer_out : nullptr);
     }
 }
 
@@ -542,7 +576,7 @@ static bool weights_ok(const sd2_weights* w, const sd2_dims& d) {
 static sd2_status create_impl(const sd2_config* cfg, const sd2_weights* verifier, const sd2_weights* drafter,
                               const void* w_steer, const sd2_mlp_steering* mlp, void* workspace,
                               size_t workspace_bytes, void* hip_stream, sd2_handle_t* out,
-                              StaticSlot* slot = nullptr) {
+                              StaticSlot* slot = nullptr, const sd2_paging* paging = nullptr) {
     if (!out) return SD2_ERR_INVALID_ARG;
     *out = nullptr;
     if (!config_ok(cfg)) return SD2_ERR_INVALID_ARG;
@@ -554,8 +588,8 @@ static sd2_status create_impl(const sd2_config* cfg, const sd2_weights* verifier
     const bool unsteered = cfg->steering == SD2_STEER_NONE;
     if (!unsteered && !aligned16(w_steer)) return SD2_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace % kAlign) != 0) return SD2_ERR_INVALID_ARG;
-    const WsForm form = ws_form(*cfg);
-    const size_t need = carve(*cfg, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, form);
+    const WsForm form = paging ? paged_form(*cfg) : ws_form(*cfg);
+    const size_t need = carve(*cfg, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, form, paging);
     if (workspace_bytes < need) return SD2_ERR_INVALID_ARG;
     // the kernels are built for gfx950 with XNACK (page-fault replay) off, MI355X's default mode
     {
@@ -606,7 +640,8 @@ static sd2_status create_impl(const sd2_config* cfg, const sd2_weights* verifier
     }
     // Graph replay needs a capturable (non-null) stream; SD2_NO_GRAPH=1 forces eager launches.
     e->use_graph = hip_stream != nullptr && getenv("SD2_NO_GRAPH") == nullptr;
-    carve(*cfg, (char*)workspace, &e->ws, &e->mv, &e->md, &e->maxm, &e->mk, form);
+    carve(*cfg, (char*)workspace, &e->ws, &e->mv, &e->md, &e->maxm, &e->mk, form, paging, &e->pages);
+    e->paged = paging != nullptr;
     const sd2_weights* src[2] = {verifier, drafter};
     ModelDev* dst[2] = {&e->mv, &e->md};
     for (int i = 0; i < 2; ++i) {
@@ -633,6 +668,7 @@ static sd2_status create_impl(const sd2_config* cfg, const sd2_weights* verifier
     launch_rope_table(e->stream, e->md, e->cap);
     launch_init_maps(e->stream, *e);
     mk_init_buffers(*e);
+    if (paging) launch_init_pages(e->stream, *e);
     sd2_status st = check_launch(e, "create");
     if (st != SD2_OK) {
         if (!slot) delete e;
@@ -646,6 +682,21 @@ sd2_status sd2_create(const sd2_config* cfg, const sd2_weights* verifier, const 
                       const void* w_steer, void* workspace, size_t workspace_bytes, void* hip_stream,
                       sd2_handle_t* out) {
     return create_impl(cfg, verifier, drafter, w_steer, nullptr, workspace, workspace_bytes, hip_stream, out);
+}
+
+size_t sd2_create_paged_bytes(const sd2_config* cfg, const sd2_paging* paging) {
+    if (!config_ok(cfg) || mlp_form(*cfg) || !paging_ok(paging)) return 0;
+    return carve(*cfg, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, paged_form(*cfg), paging);
+}
+
+sd2_status sd2_create_paged(const sd2_config* cfg, const sd2_weights* verifier, const sd2_weights* drafter,
+                            const void* w_steer, const sd2_paging* paging, void* workspace, size_t workspace_bytes,
+                            void* hip_stream, sd2_handle_t* out) {
+    if (!out) return SD2_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!paging_ok(paging)) return SD2_ERR_INVALID_ARG;
+    return create_impl(cfg, verifier, drafter, w_steer, nullptr, workspace, workspace_bytes, hip_stream, out, nullptr,
+                       paging);
 }
 
 // Training-objective forward: buffers for sequences of n tokens in chunks of `chunk` positions.
@@ -680,7 +731,7 @@ sd2_status sd2_train_loss(sd2_handle_t h, const int32_t* tokens, const int32_t* 
                           size_t scratch_bytes) {
     if (!h || !tokens || !deltas || !out_kl || !out_loss || !scratch) return SD2_ERR_INVALID_ARG;
     Engine* e = reinterpret_cast<Engine*>(h);
-    if (e->cfg.steering != SD2_STEER_INPUT) return SD2_ERR_UNSUPPORTED;
+    if (e->cfg.steering != SD2_STEER_INPUT || e->paged) return SD2_ERR_UNSUPPORTED;
     if (n < 2 || rows_per_chunk < 1 || rows_per_chunk > kPrefillRowsSmall) return SD2_ERR_INVALID_ARG;
     if (n > e->cap) return SD2_ERR_CAPACITY;
     if ((uintptr_t)scratch % kAlign || scratch_bytes < loss_carve(e->cfg, n, rows_per_chunk, nullptr, nullptr))
@@ -738,6 +789,11 @@ sd2_status sd2_prefill(sd2_handle_t h, int32_t batch, const int32_t* tokens, con
     Engine* e = reinterpret_cast<Engine*>(h);
     if (batch < 1 || batch > e->cfg.max_batch || !tokens || !lens || max_prompt < 1) return SD2_ERR_INVALID_ARG;
     if ((int64_t)max_prompt + e->cfg.max_new_tokens + e->cfg.k + 1 > e->cap) return SD2_ERR_CAPACITY;
+    if (e->paged) {
+        // every prompt's pages, whatever the lengths are
+        const int64_t per = (max_prompt - 1 + e->pages.page_size - 1) / e->pages.page_size;
+        if (per * batch > e->pages.n_pages) return SD2_ERR_CAPACITY;
+    }
     hipStream_t s = e->stream;
     e->batch = batch;
     int chunk = std::max(1, std::min(max_prompt - 1, e->prefill_rows / batch));
@@ -746,7 +802,10 @@ sd2_status sd2_prefill(sd2_handle_t h, int32_t batch, const int32_t* tokens, con
     hipError_t err = hipMemsetAsync(e->ws.hcap, 0, sizeof(float) * (size_t)batch * e->mv.dm.d_model, s);
     if (err != hipSuccess) return hip_fail(e, err, "hipMemsetAsync");
     // several prompts: the rows a chunk has of each are packed, and the launches cover only those
-    e->live_off = batch > 1 ? e->ws.row_off : nullptr;
+    // (always in pages, whose attention goes by a sequence's last row)
+    e->live_off = batch > 1 || e->paged ? e->ws.row_off : nullptr;
+    if (e->paged && (err = launch_prefill_pages(s, *e, batch, lens, max_prompt)) != hipSuccess)
+        return hip_fail(e, err, "prefill pages");
     for (int c = 0; c < nchunks; ++c) {
         launch_plan_embed(s, *e, e->mv, kPlanPrefill, c, rows, tokens, lens, max_prompt, chunk);
         for (int l = 0; l < e->mv.dm.n_layers; ++l) {
@@ -795,6 +854,45 @@ sd2_status sd2_round_forced(sd2_handle_t h, const int32_t* forced, int32_t* out_
     sd2_status st = check_launch(e, "round_forced");
     if (st != SD2_OK) return st;
     return run_round(e, out_tokens, out_counts);
+}
+
+// What the calls on a running paged generation have in common.
+static sd2_status paged_handle(sd2_handle_t h, Engine** e) {
+    if (!h) return SD2_ERR_INVALID_ARG;
+    *e = reinterpret_cast<Engine*>(h);
+    if (!(*e)->paged) return SD2_ERR_UNSUPPORTED;
+    return (*e)->prefilled ? SD2_OK : SD2_ERR_STATE;
+}
+
+sd2_status sd2_fork(sd2_handle_t h, int32_t seq, int32_t count) {
+    Engine* e;
+    sd2_status st = paged_handle(h, &e);
+    if (st != SD2_OK) return st;
+    if (seq < 0 || seq >= e->batch || count < 1) return SD2_ERR_INVALID_ARG;
+    if (count > e->cfg.max_batch - e->batch) return SD2_ERR_CAPACITY;
+    const hipError_t err = launch_fork(e->stream, *e, seq, count);
+    if (err != hipSuccess) return hip_fail(e, err, "fork");
+    if ((st = check_launch(e, "fork")) == SD2_OK) e->batch += count;
+    return st;
+}
+
+sd2_status sd2_release(sd2_handle_t h, int32_t seq) {
+    Engine* e;
+    sd2_status st = paged_handle(h, &e);
+    if (st != SD2_OK) return st;
+    if (seq < 0 || seq >= e->batch) return SD2_ERR_INVALID_ARG;
+    const hipError_t err = launch_release(e->stream, *e, seq);
+    if (err != hipSuccess) return hip_fail(e, err, "release");
+    return check_launch(e, "release");
+}
+
+sd2_status sd2_compact(sd2_handle_t h, int32_t* live) {
+    Engine* e;
+    sd2_status st = paged_handle(h, &e);
+    if (st != SD2_OK) return st;
+    const hipError_t err = pages_compact(e->stream, e->pages, live, e->ws.pg_ws);
+    if (err != hipSuccess) return hip_fail(e, err, "compact");
+    return check_launch(e, "compact");
 }
 
 sd2_status sd2_destroy(sd2_handle_t h) {
@@ -889,6 +987,16 @@ sd2_status sd2_debug_read(sd2_handle_t h, int32_t what, void* dst_host, size_t b
         case SD2_DBG_HIDDEN_V: src = e->ws.hidden_dbg; want = sizeof(float) * (size_t)B * (k + 1) * e->mv.dm.d_model; break;
         case SD2_DBG_PATH: want = sizeof(int32_t) * 2; break;
         case SD2_DBG_NONFINITE: src = e->ws.nonfinite; want = sizeof(int32_t); break;
+        case SD2_DBG_REFS:
+            if (!e->paged) return SD2_ERR_STATE;
+            src = e->ws.pg_refs;
+            want = sizeof(int32_t) * (size_t)e->pages.n_pages;
+            break;
+        case SD2_DBG_TABLE:
+            if (!e->paged) return SD2_ERR_STATE;
+            src = e->ws.pg_table;
+            want = sizeof(int32_t) * (size_t)e->pages.max_seqs * e->pages.max_pages;
+            break;
         case SD2_DBG_TRACE:
             if (!e->mk.trace) return SD2_ERR_STATE;
             src = e->mk.trace;

@@ -407,7 +407,7 @@ struct RopeArgs {
     int qkv_dim, H, Hkv, hd, cap, max_batch, layer;
     const int32_t *row_pos, *row_seq;
     const float *cosv, *sinv;
-    float *kc, *vc;
+    float *kc, *vc;  // null: k is rotated in place as well, and appended by the caller
 };
 
 __global__ __launch_bounds__(128) void k_rope_append(RopeArgs a) {
@@ -431,12 +431,13 @@ __global__ __launch_bounds__(128) void k_rope_append(RopeArgs a) {
     size_t base = ((size_t)a.layer * a.max_batch + b) * a.Hkv;
     for (int idx = threadIdx.x; idx < a.Hkv * half; idx += blockDim.x) {
         int h = idx / half, i = idx % half;
-        const float* kh = k + h * a.hd;
+        float* kh = k + h * a.hd;
         float x0 = kh[i], x1 = kh[i + half], c = cr[i], sn = sr[i];
-        float* dst = a.kc + ((base + h) * a.cap + pos) * a.hd;
+        float* dst = a.kc ? a.kc + ((base + h) * a.cap + pos) * a.hd : kh;
         dst[i] = x0 * c - x1 * sn;
         dst[i + half] = x1 * c + x0 * sn;
     }
+    if (!a.kc) return;
     for (int idx = threadIdx.x; idx < a.Hkv * a.hd; idx += blockDim.x) {
         int h = idx / a.hd, i = idx % a.hd;
         a.vc[((base + h) * a.cap + pos) * a.hd + i] = v[idx];
@@ -481,6 +482,7 @@ void launch_layer(hipStream_t s, Engine& e, ModelDev& m, int layer, int rows, in
         c.H = H; c.Hkv = Hkv; c.hd = hd; c.row_pos = e.ws.row_pos; c.row_seq = e.ws.row_seq;
         c.rcos = m.rope_cos; c.rsin = m.rope_sin; c.qout = e.ws.qkv; c.kc = m.kc; c.vc = m.vc;
         c.cap = e.cap; c.max_batch = e.cfg.max_batch; c.layer = layer;
+        if (e.paged) c.paged = paged_view(e.pages, e.ws.pg_table, m, layer);
         launch_wsgemv(&e, s, c);
         launch_attn(e, s, m, layer, rows, rps, e.ws.qkv, H * hd);
         // O projection + residual (+ slice sums of squares for the FFN norm)
@@ -517,9 +519,16 @@ void launch_layer(hipStream_t s, Engine& e, ModelDev& m, int layer, int rows, in
         RopeArgs a;
         a.qkv = e.ws.qkv; a.qkv_dim = m.qkv_dim; a.H = H; a.Hkv = Hkv; a.hd = hd; a.cap = e.cap;
         a.max_batch = e.cfg.max_batch; a.layer = layer; a.row_pos = e.ws.row_pos; a.row_seq = e.ws.row_seq;
-        a.cosv = m.rope_cos; a.sinv = m.rope_sin; a.kc = m.kc; a.vc = m.vc;
+        a.cosv = m.rope_cos; a.sinv = m.rope_sin; a.kc = e.paged ? nullptr : m.kc; a.vc = m.vc;
         prof_begin(&e, kProfOther, 0.0);
         k_rope_append<<<rows, 128, 0, s>>>(a);
+        if (e.paged) {
+            const float* k = e.ws.qkv + H * hd;
+            const PagedRows r{rows / rps, rps, rows, e.live_off, nullptr, e.ws.row_pos};
+            const hipError_t err = paged_append(s, paged_view(e.pages, e.ws.pg_table, m, layer), r, k, m.qkv_dim,
+                                                k + Hkv * hd, m.qkv_dim, sizeof(float));
+            if (err != hipSuccess) e.launch_err = err;
+        }
         prof_end(&e);
     }
     launch_attn(e, s, m, layer, rows, rps, e.ws.qkv, m.qkv_dim);
@@ -559,19 +568,115 @@ void launch_lm_head(Engine& e, ModelDev& m, int rows, float* Y, const int32_t* o
                 kEpiStore, Y, m.dm.vocab, out_map);
 }
 
-void launch_steer(Engine& e, const float* X, const float* ss, const int32_t* in_map, int rows) {
+void launch_steer(Engine& e, const float* X, const float* ss, const int32_t* in_map, int rows, const int32_t* out_map) {
     if (e.bf16) {
         WsCall c = ws_base(e, e.mv);
         c.X = X; c.in_map = in_map; c.M = rows; c.K = e.mv.dm.d_model; c.gamma = e.mv.final_norm; c.ss = ss;
         c.W[0] = e.w_steer; c.seg_rows[0] = e.md.dm.d_model; c.nseg = 1; c.mode = kEpiStore;
-        c.Y = e.ws.steer; c.ldy = e.md.dm.d_model;
+        c.Y = e.ws.steer; c.ldy = e.md.dm.d_model; c.out_map = out_map;
         launch_wsgemv(&e, e.stream, c);
         return;
     }
     const void* ws[1] = {e.w_steer};
     int rws[1] = {e.md.dm.d_model};
     launch_gemv(&e, e.stream, e.bf16, X, in_map, rows, e.mv.dm.d_model, e.mv.final_norm, e.mv.dm.rms_eps, ws, rws,
-                1, kEpiStore, e.ws.steer, e.md.dm.d_model, nullptr);
+                1, kEpiStore, e.ws.steer, e.md.dm.d_model, out_map);
+}
+
+// ===========================================================================
+// Paged caches: what the page calls of a prefill and of a round are asked for, and what a fork copies.
+// A page holds its positions in every layer of both models, so one table serves both; the verifier and
+// the drafter differ by at most one cached position.
+// ===========================================================================
+__global__ void k_init_pages(int32_t* table, int entries) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < entries) table[i] = -1;
+}
+void launch_init_pages(hipStream_t s, Engine& e) {
+    const int n = e.pages.max_seqs * e.pages.max_pages;
+    k_init_pages<<<(n + 255) / 256, 256, 0, s>>>(e.ws.pg_table, n);
+}
+
+__global__ void k_prefill_pages(int batch, int max_batch, const int32_t* prompt_len, int max_prompt, int32_t* first,
+                                int32_t* last, int32_t* trim) {
+    for (int b = threadIdx.x; b < max_batch; b += blockDim.x) {
+        first[b] = 0;
+        last[b] = b < batch ? min(max(prompt_len[b], 1), max_prompt) - 1 : 0;
+        trim[b] = 0;
+    }
+}
+hipError_t launch_prefill_pages(hipStream_t s, Engine& e, int batch, const int32_t* prompt_len, int max_prompt) {
+    const int mb = e.cfg.max_batch;
+    k_prefill_pages<<<1, 256, 0, s>>>(batch, mb, prompt_len, max_prompt, e.ws.pg_first, e.ws.pg_last, e.ws.pg_trim);
+    const hipError_t err = pages_trim(s, e.pages, mb, e.ws.pg_trim);
+    return err != hipSuccess ? err : pages_reserve(s, e.pages, batch, e.ws.pg_first, e.ws.pg_last, nullptr,
+                                                   e.ws.pg_granted, e.ws.pg_ws);
+}
+
+// Positions min(len_v, len_d) .. t + k - 1 are what a round writes; finished sequences give up their pages.
+__global__ void k_round_pages(int batch, int k, int cap, const int32_t* t, const int32_t* len_v, const int32_t* len_d,
+                              const int32_t* done, int32_t* first, int32_t* last, int32_t* trim) {
+    const int b = threadIdx.x;
+    if (b >= batch) return;
+    const bool over = done[b] == 1;
+    first[b] = over ? 0 : min(len_v[b], len_d[b]);
+    last[b] = over ? 0 : min(t[b] + k, cap);
+    trim[b] = over ? 0 : -1;
+}
+// done = 2: no pages for this round; such a sequence keeps its steering and is tried again next time.
+__global__ void k_round_stall(int batch, const int32_t* last, const int32_t* granted, int32_t* done, int32_t* steer_out) {
+    const int b = threadIdx.x;
+    if (b >= batch) return;
+    int d = done[b];
+    if (d != 1) done[b] = d = granted[b] < last[b] ? 2 : 0;
+    steer_out[b] = d == 2 ? -1 : b;
+}
+hipError_t launch_round_pages(hipStream_t s, Engine& e) {
+    static_assert(SD2_PAGED_MAX_SEQS >= 256, "a handle's sequences fit");
+    Workspace& w = e.ws;
+    prof_begin(&e, kProfOther, 0.0);
+    k_round_pages<<<1, 256, 0, s>>>(e.batch, e.cfg.k, e.cap, w.t, w.len_v, w.len_d, w.done, w.pg_first, w.pg_last, w.pg_trim);
+    hipError_t err = pages_trim(s, e.pages, e.batch, w.pg_trim);
+    if (err == hipSuccess)
+        err = pages_reserve(s, e.pages, e.batch, w.pg_first, w.pg_last, nullptr, w.pg_granted, w.pg_ws);
+    if (err == hipSuccess) k_round_stall<<<1, 256, 0, s>>>(e.batch, w.pg_last, w.pg_granted, w.done, w.steer_out);
+    prof_end(&e);
+    return err;
+}
+
+__global__ __launch_bounds__(256) void k_fork_state(int seq, int to, int32_t* t, int32_t* len_v, int32_t* len_d,
+                                                    int32_t* produced, int32_t* done, int32_t* hist, int cap, float* steer,
+                                                    int dD) {
+    const int b = to + blockIdx.x;
+    for (int i = threadIdx.x; i < cap; i += 256) hist[(size_t)b * cap + i] = hist[(size_t)seq * cap + i];
+    for (int i = threadIdx.x; i < dD; i += 256) steer[(size_t)b * dD + i] = steer[(size_t)seq * dD + i];
+    if (threadIdx.x == 0) {
+        t[b] = t[seq];
+        len_v[b] = len_v[seq];
+        len_d[b] = len_d[seq];
+        produced[b] = produced[seq];
+        done[b] = done[seq];
+    }
+}
+hipError_t launch_fork(hipStream_t s, Engine& e, int seq, int count) {
+    int32_t src[256], dst[256];
+    for (int i = 0; i < count; ++i) {
+        src[i] = seq;
+        dst[i] = e.batch + i;
+    }
+    Workspace& w = e.ws;
+    k_fork_state<<<count, 256, 0, s>>>(seq, e.batch, w.t, w.len_v, w.len_d, w.produced, w.done, w.hist, e.cap, w.steer,
+                                       e.md.dm.d_model);
+    return pages_fork(s, e.pages, count, src, dst);
+}
+
+__global__ void k_release(int seq, int max_batch, int32_t* done, int32_t* trim) {
+    for (int b = threadIdx.x; b < max_batch; b += blockDim.x) trim[b] = b == seq ? 0 : -1;
+    if (threadIdx.x == 0) done[seq] = 1;
+}
+hipError_t launch_release(hipStream_t s, Engine& e, int seq) {
+    k_release<<<1, 256, 0, s>>>(seq, e.cfg.max_batch, e.ws.done, e.ws.pg_trim);
+    return pages_trim(s, e.pages, e.batch, e.ws.pg_trim);
 }
 
 // ===========================================================================

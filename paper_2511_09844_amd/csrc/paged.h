@@ -24,7 +24,7 @@ struct PagedRows {
     int32_t nseq, max_rows, total_rows;
     const int32_t* row_off;
     const int32_t* lens;     // or null: one more than the position of the sequence's last row
-    const int32_t* row_pos;  // (lens null) [total_rows]
+    const int32_t* row_pos;  // (lens null) [total_rows]; paged_append leaves out rows at -1
 };
 
 struct PagedAttnArgs {
@@ -42,8 +42,8 @@ struct PagedAttnArgs {
 // Workspace of a call, and the call.  max_len: the largest length expected.  bf16: of q, the cache
 // and out (else fp32).
 size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len);
-hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t ws_bytes,
-                      hipEvent_t e0 = nullptr, hipEvent_t e1 = nullptr);
+// With less than that the keys are split less.
+hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t ws_bytes);
 
 // k, v rows [total_rows][Hkv][hd] (row strides in elements) into their pages; size: bytes of an element.
 hipError_t paged_append(hipStream_t s, const PagedView& c, const PagedRows& r, const void* k, int64_t k_stride,

@@ -436,7 +436,8 @@ struct DecodePlan {
     int64_t groups, ml;  // floats of the sums
 };
 
-DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
+// room: floats of partials.
+DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t room) {
     DecodePlan p;
     const int qv = std::min<int64_t>((int64_t)r.max_rows * (H / c.Hkv), 1 << 20);
     p.nt = qv <= 16 ? 1 : 2;
@@ -444,6 +445,8 @@ DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16,
     p.groups = (int64_t)std::max(r.nseq, 1) * c.Hkv * p.ncg;
     const int64_t step = kDecodeWaves * (bf16 ? 32 : 16), most = std::min<int64_t>((max_len + step - 1) / step, 128);
     p.nspan = (int)std::max<int64_t>(1, std::min<int64_t>(most, (1024 + p.groups - 1) / p.groups));
+    const size_t per = (size_t)p.groups * 16 * p.nt * (c.hd + 2);
+    if (p.nspan > 1 && per * p.nspan > room) p.nspan = (int)std::max<size_t>(1, room / per);
     p.ml = p.groups * p.nspan * 16 * p.nt * c.hd;
     return p;
 }
@@ -460,25 +463,26 @@ hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p
 }
 
 template <typename T, int HD>
-hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws) {
-    const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len);
+hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws, size_t room) {
+    const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, room);
     return p.nt == 1 ? run_decode<T, HD, 1>(s, a, p, ws) : run_decode<T, HD, 2>(s, a, p, ws);
 }
 
 }  // namespace
 
 size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
-    const DecodePlan p = decode_plan(c, r, H, bf16, max_len);
+    const DecodePlan p = decode_plan(c, r, H, bf16, max_len, SIZE_MAX);
     return p.nspan == 1 ? 256 : (size_t)(p.ml + p.groups * p.nspan * 16 * p.nt * 2) * 4;
 }
 
-hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t, hipEvent_t,
-                      hipEvent_t) {
+hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t ws_bytes) {
+    float* const w = (float*)ws;
+    const size_t room = ws_bytes / sizeof(float);
     if (!a.r.total_rows || !a.r.nseq) return hipSuccess;
     switch (a.c.hd) {
-        case 32: return bf16 ? decode<uint16_t, 32>(s, a, max_len, (float*)ws) : decode<float, 32>(s, a, max_len, (float*)ws);
-        case 64: return bf16 ? decode<uint16_t, 64>(s, a, max_len, (float*)ws) : decode<float, 64>(s, a, max_len, (float*)ws);
-        case 128: return bf16 ? decode<uint16_t, 128>(s, a, max_len, (float*)ws) : decode<float, 128>(s, a, max_len, (float*)ws);
+        case 32: return bf16 ? decode<uint16_t, 32>(s, a, max_len, w, room) : decode<float, 32>(s, a, max_len, w, room);
+        case 64: return bf16 ? decode<uint16_t, 64>(s, a, max_len, w, room) : decode<float, 64>(s, a, max_len, w, room);
+        case 128: return bf16 ? decode<uint16_t, 128>(s, a, max_len, w, room) : decode<float, 128>(s, a, max_len, w, room);
         default: return hipErrorInvalidValue;
     }
 }

@@ -32,7 +32,7 @@ __global__ __launch_bounds__(256) void k_paged_append(AppendArgs a) {
     int n;
     const int r0 = paged_rows(a.r, b, n);
     if (row < r0 || row >= r0 + n) return;
-    const int pos = paged_len(a.r, b, r0, n) - n + (row - r0);
+    const int pos = a.r.row_pos ? a.r.row_pos[row] : paged_len(a.r, b, r0, n) - n + (row - r0);
     if (pos < 0) return;
     const int page = paged_page(a.c, b, pos >> a.c.shift);
     if (page < 0) return;

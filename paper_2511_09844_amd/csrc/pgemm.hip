@@ -95,6 +95,7 @@ struct PgArgs {
     const float *rcos, *rsin;
     float *qout, *kc, *vc;
     int cap, max_batch, layer;
+    PagedView paged;  // table not null: K and V rows go to their pages
     const float* ubias;
     int ub_ld;
 };
@@ -211,8 +212,16 @@ __device__ __forceinline__ void pg_epilogue(const PgArgs& a, int P, int row, boo
             y = a.qout + (size_t)row * a.H * a.hd + h * a.hd + i;
         } else {
             if (pos < 0) return;
-            y = (seg == 1 ? a.kc : a.vc) +
-                ((((size_t)a.layer * a.max_batch + a.row_seq[row]) * a.Hkv + h) * a.cap + pos) * a.hd + i;
+            if (a.paged.table) {
+                const int page = paged_page(a.paged, a.row_seq[row], pos >> a.paged.shift);
+                if (page < 0) return;
+                const int slot = pos & ((1 << a.paged.shift) - 1);
+                y = (float*)(seg == 1 ? a.paged.k : a.paged.v) + page * a.paged.page_stride +
+                    ((size_t)(h << a.paged.shift) + slot) * a.hd + i;
+            } else {
+                y = (seg == 1 ? a.kc : a.vc) +
+                    ((((size_t)a.layer * a.max_batch + a.row_seq[row]) * a.Hkv + h) * a.cap + pos) * a.hd + i;
+            }
         }
         *(pg_f4*)y = v0;
         *(pg_f4*)(y + half) = v1;
@@ -674,6 +683,7 @@ bool launch_pgemm(Engine* e, hipStream_t s, const WsCall& c) {
     a.H = c.H; a.Hkv = c.Hkv; a.hd = c.hd; a.row_pos = c.row_pos; a.row_seq = c.row_seq;
     a.rcos = c.rcos; a.rsin = c.rsin; a.qout = c.qout; a.kc = c.kc; a.vc = c.vc;
     a.cap = c.cap; a.max_batch = c.max_batch; a.layer = c.layer; a.ubias = c.ubias; a.ub_ld = c.ub_ld;
+    a.paged = c.paged;
     ProfEntry* pe = prof_slot(e, kProfGemv, (double)N * c.K * 2.0 + (double)c.M * c.K * 4.0 + (double)c.M * N * 4.0);
     if (p.skinny) sg_launch(s, pe, c.mode, a);
     else if (p.MG == 1) pg_launch<1, 2, 4, 1>(s, pe, c.mode, dim3(p.grid), a);

@@ -427,6 +427,10 @@ void launch_wsgemv(Engine* e, hipStream_t s, const WsCall& c) {
     // rows that come as planes, and more than one 16-row group, run on the plane kernel
     // (pgemm.hip); up to 16 fp32 rows (the steering projections) save the launch that makes planes
     if ((c.planes || c.M > 16) && launch_pgemm(e, s, c)) return;
+    if (c.paged.table) {  // (rows into pages: launch_pgemm only, which takes every shape of a paged handle)
+        e->bad_launch = true;
+        return;
+    }
     if (c.planes) {  // there are no fp32 rows to fall back on
         if (e) e->bad_launch = true;
         return;

@@ -133,3 +133,29 @@ def test_paged_struct_layouts_match_the_header(tmp_path):
     got = [list(map(int, line.split())) for line in subprocess.check_output([str(exe)]).decode().splitlines()]
     for line, s in zip(got, structs.values()):
         assert line == [ctypes.sizeof(s)] + [getattr(s, f[0]).offset for f in s._fields_], s
+
+
+def test_paged_handles_refused():
+    import sd2_inputs as si
+    lib, cfg, h = B.load(), B.config_of(si.TINY), B.P()
+    ref = ctypes.byref(cfg)
+
+    def size(page, n, c=cfg):
+        return lib.sd2_create_paged_bytes(ctypes.byref(c), ctypes.byref(B.Paging(page, n)))
+
+    assert size(16, 8) > 0 and size(64, 8) > size(32, 8)
+    # a page holds page_size rows of k and v in every layer and KV head of both models
+    per = 16 * 2 * 4 * (4 * 8 * 32 + 2 * 4 * 32)
+    assert 1000 * per <= size(16, 1008) - size(16, 8) <= 1000 * (per + 64)
+    bad = [(0, 8), (8, 8), (48, 8), (2048, 8), (16, 0), (16, -1), (16, (1 << 24) + 1)]
+    for page, n in bad:
+        assert size(page, n) == 0
+        pg = B.Paging(page, n)
+        assert lib.sd2_create_paged(ref, None, None, None, ctypes.byref(pg), None, 0, None, ctypes.byref(h)) == -1
+    assert lib.sd2_create_paged_bytes(ref, None) == 0
+    mlp = B.config_of(si.TINY, steering=B.STEER_MLP)
+    assert size(16, 8, mlp) == 0
+    pg = B.Paging(16, 8)
+    assert lib.sd2_create_paged(ctypes.byref(mlp), None, None, None, ctypes.byref(pg), None, 0, None, ctypes.byref(h)) == -1
+    assert lib.sd2_create_paged(ref, None, None, None, ctypes.byref(pg), None, 0, None, None) == -1
+    assert lib.sd2_fork(None, 0, 1) == -1 and lib.sd2_release(None, 0) == -1 and lib.sd2_compact(None, None) == -1
