@@ -431,6 +431,435 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
     put<T, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
 }
 
+// ---------------------------------------------------------------------------------------------
+// Many rows per sequence (prompts): k_pprompt.  A workgroup takes 256 (bf16) query vectors of a sequence
+// and KV head, 64 per wave as two column tiles of 32, and goes through the keys in tiles of KT that its
+// four waves stage in LDS, requested one tile ahead.  The products are those of k_pdecode on 32 x 32 tiles:
+// in the result of S^T = K Q^T lane group g holds keys 8 (r / 4) + 4 g + r % 4, r < 16, of one query vector,
+// which are the contraction slots of two PV products.  LDS holds both operands as the lanes read
+// them, a fragment of 64 x 16 bytes after the other: K as it is (two waves), V permuted on the way
+// from memory so that 16 bytes are eight keys of one column (the other two); within a fragment the 16-byte
+// units are permuted so that neither side meets bank conflicts.
+// The running maximum is raised only when a score exceeds it by 2^kLazy: until then the weights
+// are at most that large, and the sums need no rescaling.
+// ---------------------------------------------------------------------------------------------
+typedef float f16v __attribute__((ext_vector_type(16)));
+constexpr float kLazy = 8.f;
+
+struct PromptArgs {
+    PagedAttnArgs a;
+    int tiles;  // workgroups of a KV head
+};
+
+// Maximum and sum over the two halves of a wave.
+__device__ __forceinline__ float half_max(float v) {
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Which sequence workgroup `tile` of a KV head belongs to, and its first query vector there: QV to a
+// workgroup, sequence after sequence.  -1: none.
+template <int QV>
+__device__ __forceinline__ int prompt_tile(const PagedRows& r, int G, int tile, int& v0) {
+    if (!r.row_off) {
+        const int per = ((int64_t)r.max_rows * G + QV - 1) / QV;
+        v0 = tile % per * QV;
+        return tile / per;
+    }
+    const int lane = threadIdx.x & 63;
+    int at = 0;
+    for (int b0 = 0; b0 < r.nseq; b0 += 64) {
+        int n = 0;
+        if (b0 + lane < r.nseq) paged_rows(r, b0 + lane, n);
+        const int mine = ((int64_t)n * G + QV - 1) / QV;
+        int inc = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int y = __shfl_up(inc, d, 64);
+            if (lane >= d) inc += y;
+        }
+        const uint64_t here = __ballot(tile < at + inc);
+        if (here) {
+            const int l = __builtin_ctzll(here);
+            v0 = (tile - at - __shfl(inc - mine, l, 64)) * QV;
+            return __builtin_amdgcn_readfirstlane(b0 + l);
+        }
+        at += __shfl(inc, 63, 64);
+    }
+    return -1;
+}
+
+template <int HD>
+__global__ __launch_bounds__(256, 1) void k_pprompt_bf16(PromptArgs d) {
+    constexpr int KT = 64 * 128 / HD, NB = KT / 32, NS = HD / 16, NC = HD / 32, CH = HD / 8, QV = 256;
+    __shared__ __attribute__((aligned(16))) u4 ks[2][KT * CH], vs[2][KT * CH];
+    const PagedAttnArgs& a = d.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, g = lane >> 5;
+    const int G = a.H / a.c.Hkv;
+    // KV heads lie on XCDs in turn, each sequence's last rows, which read the most keys, go first
+    const int kvh = blockIdx.x % a.c.Hkv;
+    int v0 = 0;
+    const int b = prompt_tile<QV>(a.r, G, d.tiles - 1 - blockIdx.x / a.c.Hkv, v0);
+    if (b < 0) return;
+    v0 = __builtin_amdgcn_readfirstlane(v0);
+    int nrows;
+    const int r0 = paged_rows(a.r, b, nrows);
+    const int nqv = nrows * G;
+    if (v0 >= nqv) return;
+    const int len = paged_len(a.r, b, r0, nrows), at0 = len - nrows;
+    const int wv = v0 + 64 * wave;                       // the wave's first query vector
+    const int end = min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift);
+    const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 63, nqv - 1) / G + 1) : 0;
+    u4 q[2][NS];
+    int pos[2];
+    // (a negative scale turns into the sign of q)
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    const float c = fabsf(a.scale) * kLog2e;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int v = min(wv + 32 * t + n, nqv - 1);
+        pos[t] = at0 + v / G;
+        const uint16_t* p = (const uint16_t*)a.q + (r0 + v / G) * a.q_stride + (kvh * G + v % G) * HD + 8 * g;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) q[t][s] = *(const u4*)(p + 16 * s) ^ flip;
+    }
+    f16v o[2][NC];
+    float m[2], l[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        m[t] = -INFINITY;
+        l[t] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[t][i][r] = 0.f;
+    }
+    // pages of the KT / 16 groups of keys of a tile, a lane each
+    auto look = [&](int k0) {
+        const int key = k0 + 16 * lane;
+        return lane < KT / 16 && key < end ? paged_page(a.c, b, key >> a.c.shift) : -1;
+    };
+    const int mask = (1 << a.c.shift) - 1;
+    const bool isv = wave < 2;
+    const int kw = (wave & 1) * (KT / 2);                // the half of the tile that this wave stages
+    u4 st[8];
+    // V: the lane's eight keys 16 u + 8 (j / 4) + 4 vg + j % 4 and eight columns
+    const int vch = lane % CH, vg = lane / CH & 1, vu = lane / (2 * CH);
+    auto load = [&](int k0, int pg) {
+        if (isv) {
+            const int key = k0 + kw + 16 * vu, page = __shfl(pg, kw / 16 + vu, 64);
+            const int rows = page < 0 ? 0 : min(end - key, 16);
+            const uint16_t* p = (const uint16_t*)a.c.v + max(page, 0) * a.c.page_stride +
+                                (((int64_t)kvh << a.c.shift) + (key & mask)) * HD + 8 * vch;
+            if (__all(rows == 16)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) st[j] = *(const u4*)(p + (8 * (j / 4) + 4 * vg + j % 4) * HD);
+            } else {
+                // rows that do not exist: another row's address, and zeros
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int row = 8 * (j / 4) + 4 * vg + j % 4;
+                    st[j] = *(const u4*)(p + (row < rows ? row : 0) * HD);
+                    st[j] = row < rows ? st[j] : u4{0, 0, 0, 0};
+                }
+            }
+        } else {
+            constexpr int RI = 64 / CH;  // rows of an instruction
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int tile = kw / 16 + i * RI / 16, key = k0 + 16 * tile;
+                const int page = __builtin_amdgcn_readlane(pg, tile);
+                const int rows = page < 0 ? 0 : max(min(end - key, 16), 0);
+                const uint16_t* p = (const uint16_t*)a.c.k + max(page, 0) * a.c.page_stride +
+                                    (((int64_t)kvh << a.c.shift) + (key & mask)) * HD;
+                const auto rk = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, rows * HD * 2, 0x00020000);
+                st[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, ((i * RI % 16 + lane / CH) * HD + lane % CH * 8) * 2, 0, 0);
+            }
+        }
+    };
+    auto store = [&](int buf) {
+        if (isv) {
+            // column 8 vch + i of the lane's keys: fragment (16-key group, 32 columns), lane vg * 32 + column % 32
+            const int f = ((kw / 16 + vu) * NC + vch / 4) * 64 + vg * 32 + vch % 4 * 8;
+            const int x = (vg * 4 + vch % 4) ^ (vch / 4 % 2 * 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                u4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    w[e] = __builtin_amdgcn_perm(st[2 * e + 1][i / 2], st[2 * e][i / 2], i % 2 ? 0x07060302 : 0x05040100);
+                vs[buf][f + (i ^ x)] = w;
+            }
+        } else {
+            constexpr int RI = 64 / CH;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int row = kw + i * RI + lane / CH, cc = lane % CH;
+                const int at = (cc & 1) * 32 + row % 32;
+                ks[buf][(row / 32 * NS + cc / 2) * 64 + (at & ~7) + ((at ^ cc) & 7)] = st[i];
+            }
+        }
+    };
+    const int nt = end > 0 ? (end + KT - 1) / KT : 0;
+    int pg = look(0);
+    uint64_t have = __ballot(pg >= 0);
+    load(0, pg);
+    pg = look(KT);
+    store(0);
+    for (int t = 0; t < nt; ++t) {
+        __syncthreads();
+        const uint64_t now = have;
+        if (t + 1 < nt) {
+            have = __ballot(pg >= 0);
+            load((t + 1) * KT, pg);
+            pg = look((t + 2) * KT);
+        }
+        const u4 *kf = ks[t & 1], *vf = vs[t & 1];
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const int k0 = t * KT + 32 * kb;
+            if (k0 >= wend) break;
+            f16v s[2];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[0][r] = s[1][r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                const b8 x = __builtin_bit_cast(b8, kf[(kb * NS + i) * 64 + (lane & ~7) + ((lane ^ (2 * i + g)) & 7)]);
+                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(b8, q[0][i]), s[0], 0, 0, 0);
+                s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(b8, q[1][i]), s[1], 0, 0, 0);
+            }
+            const uint32_t hv = now >> (2 * kb) & 3;
+            if (k0 + 31 > wfirst || hv != 3) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int key = 8 * (r / 4) + 4 * g + r % 4;
+                        s[j][r] = k0 + key <= pos[j] && (hv >> (r / 8) & 1) ? s[j][r] : -INFINITY;
+                    }
+            }
+            u4 p[2][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float mx = s[j][0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[j][r]);
+                mx = half_max(mx) * c;
+                if (__any(mx > m[j] + kLazy)) {
+                    const float mn = fmaxf(m[j], mx), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[j] - mn);
+                    m[j] = mn;
+                    l[j] *= f;
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) o[j][i] *= f;
+                }
+                const float base = m[j] == -INFINITY ? 0.f : m[j];
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r], c, -base));
+                    sum += s[j][r];
+                }
+                l[j] += sum;
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) p[j][r / 8][r % 8 / 2] = pack_bf16(s[j][r], s[j][r + 1]);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    const b8 x = __builtin_bit_cast(b8, vf[((2 * kb + u) * NC + i) * 64 + (lane & ~7) + ((lane ^ (lane >> 3) ^ (i % 2 * 4)) & 7)]);
+                    o[0][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(b8, p[0][u]), o[0][i], 0, 0, 0);
+                    o[1][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(b8, p[1][u]), o[1][i], 0, 0, 0);
+                }
+        }
+        if (t + 1 < nt) store((t + 1) & 1);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int v = wv + 32 * j + n;
+        const float sum = half_sum(l[j]), inv = sum > 0.f ? 1.f / sum : 0.f;
+        if (v >= nqv) continue;
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const float y[4] = {o[j][i][r] * inv, o[j][i][r + 1] * inv, o[j][i][r + 2] * inv, o[j][i][r + 3] * inv};
+                put<uint16_t, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + 32 * i + 2 * r + 4 * g, y);
+            }
+    }
+}
+
+// The same on fp32 matrix instructions, 32 query vectors per wave and tiles of 32 keys, row by row in LDS
+// (rows of K four words apart from whole bank rounds).  A lane reads a row of K, or HD / 32 neighbouring
+// columns of its keys of V, at a time.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
+    constexpr int KT = 32, QV = 128, C4 = HD / 4, KL = HD + 4, VW = HD / 32, NU = KT * C4 / 256;
+    __shared__ __attribute__((aligned(16))) float ks[2][KT * KL], vs[2][KT * HD];
+    const PagedAttnArgs& a = d.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 31, g = lane >> 5;
+    const int G = a.H / a.c.Hkv;
+    const int kvh = blockIdx.x % a.c.Hkv;
+    int v0 = 0;
+    const int b = prompt_tile<QV>(a.r, G, d.tiles - 1 - blockIdx.x / a.c.Hkv, v0);
+    if (b < 0) return;
+    v0 = __builtin_amdgcn_readfirstlane(v0);
+    int nrows;
+    const int r0 = paged_rows(a.r, b, nrows);
+    const int nqv = nrows * G;
+    if (v0 >= nqv) return;
+    const int len = paged_len(a.r, b, r0, nrows), at0 = len - nrows;
+    const int wv = v0 + 32 * wave;
+    const int end = min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift);
+    const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 31, nqv - 1) / G + 1) : 0;
+    const float c = a.scale * kLog2e;
+    f4 q[HD / 8];
+    const int v = wv + n, vc = min(v, nqv - 1), pos = at0 + vc / G;
+    {
+        const float* p = (const float*)a.q + (r0 + vc / G) * a.q_stride + (kvh * G + vc % G) * HD + 4 * g;
+#pragma unroll
+        for (int s = 0; s < HD / 8; ++s) q[s] = *(const f4*)(p + 8 * s) * c;
+    }
+    f16v o[VW];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < VW; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    const int mask = (1 << a.c.shift) - 1;
+    u4 st[2][NU];
+    auto look = [&](int k0, int (&page)[2]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            page[t] = k0 + 16 * t < end ? __builtin_amdgcn_readfirstlane(paged_page(a.c, b, (k0 + 16 * t) >> a.c.shift)) : -1;
+    };
+    // unit i of a thread: row i * 1024 / HD + tid / C4, whose group of 16 keys is the same for a wave
+    auto load = [&](int k0, const int (&page)[2]) {
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+            const int t = HD == 32 ? wave >> 1 : i * (1024 / HD) / 16, key = k0 + 16 * t;
+            const int pg = HD == 32 ? (t ? page[1] : page[0]) : page[t];
+            const int rows = pg < 0 ? 0 : max(min(end - key, 16), 0);
+            const int64_t at = max(pg, 0) * a.c.page_stride + (((int64_t)kvh << a.c.shift) + (key & mask)) * HD;
+            const int off = ((i * (1024 / HD) + tid / C4) % 16 * HD + tid % C4 * 4) * 4;
+            st[0][i] = __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((float*)a.c.k + at, 0, rows * HD * 4, 0x00020000), off, 0, 0);
+            st[1][i] = __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((float*)a.c.v + at, 0, rows * HD * 4, 0x00020000), off, 0, 0);
+        }
+    };
+    auto store = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+            const int row = i * (1024 / HD) + tid / C4, x = tid % C4 * 4;
+            *(u4*)(ks[buf] + row * KL + x) = st[0][i];
+            *(u4*)(vs[buf] + row * HD + x) = st[1][i];
+        }
+    };
+    const int nt = end > 0 ? (end + KT - 1) / KT : 0;
+    int pg[2], nx[2];
+    look(0, pg);
+    look(KT, nx);
+    load(0, pg);
+    store(0);
+    for (int t = 0; t < nt; ++t) {
+        __syncthreads();
+        const int k0 = t * KT;
+        const bool whole = k0 + 31 <= wfirst && pg[0] >= 0 && pg[1] >= 0;
+        const bool have[2] = {pg[0] >= 0, pg[1] >= 0};
+        if (t + 1 < nt) {
+            pg[0] = nx[0];
+            pg[1] = nx[1];
+            load(k0 + KT, pg);
+            look(k0 + 2 * KT, nx);
+        }
+        const float *kf = ks[t & 1], *vf = vs[t & 1];
+        if (k0 < wend) {
+            f16v s, s1;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = s1[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < HD / 8; ++i) {
+                const f4 x = *(const f4*)(kf + n * KL + 8 * i + 4 * g);
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[i][e], s, 0, 0, 0);
+                    s1 = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e + 1], q[i][e + 1], s1, 0, 0, 0);
+                }
+            }
+            s += s1;
+            if (!whole)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = 8 * (r / 4) + 4 * g + r % 4;
+                    s[r] = k0 + key <= pos && have[r / 8] ? s[r] : -INFINITY;
+                }
+            float mx = s[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+            mx = half_max(mx);
+            if (__any(mx > m + kLazy)) {
+                const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= f;
+#pragma unroll
+                for (int i = 0; i < VW; ++i) o[i] *= f;
+            }
+            const float base = m == -INFINITY ? 0.f : m;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(s[r] - base);
+                sum += s[r];
+            }
+            l += sum;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float* p = vf + (8 * (r / 4) + 4 * g + r % 4) * HD + n * VW;
+                float x[VW];
+                if constexpr (VW == 4) *(f4*)x = *(const f4*)p;
+                else if constexpr (VW == 2) *(f2*)x = *(const f2*)p;
+                else x[0] = *p;
+#pragma unroll
+                for (int i = 0; i < VW; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], s[r], o[i], 0, 0, 0);
+            }
+        }
+        if (t + 1 < nt) store((t + 1) & 1);
+    }
+    const float sum = half_sum(l), inv = sum > 0.f ? 1.f / sum : 0.f;
+    if (v >= nqv) return;
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+        float y[4 * VW];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < VW; ++i) y[e * VW + i] = o[i][r + e] * inv;
+        put<float, 4 * VW>(a, r0 + v / G, (kvh * G + v % G) * HD + (2 * r + 4 * g) * VW, y);
+    }
+}
+
+template <typename T, int HD>
+hipError_t prompt(hipStream_t s, const PagedAttnArgs& a) {
+    constexpr int QV = sizeof(T) == 2 ? 256 : 128;
+    const int64_t G = a.H / a.c.Hkv;
+    const int64_t tiles = a.r.row_off ? a.r.total_rows * G / QV + a.r.nseq : a.r.nseq * ((a.r.max_rows * G + QV - 1) / QV);
+    if (tiles * a.c.Hkv > INT32_MAX) return hipErrorInvalidValue;
+    const PromptArgs d{a, (int)tiles};
+    if constexpr (sizeof(T) == 2) return launch(k_pprompt_bf16<HD>, dim3((unsigned)(tiles * a.c.Hkv)), dim3(256), s, d);
+    else return launch(k_pprompt_f32<HD>, dim3((unsigned)(tiles * a.c.Hkv)), dim3(256), s, d);
+}
+
+// Whether a call goes to k_pprompt: it takes the keys of a row in one piece, so it needs rows enough.
+bool many_rows(const PagedView& c, const PagedRows& r, int H, bool bf16) {
+    const int64_t G = H / c.Hkv, qv = std::min(r.max_rows, r.total_rows) * G;
+    return qv > 64 && r.total_rows * G * c.Hkv >= 64 * (bf16 ? 256 : 128);
+}
+
 struct DecodePlan {
     int nt, ncg, nspan;
     int64_t groups, ml;  // floats of the sums
@@ -464,6 +893,7 @@ hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p
 
 template <typename T, int HD>
 hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws, size_t room) {
+    if (many_rows(a.c, a.r, a.H, sizeof(T) == 2)) return prompt<T, HD>(s, a);
     const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, room);
     return p.nt == 1 ? run_decode<T, HD, 1>(s, a, p, ws) : run_decode<T, HD, 2>(s, a, p, ws);
 }
@@ -471,6 +901,7 @@ hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float*
 }  // namespace
 
 size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
+    if (many_rows(c, r, H, bf16)) return 256;
     const DecodePlan p = decode_plan(c, r, H, bf16, max_len, SIZE_MAX);
     return p.nspan == 1 ? 256 : (size_t)(p.ml + p.groups * p.nspan * 16 * p.nt * 2) * 4;
 }
