@@ -83,7 +83,8 @@ __device__ __forceinline__ void put(const PagedAttnArgs& a, int row, int c, cons
 // The keys a workgroup of k_pdecode takes at a time, 16 or 32 per wave.
 template <typename T>
 constexpr int kBlockKeys = sizeof(T) == 2 ? 32 : 16;
-constexpr int kDecodeWaves = 4;
+// Waves of a workgroup: as many as two per SIMD, with up to 32 query vectors (see Block: one buffer then).
+constexpr int kDecodeWaves = 8;
 
 struct DecodeArgs {
     PagedAttnArgs a;
@@ -116,7 +117,9 @@ struct Block {
     vv v[TK * 4][VU];
 };
 
-template <typename T, int HD>
+// Which of a block's operands.
+enum { kLoadK = 1, kLoadV = 2 };
+template <typename T, int HD, int WHAT>
 __device__ __forceinline__ void load_block(Block<T, HD>& x, const PagedView& c, int kvh, const int* page, int k0, int end,
                                            int lane) {
     using B = Block<T, HD>;
@@ -127,20 +130,24 @@ __device__ __forceinline__ void load_block(Block<T, HD>& x, const PagedView& c, 
         const int key = k0 + 16 * t;
         const int rows = page[t] < 0 ? 0 : max(min(end - key, 16), 0);
         const int64_t at = (int64_t)max(page[t], 0) * c.page_stride + (((int64_t)kvh << c.shift) + (key & ((1 << c.shift) - 1))) * HD;
-        const auto rk = __builtin_amdgcn_make_buffer_rsrc((T*)c.k + at, 0, rows * RB, 0x00020000);
-        const auto rv = __builtin_amdgcn_make_buffer_rsrc((T*)c.v + at, 0, rows * RB, 0x00020000);
+        if constexpr (WHAT & kLoadK) {
+            const auto rk = __builtin_amdgcn_make_buffer_rsrc((T*)c.k + at, 0, rows * RB, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < B::NK; ++i)
-            x.k[t][i] = __builtin_amdgcn_raw_buffer_load_b128(rk, n * RB + 16 * g + 64 * i, 0, 0);
+            for (int i = 0; i < B::NK; ++i)
+                x.k[t][i] = __builtin_amdgcn_raw_buffer_load_b128(rk, n * RB + 16 * g + 64 * i, 0, 0);
+        }
+        if constexpr (WHAT & kLoadV) {
+            const auto rv = __builtin_amdgcn_make_buffer_rsrc((T*)c.v + at, 0, rows * RB, 0x00020000);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int u = 0; u < B::VU; ++u) {
-                const int off = (4 * g + r) * RB + (u * 16 + n) * B::VW * (int)sizeof(T);
-                if constexpr (B::VD == 4) x.v[4 * t + r][u] = __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0);
-                else if constexpr (B::VD == 2) x.v[4 * t + r][u] = __builtin_amdgcn_raw_buffer_load_b64(rv, off, 0, 0);
-                else x.v[4 * t + r][u] = __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0);
-            }
+                for (int u = 0; u < B::VU; ++u) {
+                    const int off = (4 * g + r) * RB + (u * 16 + n) * B::VW * (int)sizeof(T);
+                    if constexpr (B::VD == 4) x.v[4 * t + r][u] = __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0);
+                    else if constexpr (B::VD == 2) x.v[4 * t + r][u] = __builtin_amdgcn_raw_buffer_load_b64(rv, off, 0, 0);
+                    else x.v[4 * t + r][u] = __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, 0);
+                }
+        }
     }
 }
 
@@ -150,40 +157,51 @@ struct Acc {
     float m[NT], l[NT];
 };
 
+// Scores of a block, in units of log2, those that a row does not read at -inf.
 template <typename T, int HD, int NT>
-__device__ __forceinline__ void block_step(const Block<T, HD>& x, const u4 (&q)[NT][Block<T, HD>::NK], Acc<T, HD, NT>& acc,
-                                           const int* page, int k0, const int (&pos)[NT], bool whole, float scale, int lane) {
+__device__ __forceinline__ void block_scores(const Block<T, HD>& x, const u4 (&q)[NT][Block<T, HD>::NK],
+                                             f4 (&sc)[NT][Block<T, HD>::TK], const int* page, int k0, const int (&pos)[NT],
+                                             bool whole, float scale, int lane) {
     using B = Block<T, HD>;
     const int g = lane >> 4;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        f4 s[B::TK];
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int t = 0; t < B::TK; ++t) {
-            s[t] = f4{0.f, 0.f, 0.f, 0.f};
+            f4 s = f4{0.f, 0.f, 0.f, 0.f};
             if constexpr (B::H) {
 #pragma unroll
                 for (int i = 0; i < B::NK; ++i)
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, x.k[t][i]),
-                                                                   __builtin_bit_cast(b8, q[j][i]), s[t], 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, x.k[t][i]), __builtin_bit_cast(b8, q[j][i]),
+                                                                s, 0, 0, 0);
             } else {
-                f4 s1 = s[t];  // two chains
+                f4 s1 = s;  // two chains
 #pragma unroll
                 for (int i = 0; i < B::NK; ++i) {
                     const f4 kk = __builtin_bit_cast(f4, x.k[t][i]), qq = __builtin_bit_cast(f4, q[j][i]);
 #pragma unroll
                     for (int e = 0; e < 4; e += 2) {
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[e], qq[e], s[t], 0, 0, 0);
+                        s = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[e], qq[e], s, 0, 0, 0);
                         s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[e + 1], qq[e + 1], s1, 0, 0, 0);
                     }
                 }
-                s[t] += s1;
+                s += s1;
             }
-            s[t] *= scale;
+            s *= scale;
             if (!whole)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s[t][r] = page[t] >= 0 && k0 + 16 * t + 4 * g + r <= pos[j] ? s[t][r] : -INFINITY;
+                for (int r = 0; r < 4; ++r) s[r] = page[t] >= 0 && k0 + 16 * t + 4 * g + r <= pos[j] ? s[r] : -INFINITY;
+            sc[j][t] = s;
         }
+}
+
+// The block's part of the softmax and of its product with V.
+template <typename T, int HD, int NT>
+__device__ __forceinline__ void block_sums(const Block<T, HD>& x, f4 (&sc)[NT][Block<T, HD>::TK], Acc<T, HD, NT>& acc) {
+    using B = Block<T, HD>;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        f4(&s)[B::TK] = sc[j];
         float mx = -INFINITY;
 #pragma unroll
         for (int t = 0; t < B::TK; ++t) mx = fmaxf(mx, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
@@ -206,38 +224,45 @@ __device__ __forceinline__ void block_step(const Block<T, HD>& x, const u4 (&q)[
                 sum += s[t][r];
             }
         acc.l[j] += sum;
-        if constexpr (B::H) {
-            // the weights as bf16, the type of the matrix instruction that v enters as it is: half a step of
-            // 2^-8 each, as much as the output's own rounding
-            const b8 p = __builtin_bit_cast(b8, u4{pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]),
-                                                   pack_bf16(s[1][0], s[1][1]), pack_bf16(s[1][2], s[1][3])});
+    }
+    if constexpr (B::H) {
+        // the weights as bf16, the type of the matrix instruction that v enters as it is: half a step of
+        // 2^-8 each, as much as the output's own rounding
+        b8 p[NT];
 #pragma unroll
-            for (int i = 0; i < HD / 16; ++i) {
-                u4 w;
+        for (int j = 0; j < NT; ++j)
+            p[j] = __builtin_bit_cast(b8, u4{pack_bf16(sc[j][0][0], sc[j][0][1]), pack_bf16(sc[j][0][2], sc[j][0][3]),
+                                             pack_bf16(sc[j][1][0], sc[j][1][1]), pack_bf16(sc[j][1][2], sc[j][1][3])});
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-                    w[d] = __builtin_amdgcn_perm(x.v[2 * d + 1][0][i / 2], x.v[2 * d][0][i / 2], i % 2 ? 0x07060302 : 0x05040100);
-                acc.o[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, w), p, acc.o[j][i], 0, 0, 0);
-            }
-        } else {
+        for (int i = 0; i < HD / 16; ++i) {
+            u4 w;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int d = 0; d < 4; ++d)
+                w[d] = __builtin_amdgcn_perm(x.v[2 * d + 1][0][i / 2], x.v[2 * d][0][i / 2], i % 2 ? 0x07060302 : 0x05040100);
 #pragma unroll
-                for (int u = 0; u < B::VU; ++u)
-#pragma unroll
-                    for (int e = 0; e < B::VW; ++e)
-                        acc.o[j][u * B::VW + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[r][u][e]), s[0][r],
-                                                                                     acc.o[j][u * B::VW + e], 0, 0, 0);
+            for (int j = 0; j < NT; ++j)
+                acc.o[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, w), p[j], acc.o[j][i], 0, 0, 0);
         }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int u = 0; u < B::VU; ++u)
+#pragma unroll
+                for (int e = 0; e < B::VW; ++e)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+                        acc.o[j][u * B::VW + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[r][u][e]), sc[j][0][r],
+                                                                                     acc.o[j][u * B::VW + e], 0, 0, 0);
     }
 }
 
 // Query vector v of a sequence and KV head: row v / G of the sequence, head kvh * G + v % G.
 template <typename T, int HD, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_pdecode(DecodeArgs d) {
+__global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) {
     using B = Block<T, HD>;
     constexpr int QV = 16 * NT, BK = kBlockKeys<T>;
-    __shared__ __attribute__((aligned(16))) f4 os[2][NT * (HD / 16)][64];
+    __shared__ __attribute__((aligned(16))) f4 os[kDecodeWaves / 2][NT * (HD / 16)][64];
     __shared__ float ms[kDecodeWaves][QV][2];
     const PagedAttnArgs& a = d.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -289,27 +314,50 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_pdecode(DecodeArgs d) 
     };
     constexpr int step = kDecodeWaves * BK;
     int k0 = kb + wave * BK;
-    Block<T, HD> x[2];
     int page[3][B::TK];
     look(k0, page[0]);
     look(k0 + step, page[1]);
-    load_block<T, HD>(x[0], a.c, kvh, page[0], k0, ke, lane);
-    for (; k0 < ke; k0 += 2 * step) {
+    f4 sc[NT][B::TK];
+    auto whole = [&](int k) {
+        bool w = k + BK - 1 <= min(first, ke - 1);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int k = k0 + i * step;
-            if (k >= ke) break;
-            look(k + 2 * step, page[2]);
-            load_block<T, HD>(x[1 - i], a.c, kvh, page[1], k + step, ke, lane);
-            bool whole = k + BK - 1 <= min(first, ke - 1);
+        for (int t = 0; t < B::TK; ++t) w &= page[0][t] >= 0;
+        return w;
+    };
+    auto shift = [&] {
 #pragma unroll
-            for (int t = 0; t < B::TK; ++t) whole &= page[0][t] >= 0;
-            block_step<T, HD, NT>(x[i], q, acc, page[0], k, pos, whole, scale, lane);
+        for (int t = 0; t < B::TK; ++t) {
+            page[0][t] = page[1][t];
+            page[1][t] = page[2][t];
+        }
+    };
+    if constexpr (NT == 1) {
+        // the next block is requested before this one is used
+        Block<T, HD> x[2];
+        load_block<T, HD, kLoadK | kLoadV>(x[0], a.c, kvh, page[0], k0, ke, lane);
+        for (; k0 < ke; k0 += 2 * step) {
 #pragma unroll
-            for (int t = 0; t < B::TK; ++t) {
-                page[0][t] = page[1][t];
-                page[1][t] = page[2][t];
+            for (int i = 0; i < 2; ++i) {
+                const int k = k0 + i * step;
+                if (k >= ke) break;
+                look(k + 2 * step, page[2]);
+                load_block<T, HD, kLoadK | kLoadV>(x[1 - i], a.c, kvh, page[1], k + step, ke, lane);
+                block_scores<T, HD, NT>(x[i], q, sc, page[0], k, pos, whole(k), scale, lane);
+                block_sums<T, HD, NT>(x[i], sc, acc);
+                shift();
             }
+        }
+    } else {
+        // registers for one block: its K is replaced when the scores are there, its V when the sums are
+        Block<T, HD> x;
+        load_block<T, HD, kLoadK | kLoadV>(x, a.c, kvh, page[0], k0, ke, lane);
+        for (; k0 < ke; k0 += step) {
+            look(k0 + 2 * step, page[2]);
+            block_scores<T, HD, NT>(x, q, sc, page[0], k0, pos, whole(k0), scale, lane);
+            load_block<T, HD, kLoadK>(x, a.c, kvh, page[1], k0 + step, ke, lane);
+            block_sums<T, HD, NT>(x, sc, acc);
+            load_block<T, HD, kLoadV>(x, a.c, kvh, page[1], k0 + step, ke, lane);
+            shift();
         }
     }
     // the waves' parts on one maximum, then added
@@ -338,7 +386,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_pdecode(DecodeArgs d) 
         for (int i = 0; i < HD / 16; ++i) acc.o[j][i] *= f;
     }
 #pragma unroll
-    for (int half = 2; half > 0; half /= 2) {
+    for (int half = kDecodeWaves / 2; half > 0; half /= 2) {
         if (wave >= half && wave < 2 * half)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
@@ -872,8 +920,8 @@ DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16,
     p.nt = qv <= 16 ? 1 : 2;
     p.ncg = (qv + 16 * p.nt - 1) / (16 * p.nt);
     p.groups = (int64_t)std::max(r.nseq, 1) * c.Hkv * p.ncg;
-    const int64_t step = kDecodeWaves * (bf16 ? 32 : 16), most = std::min<int64_t>((max_len + step - 1) / step, 128);
-    p.nspan = (int)std::max<int64_t>(1, std::min<int64_t>(most, (1024 + p.groups - 1) / p.groups));
+    const int64_t step = kDecodeWaves * (bf16 ? 32 : 16), most = std::min<int64_t>((max_len + 2 * step - 1) / (2 * step), 128);
+    p.nspan = (int)std::max<int64_t>(1, std::min<int64_t>(most, (512 + p.groups - 1) / p.groups));
     const size_t per = (size_t)p.groups * 16 * p.nt * (c.hd + 2);
     if (p.nspan > 1 && per * p.nspan > room) p.nspan = (int)std::max<size_t>(1, room / per);
     p.ml = p.groups * p.nspan * 16 * p.nt * c.hd;
@@ -885,7 +933,7 @@ hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p
     const DecodeArgs d{a, p.ncg, p.nspan, ws, p.ml};
     const int64_t units8 = ((int64_t)a.r.nseq * a.c.Hkv * p.nspan + 7) / 8 * 8;
     if (units8 * p.ncg > INT32_MAX) return hipErrorInvalidValue;
-    const hipError_t err = launch(k_pdecode<T, HD, NT>, dim3((unsigned)(units8 * p.ncg)), dim3(256), s, d);
+    const hipError_t err = launch(k_pdecode<T, HD, NT>, dim3((unsigned)(units8 * p.ncg)), dim3(64 * kDecodeWaves), s, d);
     if (err != hipSuccess || p.nspan == 1) return err;
     constexpr int per = 256 / (HD / 4), nb = (16 * NT + per - 1) / per;
     return launch(k_pjoin<T, HD, NT>, dim3((unsigned)(p.groups * nb)), dim3(256), s, d);

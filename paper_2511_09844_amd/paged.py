@@ -43,6 +43,7 @@ class PagedCache:
         _need(refs.numel() == n_pages, "refs: one for every page")
         self.k, self.v, self.table, self.refs = k, v, table, refs
         self.device, self.dtype = k.device, k.dtype
+        self._index, self._sizes = k.device.index, {}
         self.n_pages, self.n_layers, self.n_kv_heads, self.page_size, self.head_dim = n_pages, n_layers, n_kv, page, hd
         self.max_seqs, self.max_pages = table.shape
         self.lib = B.load()
@@ -53,6 +54,7 @@ class PagedCache:
         self._pages = pages
         self._pages_ws = self.lib.sd2_pages_workspace_bytes(ctypes.byref(pages))
         _need(self._pages_ws > 0, "the cache's sizes are outside what sd2_pages takes")
+        self._scale = 1.0 / math.sqrt(hd)
         layer = n_kv * page * hd
         self._kv = [B.PagedKv(k.data_ptr() + l * layer * size, v.data_ptr() + l * layer * size, n_layers * layer,
                               DTYPES[k.dtype], page, n_pages, n_kv, hd, self.max_pages, table.data_ptr())
@@ -116,8 +118,15 @@ class PagedCache:
     def _workspace(self, nbytes):
         return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
-    def _stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
+    def _call(self, fn, *args):
+        """A C call on the current stream of the cache's device, which is the current one meanwhile."""
+        if torch.cuda.current_device() == self._index:
+            rc = fn(*args, torch.cuda.current_stream(self._index).cuda_stream)
+        else:
+            with torch.cuda.device(self._index):
+                rc = fn(*args, torch.cuda.current_stream(self._index).cuda_stream)
+        if rc:
+            B.check(rc, None, fn.__name__)
 
     # ---- rows --------------------------------------------------------------------------------------
     def append(self, k, v, lens, layer=0, row_off=None, max_rows=None):
@@ -128,9 +137,7 @@ class PagedCache:
         ks, vs = self._packed(k, "k"), self._packed(v, "v")
         _need(k.shape == v.shape and k.shape[1] == self.n_kv_heads, "k and v: [rows][n_kv_heads][head_dim]")
         rows = self._rows(k.shape[0], lens, row_off, max_rows)
-        with torch.cuda.device(self.device):
-            B.check(self.lib.sd2_paged_append(kv, ctypes.byref(rows), k.data_ptr(), ks, v.data_ptr(), vs,
-                                              self._stream()), None, "sd2_paged_append")
+        self._call(self.lib.sd2_paged_append, kv, ctypes.byref(rows), k.data_ptr(), ks, v.data_ptr(), vs)
 
     def attend(self, q, lens, layer=0, row_off=None, max_rows=None, max_len=None, scale=None, out=None):
         """Causal attention of rows q [rows][heads][head_dim] over their sequences' pages
@@ -142,21 +149,27 @@ class PagedCache:
         heads = q.shape[1]
         _need(heads > 0 and heads % self.n_kv_heads == 0, f"{heads} heads on {self.n_kv_heads} KV heads")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _need(isinstance(out, torch.Tensor) and out.shape == q.shape, "out has to be like q")
-        _need(not q.numel() or out.data_ptr() != q.data_ptr(), "out must not be q")
-        os = self._packed(out, "out")
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            os = heads * self.head_dim
+        else:
+            _need(isinstance(out, torch.Tensor) and out.shape == q.shape, "out has to be like q")
+            _need(not q.numel() or out.data_ptr() != q.data_ptr(), "out must not be q")
+            os = self._packed(out, "out")
         rows = self._rows(q.shape[0], lens, row_off, max_rows)
         if max_len is None:
             max_len = self.max_pages * self.page_size
-        _need(1 <= max_len <= self.max_pages * self.page_size, f"max_len {max_len} of {self.max_pages} pages")
-        nbytes = self.lib.sd2_paged_attn_workspace_bytes(kv, ctypes.byref(rows), heads, max_len)
-        _need(nbytes > 0, "attend: sizes outside what sd2_paged_attn takes")
-        with torch.cuda.device(self.device):
-            ws = self._workspace(nbytes)
-            B.check(self.lib.sd2_paged_attn(kv, ctypes.byref(rows), q.data_ptr(), qs, out.data_ptr(), os, heads,
-                                            1.0 / math.sqrt(self.head_dim) if scale is None else scale, max_len,
-                                            ws.data_ptr(), nbytes, self._stream()), None, "sd2_paged_attn")
+        key = (heads, rows.nseq, rows.max_rows, rows.total_rows, row_off is None, max_len)
+        nbytes = self._sizes.get(key)
+        if nbytes is None:
+            _need(1 <= max_len <= self.max_pages * self.page_size, f"max_len {max_len} of {self.max_pages} pages")
+            nbytes = self.lib.sd2_paged_attn_workspace_bytes(kv, ctypes.byref(rows), heads, max_len)
+            _need(nbytes > 0, "attend: sizes outside what sd2_paged_attn takes")
+            if len(self._sizes) > 1000:
+                self._sizes.clear()
+            self._sizes[key] = nbytes
+        ws = self._workspace(nbytes)
+        self._call(self.lib.sd2_paged_attn, kv, ctypes.byref(rows), q.data_ptr(), qs, out.data_ptr(), os, heads,
+                   self._scale if scale is None else scale, max_len, ws.data_ptr(), nbytes)
         return out
 
     # ---- pages -------------------------------------------------------------------------------------
@@ -165,11 +178,9 @@ class PagedCache:
         per sequence: last[b], or where the first page begins that could not be had."""
         n = self._seqs("reserve", first=first, last=last, keep=keep)
         granted = torch.empty(n, dtype=torch.int32, device=self.device)
-        with torch.cuda.device(self.device):
-            ws = self._workspace(self._pages_ws)
-            B.check(self.lib.sd2_pages_reserve(ctypes.byref(self._pages), n, first.data_ptr(), last.data_ptr(),
-                                               None if keep is None else keep.data_ptr(), granted.data_ptr(),
-                                               ws.data_ptr(), self._pages_ws, self._stream()), None, "sd2_pages_reserve")
+        ws = self._workspace(self._pages_ws)
+        self._call(self.lib.sd2_pages_reserve, ctypes.byref(self._pages), n, first.data_ptr(), last.data_ptr(),
+                   None if keep is None else keep.data_ptr(), granted.data_ptr(), ws.data_ptr(), self._pages_ws)
         return granted
 
     def fork(self, src, dst):
@@ -179,23 +190,17 @@ class PagedCache:
         _need(len(src) == len(dst), "fork: as many src as dst")
         n = len(src)
         arr = ctypes.c_int32 * max(n, 1)
-        with torch.cuda.device(self.device):
-            B.check(self.lib.sd2_pages_fork(ctypes.byref(self._pages), n, arr(*src), arr(*dst), self._stream()), None,
-                    "sd2_pages_fork")
+        self._call(self.lib.sd2_pages_fork, ctypes.byref(self._pages), n, arr(*src), arr(*dst))
 
     def trim(self, lens):
         """Sequences 0 .. len(lens) - 1 keep the pages of their first lens[b] positions (sd2_pages_trim;
         a negative length: all)."""
         n = self._seqs("trim", lens=lens)
-        with torch.cuda.device(self.device):
-            B.check(self.lib.sd2_pages_trim(ctypes.byref(self._pages), n, lens.data_ptr(), self._stream()), None,
-                    "sd2_pages_trim")
+        self._call(self.lib.sd2_pages_trim, ctypes.byref(self._pages), n, lens.data_ptr())
 
     def compact(self):
         """Move the pages in use to the front (sd2_pages_compact); returns their number, int32 [1]."""
         live = torch.empty(1, dtype=torch.int32, device=self.device)
-        with torch.cuda.device(self.device):
-            ws = self._workspace(self._pages_ws)
-            B.check(self.lib.sd2_pages_compact(ctypes.byref(self._pages), live.data_ptr(), ws.data_ptr(),
-                                               self._pages_ws, self._stream()), None, "sd2_pages_compact")
+        ws = self._workspace(self._pages_ws)
+        self._call(self.lib.sd2_pages_compact, ctypes.byref(self._pages), live.data_ptr(), ws.data_ptr(), self._pages_ws)
         return live
