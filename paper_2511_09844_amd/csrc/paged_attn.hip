@@ -83,24 +83,79 @@ __device__ __forceinline__ void put(const PagedAttnArgs& a, int row, int c, cons
 // The keys a workgroup of k_pdecode takes at a time, 16 or 32 per wave.
 template <typename T>
 constexpr int kBlockKeys = sizeof(T) == 2 ? 32 : 16;
-// Waves of a workgroup: as many as two per SIMD, with up to 32 query vectors (see Block: one buffer then).
-constexpr int kDecodeWaves = 8;
+constexpr int kDecodeWaves = 4;
 
 struct DecodeArgs {
     PagedAttnArgs a;
-    int ncg;         // groups of 16 NT query vectors of a sequence and KV head, at most
-    int nspan;       // workgroups that share a group's keys
-    float* part;     // partials: [group][span][16 NT][HD] sums, then [group][span][16 NT] (maximum, sum)
-    int64_t ml;      // floats of the first
+    int ncg;       // groups of 16 NT query vectors of a sequence and KV head, at most
+    int target;    // units that the sequences are to come to (see units_of); 0: one each
+    int min_keys;  // of a unit
+    int units;     // units there may be
+    float* part;   // partials: [unit][KV head][cg] of [16 NT][HD] sums, then of [16 NT] (maximum, sum)
+    int64_t ml;    // floats of the first
 };
 
-// Keys of a span, and spans that have keys, of a sequence of n positions.
+// How the keys are dealt out.  A unit is up to `keys` positions of one sequence, the same number for all, so
+// that workgroups (a unit, KV head and group of query vectors each) get equal work however the
+// lengths differ; it follows from the lengths on the device, which a captured call does not know
+// when it is recorded.  Sequence b has the units from first[b] on.  keys is at least the total over
+// target, so that there are at most target + nseq units.
+struct Units {
+    int keys, b, first, count, end;  // of sequence b: its units, and its positions (those there are pages for)
+};
+
+// Positions of sequence b, 0 without rows.
+__device__ __forceinline__ int seq_end(const PagedAttnArgs& a, int b) {
+    int n;
+    const int r0 = paged_rows(a.r, b, n);
+    return n > 0 ? (int)min((int64_t)paged_len(a.r, b, r0, n), (int64_t)a.c.max_pages << a.c.shift) : 0;
+}
+
+// The sequence that unit `unit` belongs to (b = -1: none), or sequence `b` itself when unit is negative.
 template <typename T>
-__device__ __forceinline__ int span_keys(int n, int nspan, int& live) {
+__device__ __forceinline__ Units units_of(const DecodeArgs& d, int unit, int b) {
     constexpr int step = kDecodeWaves * kBlockKeys<T>;
-    const int keys = max(((n + nspan - 1) / nspan + step - 1) / step * step, step);
-    live = (n + keys - 1) / keys;
-    return keys;
+    const PagedAttnArgs& a = d.a;
+    Units u;
+    if (!d.target) {
+        u.b = unit < 0 ? b : unit < a.r.nseq ? unit : -1;
+        u.first = u.b;
+        u.count = 1;
+        u.end = u.b >= 0 ? seq_end(a, u.b) : 0;
+        u.keys = INT32_MAX;
+        return u;
+    }
+    const int lane = threadIdx.x & 63, nseq = a.r.nseq;
+    int mine = lane < nseq ? seq_end(a, lane) : 0;
+    float total = (float)mine;
+    for (int b0 = 64; b0 < nseq; b0 += 64) total += b0 + lane < nseq ? (float)seq_end(a, b0 + lane) : 0.f;
+    total = wave_sum_dpp(total);
+    // (rounded up past what the sum may have lost)
+    const float want = fmaxf(total / (float)d.target * 1.00001f, (float)d.min_keys);
+    u.keys = want < 1.0e9f ? ((int)want + step) / step * step : 1 << 30;
+    u.b = -1;
+    int at = 0;
+    for (int b0 = 0; b0 < nseq; b0 += 64) {
+        if (b0) mine = b0 + lane < nseq ? seq_end(a, b0 + lane) : 0;
+        const int cnt = b0 + lane < nseq ? max((int)(((int64_t)mine + u.keys - 1) / u.keys), 1) : 0;
+        int inc = cnt;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int y = __shfl_up(inc, o, 64);
+            if (lane >= o) inc += y;
+        }
+        const uint64_t here = unit < 0 ? (b >= b0 && b < b0 + 64 ? (uint64_t)1 << (b - b0) : 0) : __ballot(unit < at + inc);
+        if (here) {
+            const int l = __builtin_ctzll(here);
+            u.b = b0 + l;
+            u.first = at + __builtin_amdgcn_readlane(inc - cnt, l);
+            u.count = __builtin_amdgcn_readlane(cnt, l);
+            u.end = __builtin_amdgcn_readlane(mine, l);
+            break;
+        }
+        at += __builtin_amdgcn_readlane(inc, 63);
+    }
+    return u;
 }
 
 // One block of keys in registers, as loaded.
@@ -267,26 +322,25 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     const PagedAttnArgs& a = d.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
-    // groups of one sequence and KV head that read the same keys lie on one XCD (workgroups go round
+    // groups of one unit and KV head that read the same keys lie on one XCD (workgroups go round
     // them in turn)
-    const int units = a.r.nseq * a.c.Hkv * d.nspan, units8 = (units + 7) / 8 * 8;
-    const int cg = blockIdx.x / units8, unit = blockIdx.x % units8;
-    if (unit >= units) return;
-    const int span = unit % d.nspan, kvh = unit / d.nspan % a.c.Hkv, b = unit / d.nspan / a.c.Hkv;
+    const int per = (d.units * a.c.Hkv + 7) / 8 * 8;
+    const int cg = blockIdx.x / per, unit = blockIdx.x % per / a.c.Hkv, kvh = blockIdx.x % per % a.c.Hkv;
+    if (unit >= d.units) return;
+    const Units un = units_of<T>(d, unit, 0);
+    const int b = un.b;
+    if (b < 0) return;
     const int G = a.H / a.c.Hkv;
     int nrows;
     const int r0 = paged_rows(a.r, b, nrows);
     const int nqv = nrows * G, v0 = cg * QV;
     if (v0 >= nqv) return;
     const int len = paged_len(a.r, b, r0, nrows);
-    // positions that some row of this group reads
-    const int last = len - nrows + min(v0 + QV - 1, nqv - 1) / G;
-    const int end = min(last + 1, (int64_t)a.c.max_pages << a.c.shift);
-    int live;
-    const int keys = span_keys<T>(max(end, 0), d.nspan, live);
-    const int64_t group = ((int64_t)b * a.c.Hkv + kvh) * d.ncg + cg;
-    if (span >= max(live, 1)) return;
-    const int kb = span * keys, ke = min(end, kb + keys);
+    // the unit's positions that some row of this group reads
+    const int kb = (unit - un.first) * un.keys;
+    const int ke = min(min(len - nrows + min(v0 + QV - 1, nqv - 1) / G + 1, un.end), un.count > 1 ? kb + un.keys : INT32_MAX);
+    const bool whole_seq = un.count == 1;
+    const int64_t slot = ((int64_t)unit * a.c.Hkv + kvh) * d.ncg + cg;
     u4 q[NT][B::NK];
     int pos[NT];
 #pragma unroll
@@ -405,7 +459,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int v = v0 + 16 * j + n;
-        const float inv = d.nspan > 1 ? 1.f : lt[j] > 0.f ? 1.f / lt[j] : 0.f;
+        const float inv = !whole_seq ? 1.f : lt[j] > 0.f ? 1.f / lt[j] : 0.f;
 #pragma unroll
         for (int u = 0; u < B::VU; ++u) {
             float y[4 * B::VW];
@@ -414,41 +468,40 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
 #pragma unroll
                 for (int e = 0; e < B::VW; ++e) y[r * B::VW + e] = acc.o[j][u * B::VW + e][r] * inv;
             const int c = (16 * u + 4 * g) * B::VW;
-            if (d.nspan > 1) {
-                float* p = d.part + ((group * d.nspan + span) * QV + 16 * j + n) * HD + c;
+            if (!whole_seq) {
+                float* p = d.part + (slot * QV + 16 * j + n) * HD + c;
 #pragma unroll
                 for (int i = 0; i < 4 * B::VW; i += 4) *(f4*)(p + i) = f4{y[i], y[i + 1], y[i + 2], y[i + 3]};
             } else if (v < nqv) {
                 put<T, 4 * B::VW>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
             }
         }
-        if (d.nspan > 1 && g == 0) {
-            float* p = d.part + d.ml + ((group * d.nspan + span) * QV + 16 * j + n) * 2;
+        if (!whole_seq && g == 0) {
+            float* p = d.part + d.ml + (slot * QV + 16 * j + n) * 2;
             *(f2*)p = f2{mt[j], lt[j]};
         }
     }
 }
 
-// The spans of a group joined: a thread per query vector and 4 columns.
+// The units of a sequence joined: a thread per query vector and 4 columns.
 template <typename T, int HD, int NT>
 __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
     constexpr int QV = 16 * NT, PER = 256 / (HD / 4);
     const PagedAttnArgs& a = d.a;
-    const int nb = (QV + PER - 1) / PER;
-    const int64_t group = blockIdx.x / nb;
+    const int nb = (QV + PER - 1) / PER, group = blockIdx.x / nb;
     const int i = blockIdx.x % nb * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4;
     const int cg = group % d.ncg, kvh = group / d.ncg % a.c.Hkv, b = group / d.ncg / a.c.Hkv, G = a.H / a.c.Hkv;
+    const Units un = units_of<T>(d, -1, b);
+    const int live = un.count;
+    if (live == 1) return;
     int nrows;
     const int r0 = paged_rows(a.r, b, nrows);
     const int nqv = nrows * G, v0 = cg * QV, v = v0 + i;
     if (i >= QV || v >= nqv) return;
-    const int len = paged_len(a.r, b, r0, nrows);
-    const int end = min(len - nrows + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift);
-    int live;
-    span_keys<T>(max(end, 0), d.nspan, live);
-    live = max(live, 1);
-    const float* po = d.part + (group * d.nspan * QV + i) * HD + c;
-    const float* pm = d.part + d.ml + (group * d.nspan * QV + i) * 2;
+    // from one unit's partials to the next
+    const int64_t slot = ((int64_t)un.first * a.c.Hkv + kvh) * d.ncg + cg, next = (int64_t)a.c.Hkv * d.ncg * QV;
+    const float* po = d.part + (slot * QV + i) * HD + c;
+    const float* pm = d.part + d.ml + (slot * QV + i) * 2;
     float m = -INFINITY, l = 0.f;
     f4 o = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < live; s0 += 8) {
@@ -456,7 +509,7 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
         f4 x[8];
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-            const int64_t k = (int64_t)min(s0 + s, live - 1) * QV;
+            const int64_t k = min(s0 + s, live - 1) * next;
             ml[s] = *(const f2*)(pm + k * 2);
             x[s] = *(const f4*)(po + k * HD);
         }
@@ -908,41 +961,48 @@ bool many_rows(const PagedView& c, const PagedRows& r, int H, bool bf16) {
     return qv > 64 && r.total_rows * G * c.Hkv >= 64 * (bf16 ? 256 : 128);
 }
 
+// Up to kDirect expected positions a sequence is one unit, which writes its rows itself.
+constexpr int kDirect = 256;
+
 struct DecodePlan {
-    int nt, ncg, nspan;
-    int64_t groups, ml;  // floats of the sums
+    int nt, ncg, target, units;
+    int64_t ml;  // floats of the sums
+    size_t bytes;
 };
 
-// room: floats of partials.
-DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t room) {
+// bytes: room for partials.
+DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes) {
     DecodePlan p;
     const int qv = std::min<int64_t>((int64_t)r.max_rows * (H / c.Hkv), 1 << 20);
     p.nt = qv <= 16 ? 1 : 2;
     p.ncg = (qv + 16 * p.nt - 1) / (16 * p.nt);
-    p.groups = (int64_t)std::max(r.nseq, 1) * c.Hkv * p.ncg;
-    const int64_t step = kDecodeWaves * (bf16 ? 32 : 16), most = std::min<int64_t>((max_len + 2 * step - 1) / (2 * step), 128);
-    p.nspan = (int)std::max<int64_t>(1, std::min<int64_t>(most, (512 + p.groups - 1) / p.groups));
-    const size_t per = (size_t)p.groups * 16 * p.nt * (c.hd + 2);
-    if (p.nspan > 1 && per * p.nspan > room) p.nspan = (int)std::max<size_t>(1, room / per);
-    p.ml = p.groups * p.nspan * 16 * p.nt * c.hd;
+    const int64_t groups = (int64_t)c.Hkv * p.ncg;
+    // two workgroups per CU, or as many units again as sequences
+    int64_t target = max_len <= kDirect ? 0 : std::max<int64_t>((512 + groups - 1) / groups, r.nseq);
+    const size_t per = (size_t)groups * 16 * p.nt * (c.hd + 2) * sizeof(float);
+    if (target && per * (target + r.nseq + 8) > bytes) target = std::max<int64_t>(0, (int64_t)(bytes / per) - r.nseq - 8);
+    p.target = (int)target;
+    p.units = (int)(target ? target + r.nseq + 8 : r.nseq);
+    p.ml = target ? (int64_t)p.units * groups * 16 * p.nt * c.hd : 0;
+    p.bytes = target ? per * p.units : 0;
     return p;
 }
 
 template <typename T, int HD, int NT>
 hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p, float* ws) {
-    const DecodeArgs d{a, p.ncg, p.nspan, ws, p.ml};
-    const int64_t units8 = ((int64_t)a.r.nseq * a.c.Hkv * p.nspan + 7) / 8 * 8;
-    if (units8 * p.ncg > INT32_MAX) return hipErrorInvalidValue;
-    const hipError_t err = launch(k_pdecode<T, HD, NT>, dim3((unsigned)(units8 * p.ncg)), dim3(64 * kDecodeWaves), s, d);
-    if (err != hipSuccess || p.nspan == 1) return err;
-    constexpr int per = 256 / (HD / 4), nb = (16 * NT + per - 1) / per;
-    return launch(k_pjoin<T, HD, NT>, dim3((unsigned)(p.groups * nb)), dim3(256), s, d);
+    const DecodeArgs d{a, p.ncg, p.target, kDecodeWaves * kBlockKeys<T>, p.units, ws, p.ml};
+    const int64_t per = ((int64_t)p.units * a.c.Hkv + 7) / 8 * 8;
+    if (per * p.ncg > INT32_MAX) return hipErrorInvalidValue;
+    const hipError_t err = launch(k_pdecode<T, HD, NT>, dim3((unsigned)(per * p.ncg)), dim3(64 * kDecodeWaves), s, d);
+    if (err != hipSuccess || !p.target) return err;
+    constexpr int q = 256 / (HD / 4), nb = (16 * NT + q - 1) / q;
+    return launch(k_pjoin<T, HD, NT>, dim3((unsigned)(a.r.nseq * a.c.Hkv * p.ncg * nb)), dim3(256), s, d);
 }
 
 template <typename T, int HD>
-hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws, size_t room) {
+hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws, size_t bytes) {
     if (many_rows(a.c, a.r, a.H, sizeof(T) == 2)) return prompt<T, HD>(s, a);
-    const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, room);
+    const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, bytes);
     return p.nt == 1 ? run_decode<T, HD, 1>(s, a, p, ws) : run_decode<T, HD, 2>(s, a, p, ws);
 }
 
@@ -951,17 +1011,16 @@ hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float*
 size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
     if (many_rows(c, r, H, bf16)) return 256;
     const DecodePlan p = decode_plan(c, r, H, bf16, max_len, SIZE_MAX);
-    return p.nspan == 1 ? 256 : (size_t)(p.ml + p.groups * p.nspan * 16 * p.nt * 2) * 4;
+    return std::max<size_t>(p.bytes, 256);
 }
 
 hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t ws_bytes) {
     float* const w = (float*)ws;
-    const size_t room = ws_bytes / sizeof(float);
     if (!a.r.total_rows || !a.r.nseq) return hipSuccess;
     switch (a.c.hd) {
-        case 32: return bf16 ? decode<uint16_t, 32>(s, a, max_len, w, room) : decode<float, 32>(s, a, max_len, w, room);
-        case 64: return bf16 ? decode<uint16_t, 64>(s, a, max_len, w, room) : decode<float, 64>(s, a, max_len, w, room);
-        case 128: return bf16 ? decode<uint16_t, 128>(s, a, max_len, w, room) : decode<float, 128>(s, a, max_len, w, room);
+        case 32: return bf16 ? decode<uint16_t, 32>(s, a, max_len, w, ws_bytes) : decode<float, 32>(s, a, max_len, w, ws_bytes);
+        case 64: return bf16 ? decode<uint16_t, 64>(s, a, max_len, w, ws_bytes) : decode<float, 64>(s, a, max_len, w, ws_bytes);
+        case 128: return bf16 ? decode<uint16_t, 128>(s, a, max_len, w, ws_bytes) : decode<float, 128>(s, a, max_len, w, ws_bytes);
         default: return hipErrorInvalidValue;
     }
 }
