@@ -56,6 +56,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
 }
 
+// A value that is the same in all lanes, in scalar registers (the compiler does not see it of one that
+// was loaded through vector memory).
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
 // n neighbouring output values of a row (n columns from c, a multiple of n).
 template <typename T, int N>
 __device__ __forceinline__ void put(const PagedAttnArgs& a, int row, int c, const float* v) {
@@ -183,8 +190,9 @@ __device__ __forceinline__ void load_block(Block<T, HD>& x, const PagedView& c, 
 #pragma unroll
     for (int t = 0; t < B::TK; ++t) {
         const int key = k0 + 16 * t;
-        const int rows = page[t] < 0 ? 0 : max(min(end - key, 16), 0);
-        const int64_t at = (int64_t)max(page[t], 0) * c.page_stride + (((int64_t)kvh << c.shift) + (key & ((1 << c.shift) - 1))) * HD;
+        const int rows = uniform(page[t] < 0 ? 0 : max(min(end - key, 16), 0));
+        const int64_t at = uniform((int64_t)max(page[t], 0) * c.page_stride +
+                                   (((int64_t)kvh << c.shift) + (key & ((1 << c.shift) - 1))) * HD);
         if constexpr (WHAT & kLoadK) {
             const auto rk = __builtin_amdgcn_make_buffer_rsrc((T*)c.k + at, 0, rows * RB, 0x00020000);
 #pragma unroll
@@ -483,6 +491,36 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     }
 }
 
+// `live` partials, `next` query vectors apart, joined: 4 columns of one.
+__device__ __forceinline__ f4 join_parts(const float* po, const float* pm, int live, int64_t next, int hd) {
+    float m = -INFINITY, l = 0.f;
+    f4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < live; s0 += 8) {
+        f2 ml[8];
+        f4 x[8];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const int64_t k = min(s0 + s, live - 1) * next;
+            ml[s] = *(const f2*)(pm + k * 2);
+            x[s] = *(const f4*)(po + k * hd);
+        }
+        float mn = m;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) mn = fmaxf(mn, ml[s][0]);
+        const float base = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m - base);
+        l *= f;
+        o *= f;
+        m = mn;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float w = s0 + s < live ? __builtin_amdgcn_exp2f(ml[s][0] - base) : 0.f;
+            l += w * ml[s][1];
+            o += w * x[s];
+        }
+    }
+    return o * (l > 0.f ? 1.f / l : 0.f);
+}
+
 // The units of a sequence joined: a thread per query vector and 4 columns.
 template <typename T, int HD, int NT>
 __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
@@ -502,54 +540,39 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
     const int64_t slot = ((int64_t)un.first * a.c.Hkv + kvh) * d.ncg + cg, next = (int64_t)a.c.Hkv * d.ncg * QV;
     const float* po = d.part + (slot * QV + i) * HD + c;
     const float* pm = d.part + d.ml + (slot * QV + i) * 2;
-    float m = -INFINITY, l = 0.f;
-    f4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < live; s0 += 8) {
-        f2 ml[8];
-        f4 x[8];
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            const int64_t k = min(s0 + s, live - 1) * next;
-            ml[s] = *(const f2*)(pm + k * 2);
-            x[s] = *(const f4*)(po + k * HD);
-        }
-        float mn = m;
-#pragma unroll
-        for (int s = 0; s < 8; ++s) mn = fmaxf(mn, ml[s][0]);
-        const float base = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m - base);
-        l *= f;
-        o *= f;
-        m = mn;
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            const float w = s0 + s < live ? __builtin_amdgcn_exp2f(ml[s][0] - base) : 0.f;
-            l += w * ml[s][1];
-            o += w * x[s];
-        }
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    const float y[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    const f4 o = join_parts(po, pm, live, next, HD);
+    const float y[4] = {o[0], o[1], o[2], o[3]};
     put<T, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
 }
 
 // ---------------------------------------------------------------------------------------------
-// Many rows per sequence (prompts): k_pprompt.  A workgroup takes 256 (bf16) query vectors of a sequence
-// and KV head, 64 per wave as two column tiles of 32, and goes through the keys in tiles of KT that its
-// four waves stage in LDS, requested one tile ahead.  The products are those of k_pdecode on 32 x 32 tiles:
-// in the result of S^T = K Q^T lane group g holds keys 8 (r / 4) + 4 g + r % 4, r < 16, of one query vector,
-// which are the contraction slots of two PV products.  LDS holds both operands as the lanes read
-// them, a fragment of 64 x 16 bytes after the other: K as it is (two waves), V permuted on the way
-// from memory so that 16 bytes are eight keys of one column (the other two); within a fragment the 16-byte
-// units are permuted so that neither side meets bank conflicts.
-// The running maximum is raised only when a score exceeds it by 2^kLazy: until then the weights
-// are at most that large, and the sums need no rescaling.
+// Many rows per sequence (prompts): k_pprompt_bf16.  A workgroup takes 256 query vectors of a sequence and
+// KV head, 32 to each of its eight waves, and goes through the keys in tiles of KT, whose K and V
+// arrive in LDS by themselves (loads with LDS as their destination), one tile ahead.  The products are
+// those of k_pdecode on 32 x 32 tiles: in the result of S^T = K Q^T lane group g holds keys 8 (r / 4) + 4 g +
+// r % 4, r < 16, of one query vector, which are the contraction slots of the two PV products.  V's
+// eight keys of a column come out of LDS by reads that turn 4 x 16 blocks.
+//
+// The two waves of a SIMD take turns: while one computes weights (vector instructions) the other has the
+// matrix cores and LDS (its sums with V, then the next block's scores, the operands of both read
+// meanwhile); a barrier after each turn keeps them apart.  Unsynchronised, both tended to want the same unit:
+// 8192 positions, 32/8 heads of 128, took 660 us that way, 570 in turns.
+//
+// The running maximum is raised only when a weight exceeds 2^kLazy: until then the sums need no
+// rescaling, and a block's scores no maximum, since large weights show in their bits.
+//
+// With few workgroups the keys of each are split into spans, whose partial sums k_prompt_join joins.
 // ---------------------------------------------------------------------------------------------
 typedef float f16v __attribute__((ext_vector_type(16)));
-constexpr float kLazy = 8.f;
+constexpr int kLazy = 8;
+constexpr int kPromptWaves = 8;
 
 struct PromptArgs {
     PagedAttnArgs a;
-    int tiles;  // workgroups of a KV head
+    int tiles;    // workgroups of a KV head and span
+    int nspan;
+    float* part;  // partials: [tile][KV head][span] of [QV][HD] sums, then of [QV] (maximum, sum)
+    int64_t ml;   // floats of the first
 };
 
 // Maximum and sum over the two halves of a wave.
@@ -562,237 +585,328 @@ __device__ __forceinline__ float half_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Which sequence workgroup `tile` of a KV head belongs to, and its first query vector there: QV to a
-// workgroup, sequence after sequence.  -1: none.
+// Workgroup w of a KV head: its sequence (-1: none) and first query vector there.  A sequence's tiles of QV
+// query vectors are numbered from its first row on, and the last tiles of all sequences go first, since
+// they read the most keys.
 template <int QV>
-__device__ __forceinline__ int prompt_tile(const PagedRows& r, int G, int tile, int& v0) {
+__device__ __forceinline__ int prompt_tile(const PagedRows& r, int G, int w, int& v0) {
+    const int most = ((int64_t)r.max_rows * G + QV - 1) / QV;  // of a sequence
     if (!r.row_off) {
-        const int per = ((int64_t)r.max_rows * G + QV - 1) / QV;
-        v0 = tile % per * QV;
-        return tile / per;
+        v0 = w < most * r.nseq ? (most - 1 - w / r.nseq) * QV : 0;
+        return w < most * r.nseq ? w % r.nseq : -1;
     }
     const int lane = threadIdx.x & 63;
-    int at = 0;
-    for (int b0 = 0; b0 < r.nseq; b0 += 64) {
+    auto tiles_of = [&](int b) {
         int n = 0;
-        if (b0 + lane < r.nseq) paged_rows(r, b0 + lane, n);
-        const int mine = ((int64_t)n * G + QV - 1) / QV;
-        int inc = mine;
+        if (b < r.nseq) paged_rows(r, b, n);
+        return (int)(((int64_t)n * G + QV - 1) / QV);
+    };
+    const int mine = tiles_of(lane);
+    // tiles numbered j or more
+    auto from = [&](int j) {
+        int n = max(mine - j, 0);
+        for (int b0 = 64; b0 < r.nseq; b0 += 64) n += max(tiles_of(b0 + lane) - j, 0);
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int y = __shfl_up(inc, d, 64);
-            if (lane >= d) inc += y;
+        for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+        return uniform(n);
+    };
+    // the largest j with more than w of them
+    if (from(0) <= w) return -1;
+    int lo = 0, hi = most;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (from(mid) > w) lo = mid;
+        else hi = mid;
+    }
+    v0 = lo * QV;
+    int rank = w - from(lo + 1);  // among the sequences that have a tile lo
+    for (int b0 = 0; b0 < r.nseq; b0 += 64) {
+        const bool has = (b0 ? tiles_of(b0 + lane) : mine) > lo;
+        const uint64_t m = __ballot(has);
+        const int c = __popcll(m);
+        if (rank < c) {
+            const bool me = has && __popcll(m & (((uint64_t)1 << lane) - 1)) == rank;
+            return uniform(b0 + (int)__builtin_ctzll(__ballot(me)));
         }
-        const uint64_t here = __ballot(tile < at + inc);
-        if (here) {
-            const int l = __builtin_ctzll(here);
-            v0 = (tile - at - __shfl(inc - mine, l, 64)) * QV;
-            return __builtin_amdgcn_readfirstlane(b0 + l);
-        }
-        at += __shfl(inc, 63, 64);
+        rank -= c;
     }
     return -1;
 }
 
+// The keys of a tile that workgroup (span `span`) reads: `end` of them in all, in multiples of kt.
+struct Span {
+    int from, upto, live;  // spans that have keys
+};
+__device__ __forceinline__ Span prompt_span(int end, int nspan, int span, int kt) {
+    Span s;
+    const int keys = max((int)(((int64_t)(end + nspan - 1) / nspan + kt - 1) / kt) * kt, kt);
+    s.live = max((int)(((int64_t)end + keys - 1) / keys), 1);
+    s.from = span * keys;
+    s.upto = min(end, s.from + keys);
+    return s;
+}
+
 template <int HD>
-__global__ __launch_bounds__(256, 1) void k_pprompt_bf16(PromptArgs d) {
-    constexpr int KT = 64 * 128 / HD, NB = KT / 32, NS = HD / 16, NC = HD / 32, CH = HD / 8, QV = 256;
-    __shared__ __attribute__((aligned(16))) u4 ks[2][KT * CH], vs[2][KT * CH];
+__global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArgs d) {
+    constexpr int NW = kPromptWaves, KT = 16 * NW * 128 / HD, NB = KT / 32, NS = HD / 16, NC = HD / 32, CH = HD / 8;
+    constexpr int QV = 32 * NW, RB = HD * 2;
+    __shared__ __attribute__((aligned(1024))) char ks[2][KT * RB], vs[2][KT * RB];
     const PagedAttnArgs& a = d.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, g = lane >> 5;
     const int G = a.H / a.c.Hkv;
-    // KV heads lie on XCDs in turn, each sequence's last rows, which read the most keys, go first
-    const int kvh = blockIdx.x % a.c.Hkv;
+    // (KV heads lie on XCDs in turn)
+    const int kvh = blockIdx.x % a.c.Hkv, span = blockIdx.x / a.c.Hkv % d.nspan, tile = blockIdx.x / a.c.Hkv / d.nspan;
     int v0 = 0;
-    const int b = prompt_tile<QV>(a.r, G, d.tiles - 1 - blockIdx.x / a.c.Hkv, v0);
+    const int b = prompt_tile<QV>(a.r, G, tile, v0);
     if (b < 0) return;
-    v0 = __builtin_amdgcn_readfirstlane(v0);
     int nrows;
     const int r0 = paged_rows(a.r, b, nrows);
     const int nqv = nrows * G;
     if (v0 >= nqv) return;
     const int len = paged_len(a.r, b, r0, nrows), at0 = len - nrows;
-    const int wv = v0 + 64 * wave;                       // the wave's first query vector
-    const int end = min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift);
-    const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 63, nqv - 1) / G + 1) : 0;
-    u4 q[2][NS];
-    int pos[2];
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, span, KT);
+    if (span >= sp.live) return;
+    const int end = sp.upto;
+    const int wv = v0 + 32 * wave;                       // the wave's first query vector
+    const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 31, nqv - 1) / G + 1) : 0;
+    u4 q[NS];
     // (a negative scale turns into the sign of q)
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
     const float c = fabsf(a.scale) * kLog2e;
+    const int v = wv + n, vc = min(v, nqv - 1), pos = at0 + vc / G;
+    {
+        const uint16_t* p = (const uint16_t*)a.q + (r0 + vc / G) * a.q_stride + (kvh * G + vc % G) * HD + 8 * g;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int v = min(wv + 32 * t + n, nqv - 1);
-        pos[t] = at0 + v / G;
-        const uint16_t* p = (const uint16_t*)a.q + (r0 + v / G) * a.q_stride + (kvh * G + v % G) * HD + 8 * g;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) q[t][s] = *(const u4*)(p + 16 * s) ^ flip;
+        for (int s = 0; s < NS; ++s) q[s] = *(const u4*)(p + 16 * s) ^ flip;
     }
-    f16v o[2][NC];
-    float m[2], l[2];
+    f16v o[NC];
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        m[t] = -INFINITY;
-        l[t] = 0.f;
+    for (int i = 0; i < NC; ++i)
 #pragma unroll
-        for (int i = 0; i < NC; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[t][i][r] = 0.f;
-    }
-    // pages of the KT / 16 groups of keys of a tile, a lane each
+        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    // table entries of the KT / 16 groups of keys of a tile, a lane each, and the pages they name (apart: the
+    // first test of an entry waits for it, and for all loads before)
     auto look = [&](int k0) {
         const int key = k0 + 16 * lane;
-        return lane < KT / 16 && key < end ? paged_page(a.c, b, key >> a.c.shift) : -1;
+        int e = -1;
+        if (lane < KT / 16 && key < end) e = a.c.table[(int64_t)b * a.c.max_pages + (key >> a.c.shift)];
+        return e;
     };
+    auto named = [&](int e) { return (uint32_t)e < (uint32_t)a.c.n_pages ? e : -1; };
     const int mask = (1 << a.c.shift) - 1;
-    const bool isv = wave < 2;
-    const int kw = (wave & 1) * (KT / 2);                // the half of the tile that this wave stages
-    u4 st[8];
-    // V: the lane's eight keys 16 u + 8 (j / 4) + 4 vg + j % 4 and eight columns
-    const int vch = lane % CH, vg = lane / CH & 1, vu = lane / (2 * CH);
-    auto load = [&](int k0, int pg) {
-        if (isv) {
-            const int key = k0 + kw + 16 * vu, page = __shfl(pg, kw / 16 + vu, 64);
-            const int rows = page < 0 ? 0 : min(end - key, 16);
-            const uint16_t* p = (const uint16_t*)a.c.v + max(page, 0) * a.c.page_stride +
-                                (((int64_t)kvh << a.c.shift) + (key & mask)) * HD + 8 * vch;
-            if (__all(rows == 16)) {
+    // This wave's groups of 16 keys of a tile, straight into LDS, 1 KB an instruction: 16-byte unit u of a
+    // row at u ^ (row % 8) (K) and u ^ 2 (row % 4) (V).  Rows that do not exist arrive as zeros.
+    constexpr int RL = 16 / CH, RI = 64 / CH, NI = 16 / RI;  // rows of 256 bytes; rows of an instruction, instructions of a group
+    const int lrow = lane / CH, lch = lane % CH;
+    auto load = [&](int k0, int pg, int buf) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) st[j] = *(const u4*)(p + (8 * (j / 4) + 4 * vg + j % 4) * HD);
-            } else {
-                // rows that do not exist: another row's address, and zeros
+        for (int w = 0; w < KT / 8 / NW; ++w) {
+            const int task = wave + w * NW, grp = task % (KT / 16), key = k0 + 16 * grp, page = __builtin_amdgcn_readlane(pg, grp);
+            const int rows = uniform(page < 0 ? 0 : max(min(end - key, 16), 0));
+            const int64_t at = max(page, 0) * a.c.page_stride + (((int64_t)kvh << a.c.shift) + (key & mask)) * HD;
+            const bool isv = task >= KT / 16;
+            const int64_t base = uniform((int64_t)((uint16_t*)(isv ? a.c.v : a.c.k) + at));
+            const u4 rs = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffff, (uint32_t)(rows * RB), 0x00020000};
+            typedef __attribute__((address_space(3))) char* lds;
+            const uint32_t to = uniform((int)(uint32_t)(uintptr_t)(lds)((isv ? vs[buf] : ks[buf]) + grp * 16 * RB));
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int row = 8 * (j / 4) + 4 * vg + j % 4;
-                    st[j] = *(const u4*)(p + (row < rows ? row : 0) * HD);
-                    st[j] = row < rows ? st[j] : u4{0, 0, 0, 0};
-                }
-            }
-        } else {
-            constexpr int RI = 64 / CH;  // rows of an instruction
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int tile = kw / 16 + i * RI / 16, key = k0 + 16 * tile;
-                const int page = __builtin_amdgcn_readlane(pg, tile);
-                const int rows = page < 0 ? 0 : max(min(end - key, 16), 0);
-                const uint16_t* p = (const uint16_t*)a.c.k + max(page, 0) * a.c.page_stride +
-                                    (((int64_t)kvh << a.c.shift) + (key & mask)) * HD;
-                const auto rk = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, rows * HD * 2, 0x00020000);
-                st[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, ((i * RI % 16 + lane / CH) * HD + lane % CH * 8) * 2, 0, 0);
+            for (int i = 0; i < NI; ++i) {
+                const int row = i * RI + lrow;
+                const int off = row * RB + ((lch ^ ((isv ? 4 * ((row & 3) / RL) : row / RL) & (CH - 1))) * 16);
+                // (no builtin: with it every read of LDS waits for what is still on its way to the other buffers;
+                // `meet` below says who waits for what)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                             :: "s"(to + i * 1024), "v"(off), "s"(rs) : "memory");
             }
         }
     };
-    auto store = [&](int buf) {
-        if (isv) {
-            // column 8 vch + i of the lane's keys: fragment (16-key group, 32 columns), lane vg * 32 + column % 32
-            const int f = ((kw / 16 + vu) * NC + vch / 4) * 64 + vg * 32 + vch % 4 * 8;
-            const int x = (vg * 4 + vch % 4) ^ (vch / 4 % 2 * 4);
+    const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
+    const int nk = (wend + 31) / 32;  // blocks of 32 keys up to the last that this wave computes
+    // K: row n of a block, units 2 i + g
+    int ka[NS], va[NC];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                u4 w;
+    for (int i = 0; i < NS; ++i) ka[i] = n * RB + (((2 * i + g) ^ (n / RL & (CH - 1))) * 16);
+    // V: four keys of 16 columns, turned by the read: a lane of 16 reads four columns of key lane / 4
+    const int vk = (lane & 15) / 4;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    w[e] = __builtin_amdgcn_perm(st[2 * e + 1][i / 2], st[2 * e][i / 2], i % 2 ? 0x07060302 : 0x05040100);
-                vs[buf][f + (i ^ x)] = w;
-            }
-        } else {
-            constexpr int RI = 64 / CH;
+    for (int i = 0; i < NC; ++i)
+        va[i] = (4 * g + vk) * RB + (((4 * i + (lane >> 4 & 1) * 2 + (lane & 3) / 2) ^ (4 * (vk / RL) & (CH - 1))) * 16) + (lane & 1) * 8;
+    u4 kr[NS];
+    auto keys = [&](const char* kf, int kb) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int row = kw + i * RI + lane / CH, cc = lane % CH;
-                const int at = (cc & 1) * 32 + row % 32;
-                ks[buf][(row / 32 * NS + cc / 2) * 64 + (at & ~7) + ((at ^ cc) & 7)] = st[i];
-            }
-        }
+        for (int i = 0; i < NS; ++i) kr[i] = *(const u4*)(kf + ka[i] + kb * 32 * RB);
     };
-    const int nt = end > 0 ? (end + KT - 1) / KT : 0;
-    int pg = look(0);
-    uint64_t have = __ballot(pg >= 0);
-    load(0, pg);
-    pg = look(KT);
-    store(0);
-    for (int t = 0; t < nt; ++t) {
-        __syncthreads();
-        const uint64_t now = have;
-        if (t + 1 < nt) {
-            have = __ballot(pg >= 0);
-            load((t + 1) * KT, pg);
-            pg = look((t + 2) * KT);
+    auto scores = [&](f16v& s) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, kr[i]), __builtin_bit_cast(b8, q[i]), s, 0, 0, 0);
+    };
+    auto most = [&](const f16v& s) {
+        float mx[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx[r] = fmaxf(fmaxf(s[r], s[r + 4]), fmaxf(s[r + 8], s[r + 12]));
+        return half_max(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]))) * c;
+    };
+    // block k's scores made ready: those that are not read at -inf, and the maximum raised to them
+    auto settle = [&](f16v& s, int k, uint32_t hv) {
+        const int k0 = 32 * k;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int key = 8 * (r / 4) + 4 * g + r % 4;
+            s[r] = k0 + key <= pos && (hv >> (r / 8) & 1) ? s[r] : -INFINITY;
         }
-        const u4 *kf = ks[t & 1], *vf = vs[t & 1];
+        const float mn = fmaxf(m, most(s)), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) o[i] *= f;
+    };
+    // (bf16, see block_sums; their sum from before the rounding)
+    auto weights = [&](const f16v& s, u4 (&p)[2]) {
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -base)),
+                        y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], c, -base));
+            sum[0] += x;
+            sum[1] += y;
+            p[r / 8][r % 8 / 2] = pack_bf16(x, y);
+        }
+        return sum[0] + sum[1];
+    };
+    // Whether a weight exceeds 2^kLazy (or is no number): they are positive, so their bits compare as integers do.
+    typedef uint16_t h2 __attribute__((ext_vector_type(2)));
+    auto large = [&](const u4 (&p)[2]) {
+        h2 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __builtin_elementwise_max(__builtin_bit_cast(h2, p[0][i]), __builtin_bit_cast(h2, p[1][i]));
+        const h2 y = __builtin_elementwise_max(__builtin_elementwise_max(x[0], x[1]), __builtin_elementwise_max(x[2], x[3]));
+        return max(y[0], y[1]) > (uint16_t)((127 + kLazy) << 7);
+    };
+    typedef short h4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) h4* ldsv;
+    auto values = [&](u4 (&x)[2][NC], const char* vf, int kb) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const char* p = vf + va[i] + (kb * 32 + 16 * u) * RB;
+                const u2 lo = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldsv)p));
+                const u2 hi = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldsv)(p + 8 * RB)));
+                x[u][i] = u4{lo[0], lo[1], hi[0], hi[1]};
+            }
+    };
+    auto sums = [&](const u4 (&p)[2], const u4 (&x)[2][NC]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < NC; ++i)
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, x[u][i]), __builtin_bit_cast(b8, p[u]), o[i], 0, 0, 0);
+    };
+    auto meet = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const bool late = wave >= NW / 2;
+    const int nkw = (end + 31) / 32;  // of the workgroup
+    int pg = named(look(t0 * KT));
+    uint64_t have = __ballot(pg >= 0), next = 0;
+    load(t0 * KT, pg, t0 & 1);
+    int entry = look((t0 + 1) * KT);
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    __syncthreads();
+    f16v s;
+    u4 x[2][NC];
+    if (t0 * NB < nk) {
+        keys(ks[t0 & 1], 0);
+        scores(s);
+        values(x, vs[t0 & 1], 0);
+    }
+    bool begun = false;  // every query vector has a maximum
+    if (late) meet();
+    for (int t = t0; t < nt; ++t) {
+        const char *kf = ks[t & 1], *vf = vs[t & 1], *kn = ks[(t + 1) & 1], *vn = vs[(t + 1) & 1];
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb) {
-            const int k0 = t * KT + 32 * kb;
-            if (k0 >= wend) break;
-            f16v s[2];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[0][r] = s[1][r] = 0.f;
-#pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                const b8 x = __builtin_bit_cast(b8, kf[(kb * NS + i) * 64 + (lane & ~7) + ((lane ^ (2 * i + g)) & 7)]);
-                s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(b8, q[0][i]), s[0], 0, 0, 0);
-                s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(b8, q[1][i]), s[1], 0, 0, 0);
+            const int k = t * NB + kb;
+            if (k >= nkw) break;
+            if (kb == 0) {
+                pg = named(entry);
+                next = __ballot(pg >= 0);
+                if (t + 1 < nt) load((t + 1) * KT, pg, (t + 1) & 1);
+                entry = look((t + 2) * KT);
             }
-            const uint32_t hv = now >> (2 * kb) & 3;
-            if (k0 + 31 > wfirst || hv != 3) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int key = 8 * (r / 4) + 4 * g + r % 4;
-                        s[j][r] = k0 + key <= pos[j] && (hv >> (r / 8) & 1) ? s[j][r] : -INFINITY;
-                    }
-            }
-            u4 p[2][2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float mx = s[j][0];
-#pragma unroll
-                for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[j][r]);
-                mx = half_max(mx) * c;
-                if (__any(mx > m[j] + kLazy)) {
-                    const float mn = fmaxf(m[j], mx), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[j] - mn);
-                    m[j] = mn;
-                    l[j] *= f;
-#pragma unroll
-                    for (int i = 0; i < NC; ++i) o[j][i] *= f;
-                }
-                const float base = m[j] == -INFINITY ? 0.f : m[j];
+            u4 p[2];
+            if (k < nk) {
+                const uint32_t hv = have >> (2 * kb) & 3;
+                bool settled = begun && 32 * k + 31 <= wfirst && hv == 3;
                 float sum = 0.f;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r], c, -base));
-                    sum += s[j][r];
+                if (settled) {
+                    sum = weights(s, p);
+                    settled = !__any(large(p));
                 }
-                l[j] += sum;
-#pragma unroll
-                for (int r = 0; r < 16; r += 2) p[j][r / 8][r % 8 / 2] = pack_bf16(s[j][r], s[j][r + 1]);
+                if (!settled) {
+                    settle(s, k, hv);
+                    sum = weights(s, p);
+                    begun = !__any(m == -INFINITY);
+                }
+                l += sum;
             }
+            if (!late && kb == NB - 1) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+            __builtin_amdgcn_s_waitcnt(0xc07f);                             // lgkmcnt(0)
+            meet();
+            if (k < nk) {
+                __builtin_amdgcn_s_setprio(1);
+                keys(kb + 1 < NB ? kf : kn, (kb + 1) % NB);
+                sums(p, x);
+                scores(s);
+                values(x, kb + 1 < NB ? vf : vn, (kb + 1) % NB);
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < NC; ++i) {
-                    const b8 x = __builtin_bit_cast(b8, vf[((2 * kb + u) * NC + i) * 64 + (lane & ~7) + ((lane ^ (lane >> 3) ^ (i % 2 * 4)) & 7)]);
-                    o[0][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(b8, p[0][u]), o[0][i], 0, 0, 0);
-                    o[1][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(b8, p[1][u]), o[1][i], 0, 0, 0);
+                for (int i = 0; i < NS; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an LDS read
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
                 }
-        }
-        if (t + 1 < nt) store((t + 1) & 1);
-    }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int v = wv + 32 * j + n;
-        const float sum = half_sum(l[j]), inv = sum > 0.f ? 1.f / sum : 0.f;
-        if (v >= nqv) continue;
+                for (int i = 0; i < NS; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                }
+                __builtin_amdgcn_s_setprio(0);
+            }
+            if (late && kb == NB - 2) __builtin_amdgcn_s_waitcnt(0x0f70);
+            meet();
+        }
+        have = next;
+    }
+    if (!late) meet();
+    const float sum = half_sum(l);
+    if (v >= nqv) return;
+    if (sp.live > 1) {
+        const int64_t slot = ((int64_t)tile * a.c.Hkv + kvh) * d.nspan + span;
+        float* po = d.part + (slot * QV + wv - v0 + n) * HD + 4 * g;
 #pragma unroll
         for (int i = 0; i < NC; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const float y[4] = {o[j][i][r] * inv, o[j][i][r + 1] * inv, o[j][i][r + 2] * inv, o[j][i][r + 3] * inv};
-                put<uint16_t, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + 32 * i + 2 * r + 4 * g, y);
-            }
+            for (int r = 0; r < 16; r += 4) *(f4*)(po + 32 * i + 2 * r) = f4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+        if (g == 0) *(f2*)(d.part + d.ml + (slot * QV + wv - v0 + n) * 2) = f2{m, sum};
+        return;
     }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const float y[4] = {o[i][r] * inv, o[i][r + 1] * inv, o[i][r + 2] * inv, o[i][r + 3] * inv};
+            put<uint16_t, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + 32 * i + 2 * r + 4 * g, y);
+        }
 }
 
 // The same on fp32 matrix instructions, 32 query vectors per wave and tiles of 32 keys, row by row in LDS
@@ -806,18 +920,19 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, g = lane >> 5;
     const int G = a.H / a.c.Hkv;
-    const int kvh = blockIdx.x % a.c.Hkv;
+    const int kvh = blockIdx.x % a.c.Hkv, span = blockIdx.x / a.c.Hkv % d.nspan, tile = blockIdx.x / a.c.Hkv / d.nspan;
     int v0 = 0;
-    const int b = prompt_tile<QV>(a.r, G, d.tiles - 1 - blockIdx.x / a.c.Hkv, v0);
+    const int b = prompt_tile<QV>(a.r, G, tile, v0);
     if (b < 0) return;
-    v0 = __builtin_amdgcn_readfirstlane(v0);
     int nrows;
     const int r0 = paged_rows(a.r, b, nrows);
     const int nqv = nrows * G;
     if (v0 >= nqv) return;
     const int len = paged_len(a.r, b, r0, nrows), at0 = len - nrows;
     const int wv = v0 + 32 * wave;
-    const int end = min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift);
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, span, KT);
+    if (span >= sp.live) return;
+    const int end = sp.upto;
     const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 31, nqv - 1) / G + 1) : 0;
     const float c = a.scale * kLog2e;
     f4 q[HD / 8];
@@ -846,8 +961,8 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
         for (int i = 0; i < NU; ++i) {
             const int t = HD == 32 ? wave >> 1 : i * (1024 / HD) / 16, key = k0 + 16 * t;
             const int pg = HD == 32 ? (t ? page[1] : page[0]) : page[t];
-            const int rows = pg < 0 ? 0 : max(min(end - key, 16), 0);
-            const int64_t at = max(pg, 0) * a.c.page_stride + (((int64_t)kvh << a.c.shift) + (key & mask)) * HD;
+            const int rows = uniform(pg < 0 ? 0 : max(min(end - key, 16), 0));
+            const int64_t at = uniform(max(pg, 0) * a.c.page_stride + (((int64_t)kvh << a.c.shift) + (key & mask)) * HD);
             const int off = ((i * (1024 / HD) + tid / C4) % 16 * HD + tid % C4 * 4) * 4;
             st[0][i] = __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((float*)a.c.k + at, 0, rows * HD * 4, 0x00020000), off, 0, 0);
             st[1][i] = __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((float*)a.c.v + at, 0, rows * HD * 4, 0x00020000), off, 0, 0);
@@ -861,13 +976,13 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
             *(u4*)(vs[buf] + row * HD + x) = st[1][i];
         }
     };
-    const int nt = end > 0 ? (end + KT - 1) / KT : 0;
+    const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
     int pg[2], nx[2];
-    look(0, pg);
-    look(KT, nx);
-    load(0, pg);
-    store(0);
-    for (int t = 0; t < nt; ++t) {
+    look(t0 * KT, pg);
+    look((t0 + 1) * KT, nx);
+    load(t0 * KT, pg);
+    store(t0 & 1);
+    for (int t = t0; t < nt; ++t) {
         __syncthreads();
         const int k0 = t * KT;
         const bool whole = k0 + 31 <= wfirst && pg[0] >= 0 && pg[1] >= 0;
@@ -931,8 +1046,9 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
         }
         if (t + 1 < nt) store((t + 1) & 1);
     }
-    const float sum = half_sum(l), inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float sum = half_sum(l), inv = sp.live > 1 ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
     if (v >= nqv) return;
+    const int64_t at = (((int64_t)tile * a.c.Hkv + kvh) * d.nspan + span) * QV + wv - v0 + n;
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
         float y[4 * VW];
@@ -940,29 +1056,91 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int i = 0; i < VW; ++i) y[e * VW + i] = o[i][r + e] * inv;
-        put<float, 4 * VW>(a, r0 + v / G, (kvh * G + v % G) * HD + (2 * r + 4 * g) * VW, y);
+        const int col = (2 * r + 4 * g) * VW;
+        if (sp.live > 1) {
+#pragma unroll
+            for (int i = 0; i < 4 * VW; i += 4) *(f4*)(d.part + at * HD + col + i) = f4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+        } else {
+            put<float, 4 * VW>(a, r0 + v / G, (kvh * G + v % G) * HD + col, y);
+        }
     }
+    if (sp.live > 1 && g == 0) *(f2*)(d.part + d.ml + at * 2) = f2{m, sum};
+}
+
+// The spans of k_pprompt's tiles joined: a thread per query vector and 4 columns.
+template <typename T, int HD, int QV, int KT>
+__global__ __launch_bounds__(256) void k_prompt_join(PromptArgs d) {
+    constexpr int PER = 256 / (HD / 4), NBK = QV / PER;
+    const PagedAttnArgs& a = d.a;
+    const int kvh = blockIdx.x / NBK % a.c.Hkv, tile = blockIdx.x / NBK / a.c.Hkv, G = a.H / a.c.Hkv;
+    int v0 = 0;
+    const int b = prompt_tile<QV>(a.r, G, tile, v0);
+    if (b < 0) return;
+    int nrows;
+    const int r0 = paged_rows(a.r, b, nrows);
+    const int nqv = nrows * G;
+    const int i = blockIdx.x % NBK * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4, v = v0 + i;
+    if (v >= nqv) return;
+    const int at0 = paged_len(a.r, b, r0, nrows) - nrows;
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, 0, KT);
+    if (sp.live == 1) return;
+    const int64_t at = ((int64_t)tile * a.c.Hkv + kvh) * d.nspan * QV + i;
+    const f4 o = join_parts(d.part + at * HD + c, d.part + d.ml + at * 2, sp.live, QV, HD);
+    const float y[4] = {o[0], o[1], o[2], o[3]};
+    put<T, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
 }
 
 template <typename T, int HD>
-hipError_t prompt(hipStream_t s, const PagedAttnArgs& a) {
-    constexpr int QV = sizeof(T) == 2 ? 256 : 128;
-    const int64_t G = a.H / a.c.Hkv;
-    const int64_t tiles = a.r.row_off ? a.r.total_rows * G / QV + a.r.nseq : a.r.nseq * ((a.r.max_rows * G + QV - 1) / QV);
-    if (tiles * a.c.Hkv > INT32_MAX) return hipErrorInvalidValue;
-    const PromptArgs d{a, (int)tiles};
-    if constexpr (sizeof(T) == 2) return launch(k_pprompt_bf16<HD>, dim3((unsigned)(tiles * a.c.Hkv)), dim3(256), s, d);
-    else return launch(k_pprompt_f32<HD>, dim3((unsigned)(tiles * a.c.Hkv)), dim3(256), s, d);
+constexpr int kPromptQv = sizeof(T) == 2 ? 32 * kPromptWaves : 128;
+template <typename T, int HD>
+constexpr int kPromptKt = sizeof(T) == 2 ? 16 * kPromptWaves * 128 / HD : 32;
+
+struct PromptPlan {
+    int64_t tiles;
+    int nspan;
+    int64_t ml;
+    size_t bytes;
+};
+
+// bytes: room for partials.
+PromptPlan prompt_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes) {
+    const int QV = bf16 ? kPromptQv<uint16_t, 128> : kPromptQv<float, 128>;
+    const int64_t G = H / c.Hkv, kt = bf16 ? 16 * kPromptWaves * 128 / c.hd : 32;
+    PromptPlan p{};
+    p.tiles = r.row_off ? std::min<int64_t>(r.total_rows * G / QV + r.nseq, r.nseq * ((r.max_rows * G + QV - 1) / QV))
+                        : r.nseq * ((r.max_rows * G + QV - 1) / QV);
+    // one workgroup to a CU (fp32: two), in spans of at least two tiles (fp32: eight)
+    const int64_t want = (bf16 ? 256 : 512) / std::max<int64_t>(1, p.tiles * c.Hkv), most = max_len / (kt * (bf16 ? 2 : 8));
+    p.nspan = (int)std::max<int64_t>(1, std::min(want, most));
+    const size_t per = (size_t)p.tiles * c.Hkv * QV * (c.hd + 2) * sizeof(float);
+    if (p.nspan > 1 && per * p.nspan > bytes) p.nspan = (int)std::max<size_t>(1, bytes / per);
+    if (p.nspan > 1) {
+        p.ml = p.tiles * c.Hkv * p.nspan * QV * c.hd;
+        p.bytes = per * p.nspan;
+    }
+    return p;
 }
 
-// Whether a call goes to k_pprompt: it takes the keys of a row in one piece, so it needs rows enough.
-bool many_rows(const PagedView& c, const PagedRows& r, int H, bool bf16) {
-    const int64_t G = H / c.Hkv, qv = std::min(r.max_rows, r.total_rows) * G;
-    return qv > 64 && r.total_rows * G * c.Hkv >= 64 * (bf16 ? 256 : 128);
+template <typename T, int HD>
+hipError_t prompt(hipStream_t s, const PagedAttnArgs& a, const PromptPlan& p, float* ws) {
+    const int64_t groups = p.tiles * a.c.Hkv, nj = kPromptQv<T, HD> * (HD / 4) / 256;
+    if (groups * std::max<int64_t>(p.nspan, nj) > INT32_MAX) return hipErrorInvalidValue;
+    const PromptArgs d{a, (int)p.tiles, p.nspan, ws, p.ml};
+    hipError_t err;
+    if constexpr (sizeof(T) == 2) err = launch(k_pprompt_bf16<HD>, dim3((unsigned)(groups * p.nspan)), dim3(64 * kPromptWaves), s, d);
+    else err = launch(k_pprompt_f32<HD>, dim3((unsigned)(groups * p.nspan)), dim3(256), s, d);
+    if (err != hipSuccess || p.nspan == 1) return err;
+    return launch(k_prompt_join<T, HD, kPromptQv<T, HD>, kPromptKt<T, HD>>, dim3((unsigned)(groups * nj)), dim3(256), s, d);
 }
 
-// Up to kDirect expected positions a sequence is one unit, which writes its rows itself.
-constexpr int kDirect = 256;
+// Whether a call goes to k_pprompt.
+bool many_rows(const PagedView& c, const PagedRows& r, int H) {
+    return (int64_t)std::min(r.max_rows, r.total_rows) * (H / c.Hkv) > 64;
+}
+
+// Up to kDirect workgroup steps of expected positions a sequence is one unit, which writes its rows itself:
+// 517 positions of 8 KV heads take 9.7 us that way, and 7.3 and 3.5 in two launches.
+constexpr int kDirect = 6;
 
 struct DecodePlan {
     int nt, ncg, target, units;
@@ -978,7 +1156,7 @@ DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16,
     p.ncg = (qv + 16 * p.nt - 1) / (16 * p.nt);
     const int64_t groups = (int64_t)c.Hkv * p.ncg;
     // two workgroups per CU, or as many units again as sequences
-    int64_t target = max_len <= kDirect ? 0 : std::max<int64_t>((512 + groups - 1) / groups, r.nseq);
+    int64_t target = max_len <= kDirect * kDecodeWaves * (bf16 ? 32 : 16) ? 0 : std::max<int64_t>((512 + groups - 1) / groups, r.nseq);
     const size_t per = (size_t)groups * 16 * p.nt * (c.hd + 2) * sizeof(float);
     if (target && per * (target + r.nseq + 8) > bytes) target = std::max<int64_t>(0, (int64_t)(bytes / per) - r.nseq - 8);
     p.target = (int)target;
@@ -1001,7 +1179,7 @@ hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p
 
 template <typename T, int HD>
 hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws, size_t bytes) {
-    if (many_rows(a.c, a.r, a.H, sizeof(T) == 2)) return prompt<T, HD>(s, a);
+    if (many_rows(a.c, a.r, a.H)) return prompt<T, HD>(s, a, prompt_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, bytes), ws);
     const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, bytes);
     return p.nt == 1 ? run_decode<T, HD, 1>(s, a, p, ws) : run_decode<T, HD, 2>(s, a, p, ws);
 }
@@ -1009,7 +1187,7 @@ hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float*
 }  // namespace
 
 size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
-    if (many_rows(c, r, H, bf16)) return 256;
+    if (many_rows(c, r, H)) return std::max<size_t>(prompt_plan(c, r, H, bf16, max_len, SIZE_MAX).bytes, 256);
     const DecodePlan p = decode_plan(c, r, H, bf16, max_len, SIZE_MAX);
     return std::max<size_t>(p.bytes, 256);
 }
