@@ -570,7 +570,7 @@ constexpr int kPromptWaves = 8;
 struct PromptArgs {
     PagedAttnArgs a;
     int tiles;    // workgroups of a KV head and span
-    int nspan;
+    int nspan, keys;  // spans at most, keys of one
     float* part;  // partials: [tile][KV head][span] of [QV][HD] sums, then of [QV] (maximum, sum)
     int64_t ml;   // floats of the first
 };
@@ -606,9 +606,8 @@ __device__ __forceinline__ int prompt_tile(const PagedRows& r, int G, int w, int
     auto from = [&](int j) {
         int n = max(mine - j, 0);
         for (int b0 = 64; b0 < r.nseq; b0 += 64) n += max(tiles_of(b0 + lane) - j, 0);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-        return uniform(n);
+        // (whole numbers that fp32 sums exactly in two halves)
+        return ((int)wave_sum_dpp((float)(n >> 12)) << 12) + (int)wave_sum_dpp((float)(n & 4095));
     };
     // the largest j with more than w of them
     if (from(0) <= w) return -1;
@@ -633,16 +632,16 @@ __device__ __forceinline__ int prompt_tile(const PagedRows& r, int G, int w, int
     return -1;
 }
 
-// The keys of a tile that workgroup (span `span`) reads: `end` of them in all, in multiples of kt.
+// The keys of a tile that workgroup `span` of it reads: of `end` in all, `keys` to each, the same number
+// for all tiles, so that the workgroups' work is alike; the last span takes what is left.
 struct Span {
     int from, upto, live;  // spans that have keys
 };
-__device__ __forceinline__ Span prompt_span(int end, int nspan, int span, int kt) {
+__device__ __forceinline__ Span prompt_span(int end, int nspan, int keys, int span) {
     Span s;
-    const int keys = max((int)(((int64_t)(end + nspan - 1) / nspan + kt - 1) / kt) * kt, kt);
-    s.live = max((int)(((int64_t)end + keys - 1) / keys), 1);
-    s.from = span * keys;
-    s.upto = min(end, s.from + keys);
+    s.live = min(max((int)(((int64_t)end + keys - 1) / keys), 1), nspan);
+    s.from = span < s.live ? span * keys : 0;
+    s.upto = span + 1 < s.live ? s.from + keys : end;
     return s;
 }
 
@@ -665,7 +664,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
     const int nqv = nrows * G;
     if (v0 >= nqv) return;
     const int len = paged_len(a.r, b, r0, nrows), at0 = len - nrows;
-    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, span, KT);
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, span);
     if (span >= sp.live) return;
     const int end = sp.upto;
     const int wv = v0 + 32 * wave;                       // the wave's first query vector
@@ -930,7 +929,7 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
     if (v0 >= nqv) return;
     const int len = paged_len(a.r, b, r0, nrows), at0 = len - nrows;
     const int wv = v0 + 32 * wave;
-    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, span, KT);
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, span);
     if (span >= sp.live) return;
     const int end = sp.upto;
     const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 31, nqv - 1) / G + 1) : 0;
@@ -1068,7 +1067,7 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
 }
 
 // The spans of k_pprompt's tiles joined: a thread per query vector and 4 columns.
-template <typename T, int HD, int QV, int KT>
+template <typename T, int HD, int QV>
 __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs d) {
     constexpr int PER = 256 / (HD / 4), NBK = QV / PER;
     const PagedAttnArgs& a = d.a;
@@ -1082,7 +1081,7 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs d) {
     const int i = blockIdx.x % NBK * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4, v = v0 + i;
     if (v >= nqv) return;
     const int at0 = paged_len(a.r, b, r0, nrows) - nrows;
-    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, 0, KT);
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, 0);
     if (sp.live == 1) return;
     const int64_t at = ((int64_t)tile * a.c.Hkv + kvh) * d.nspan * QV + i;
     const f4 o = join_parts(d.part + at * HD + c, d.part + d.ml + at * 2, sp.live, QV, HD);
@@ -1090,32 +1089,32 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs d) {
     put<T, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
 }
 
-template <typename T, int HD>
+template <typename T>
 constexpr int kPromptQv = sizeof(T) == 2 ? 32 * kPromptWaves : 128;
-template <typename T, int HD>
-constexpr int kPromptKt = sizeof(T) == 2 ? 16 * kPromptWaves * 128 / HD : 32;
 
 struct PromptPlan {
     int64_t tiles;
-    int nspan;
+    int nspan, keys;
     int64_t ml;
     size_t bytes;
 };
 
 // bytes: room for partials.
 PromptPlan prompt_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes) {
-    const int QV = bf16 ? kPromptQv<uint16_t, 128> : kPromptQv<float, 128>;
-    const int64_t G = H / c.Hkv, kt = bf16 ? 16 * kPromptWaves * 128 / c.hd : 32;
+    const int QV = bf16 ? kPromptQv<uint16_t> : kPromptQv<float>;
+    const int64_t G = H / c.Hkv, kt = bf16 ? 16 * kPromptWaves * 128 / c.hd : 32, most = (r.max_rows * G + QV - 1) / QV;
     PromptPlan p{};
-    p.tiles = r.row_off ? std::min<int64_t>(r.total_rows * G / QV + r.nseq, r.nseq * ((r.max_rows * G + QV - 1) / QV))
-                        : r.nseq * ((r.max_rows * G + QV - 1) / QV);
-    // one workgroup to a CU (fp32: two), in spans of at least two tiles (fp32: eight)
-    const int64_t want = (bf16 ? 256 : 512) / std::max<int64_t>(1, p.tiles * c.Hkv), most = max_len / (kt * (bf16 ? 2 : 8));
-    p.nspan = (int)std::max<int64_t>(1, std::min(want, most));
-    const size_t per = (size_t)p.tiles * c.Hkv * QV * (c.hd + 2) * sizeof(float);
-    if (p.nspan > 1 && per * p.nspan > bytes) p.nspan = (int)std::max<size_t>(1, bytes / per);
+    p.tiles = r.row_off ? std::min(r.total_rows * G / QV + r.nseq, r.nseq * most) : r.nseq * most;
+    // Workgroups for two on every CU (fp32, whose tiles are short: four), of at least two tiles (fp32: four)
+    const int64_t groups = std::max<int64_t>(1, p.tiles * c.Hkv), least = kt * (bf16 ? 2 : 4);
+    int64_t want = std::max<int64_t>(1, (bf16 ? 512 : 1024) / groups);
+    const size_t per = (size_t)groups * QV * (c.hd + 2) * sizeof(float);
+    if (want > 1) want = std::min<int64_t>(want, std::max<size_t>(1, bytes / per));
+    const int64_t keys = std::max(least, ((max_len + want - 1) / want + kt - 1) / kt * kt);
+    p.nspan = (int)((max_len + keys - 1) / keys);
+    p.keys = (int)std::min<int64_t>(keys, 1 << 30);
     if (p.nspan > 1) {
-        p.ml = p.tiles * c.Hkv * p.nspan * QV * c.hd;
+        p.ml = groups * p.nspan * QV * c.hd;
         p.bytes = per * p.nspan;
     }
     return p;
@@ -1123,14 +1122,14 @@ PromptPlan prompt_plan(const PagedView& c, const PagedRows& r, int H, bool bf16,
 
 template <typename T, int HD>
 hipError_t prompt(hipStream_t s, const PagedAttnArgs& a, const PromptPlan& p, float* ws) {
-    const int64_t groups = p.tiles * a.c.Hkv, nj = kPromptQv<T, HD> * (HD / 4) / 256;
+    const int64_t groups = p.tiles * a.c.Hkv, nj = kPromptQv<T> * (HD / 4) / 256;
     if (groups * std::max<int64_t>(p.nspan, nj) > INT32_MAX) return hipErrorInvalidValue;
-    const PromptArgs d{a, (int)p.tiles, p.nspan, ws, p.ml};
+    const PromptArgs d{a, (int)p.tiles, p.nspan, p.keys, ws, p.ml};
     hipError_t err;
     if constexpr (sizeof(T) == 2) err = launch(k_pprompt_bf16<HD>, dim3((unsigned)(groups * p.nspan)), dim3(64 * kPromptWaves), s, d);
     else err = launch(k_pprompt_f32<HD>, dim3((unsigned)(groups * p.nspan)), dim3(256), s, d);
     if (err != hipSuccess || p.nspan == 1) return err;
-    return launch(k_prompt_join<T, HD, kPromptQv<T, HD>, kPromptKt<T, HD>>, dim3((unsigned)(groups * nj)), dim3(256), s, d);
+    return launch(k_prompt_join<T, HD, kPromptQv<T>>, dim3((unsigned)(groups * nj)), dim3(256), s, d);
 }
 
 // Whether a call goes to k_pprompt.
