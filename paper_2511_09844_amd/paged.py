@@ -20,6 +20,9 @@ import torch
 from . import binding as B
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+# the current stream of a device, as HIP's handle (torch's own shortcut to it where there is one: a
+# microsecond less per call)
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def _need(ok, msg):
@@ -44,6 +47,7 @@ class PagedCache:
         self.k, self.v, self.table, self.refs = k, v, table, refs
         self.device, self.dtype = k.device, k.dtype
         self._index, self._sizes = k.device.index, {}
+        self._unused = torch.empty(256, dtype=torch.uint8, device=k.device)  # workspace of calls that need none
         self.n_pages, self.n_layers, self.n_kv_heads, self.page_size, self.head_dim = n_pages, n_layers, n_kv, page, hd
         self.max_seqs, self.max_pages = table.shape
         self.lib = B.load()
@@ -104,14 +108,11 @@ class PagedCache:
         _need(max_rows is None or max_rows >= 1, "max_rows: at least 1")
         return B.PagedRows(n, max(total, 1) if max_rows is None else max_rows, total, row_off.data_ptr(), lens.data_ptr())
 
-    def _seqs(self, what, **tensors):
-        n = None
-        for name, t in tensors.items():
-            if t is None:
-                continue
-            self._int32(t, 1, name, self.device)
-            _need(n in (None, t.numel()), f"{what}: tensors of one length")
-            n = t.numel()
+    def _seqs(self, what, *tensors):
+        n = tensors[0].numel() if isinstance(tensors[0], torch.Tensor) else 0
+        for t in tensors:
+            self._int32(t, 1, what, self.device)
+            _need(t.numel() == n, f"{what}: tensors of one length")
         _need(n <= self.max_seqs, f"{what}: {n} sequences, the table has {self.max_seqs}")
         return n
 
@@ -121,10 +122,10 @@ class PagedCache:
     def _call(self, fn, *args):
         """A C call on the current stream of the cache's device, which is the current one meanwhile."""
         if torch.cuda.current_device() == self._index:
-            rc = fn(*args, torch.cuda.current_stream(self._index).cuda_stream)
+            rc = fn(*args, _stream_of(self._index))
         else:
             with torch.cuda.device(self._index):
-                rc = fn(*args, torch.cuda.current_stream(self._index).cuda_stream)
+                rc = fn(*args, _stream_of(self._index))
         if rc:
             B.check(rc, None, fn.__name__)
 
@@ -167,7 +168,8 @@ class PagedCache:
             if len(self._sizes) > 1000:
                 self._sizes.clear()
             self._sizes[key] = nbytes
-        ws = self._workspace(nbytes)
+        # (the smallest size is that of calls without partial sums)
+        ws = self._unused if nbytes == 256 else self._workspace(nbytes)
         self._call(self.lib.sd2_paged_attn, kv, ctypes.byref(rows), q.data_ptr(), qs, out.data_ptr(), os, heads,
                    self._scale if scale is None else scale, max_len, ws.data_ptr(), nbytes)
         return out
@@ -176,8 +178,8 @@ class PagedCache:
     def reserve(self, first, last, keep=None):
         """Make positions first[b] .. last[b] - 1 writable (sd2_pages_reserve); returns granted, int32
         per sequence: last[b], or where the first page begins that could not be had."""
-        n = self._seqs("reserve", first=first, last=last, keep=keep)
-        granted = torch.empty(n, dtype=torch.int32, device=self.device)
+        n = self._seqs("first, last, keep", first, last, *(() if keep is None else (keep,)))
+        granted = torch.empty_like(last)
         ws = self._workspace(self._pages_ws)
         self._call(self.lib.sd2_pages_reserve, ctypes.byref(self._pages), n, first.data_ptr(), last.data_ptr(),
                    None if keep is None else keep.data_ptr(), granted.data_ptr(), ws.data_ptr(), self._pages_ws)
@@ -195,7 +197,7 @@ class PagedCache:
     def trim(self, lens):
         """Sequences 0 .. len(lens) - 1 keep the pages of their first lens[b] positions (sd2_pages_trim;
         a negative length: all)."""
-        n = self._seqs("trim", lens=lens)
+        n = self._seqs("lens", lens)
         self._call(self.lib.sd2_pages_trim, ctypes.byref(self._pages), n, lens.data_ptr())
 
     def compact(self):
