@@ -80,6 +80,21 @@ __device__ __forceinline__ int paged_rows(const PagedRows& r, int b, int& n) {
 __device__ __forceinline__ int paged_len(const PagedRows& r, int b, int r0, int n) {
     return max(r.lens ? r.lens[b] : n > 0 ? r.row_pos[r0 + n - 1] + 1 : 0, 0);
 }
+// Both, loaded at once.
+struct SeqRows {
+    int r0, n, len;
+};
+__device__ __forceinline__ SeqRows seq_rows(const PagedRows& r, int b) {
+    SeqRows s;
+    const int len = r.lens ? r.lens[b] : 0;
+    s.r0 = paged_rows(r, b, s.n);
+    s.len = r.lens ? max(len, 0) : paged_len(r, b, s.r0, s.n);
+    return s;
+}
+// Those that lane l holds, for all lanes.
+__device__ __forceinline__ SeqRows lane_rows(const SeqRows& s, int l) {
+    return SeqRows{__builtin_amdgcn_readlane(s.r0, l), __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.len, l)};
+}
 // The sequence that row `row` belongs to, or -1 (rows behind the last one's).
 __device__ __forceinline__ int paged_seq(const PagedRows& r, int row) {
     if (!r.row_off) return row / r.max_rows;

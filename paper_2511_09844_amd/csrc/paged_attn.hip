@@ -108,14 +108,13 @@ struct DecodeArgs {
 // when it is recorded.  Sequence b has the units from first[b] on.  keys is at least the total over
 // target, so that there are at most target + nseq units.
 struct Units {
-    int keys, b, first, count, end;  // of sequence b: its units, and its positions (those there are pages for)
+    int keys, b, first, count;  // of sequence b: its units
+    SeqRows rows;
 };
 
-// Positions of sequence b, 0 without rows.
-__device__ __forceinline__ int seq_end(const PagedAttnArgs& a, int b) {
-    int n;
-    const int r0 = paged_rows(a.r, b, n);
-    return n > 0 ? (int)min((int64_t)paged_len(a.r, b, r0, n), (int64_t)a.c.max_pages << a.c.shift) : 0;
+// Positions of a sequence that pages may hold, 0 without rows.
+__device__ __forceinline__ int seq_end(const PagedAttnArgs& a, const SeqRows& s) {
+    return s.n > 0 ? (int)min((int64_t)s.len, (int64_t)a.c.max_pages << a.c.shift) : 0;
 }
 
 // The sequence that unit `unit` belongs to (b = -1: none), or sequence `b` itself when unit is negative.
@@ -128,14 +127,14 @@ __device__ __forceinline__ Units units_of(const DecodeArgs& d, int unit, int b) 
         u.b = unit < 0 ? b : unit < a.r.nseq ? unit : -1;
         u.first = u.b;
         u.count = 1;
-        u.end = u.b >= 0 ? seq_end(a, u.b) : 0;
+        u.rows = u.b >= 0 ? seq_rows(a.r, u.b) : SeqRows{};
         u.keys = INT32_MAX;
         return u;
     }
     const int lane = threadIdx.x & 63, nseq = a.r.nseq;
-    int mine = lane < nseq ? seq_end(a, lane) : 0;
-    float total = (float)mine;
-    for (int b0 = 64; b0 < nseq; b0 += 64) total += b0 + lane < nseq ? (float)seq_end(a, b0 + lane) : 0.f;
+    SeqRows mine = lane < nseq ? seq_rows(a.r, lane) : SeqRows{};
+    float total = (float)seq_end(a, mine);
+    for (int b0 = 64; b0 < nseq; b0 += 64) total += b0 + lane < nseq ? (float)seq_end(a, seq_rows(a.r, b0 + lane)) : 0.f;
     total = wave_sum_dpp(total);
     // (rounded up past what the sum may have lost)
     const float want = fmaxf(total / (float)d.target * 1.00001f, (float)d.min_keys);
@@ -143,8 +142,8 @@ __device__ __forceinline__ Units units_of(const DecodeArgs& d, int unit, int b) 
     u.b = -1;
     int at = 0;
     for (int b0 = 0; b0 < nseq; b0 += 64) {
-        if (b0) mine = b0 + lane < nseq ? seq_end(a, b0 + lane) : 0;
-        const int cnt = b0 + lane < nseq ? max((int)(((int64_t)mine + u.keys - 1) / u.keys), 1) : 0;
+        if (b0) mine = b0 + lane < nseq ? seq_rows(a.r, b0 + lane) : SeqRows{};
+        const int cnt = b0 + lane < nseq ? max((seq_end(a, mine) + (u.keys - 1)) / u.keys, 1) : 0;
         int inc = cnt;
 #pragma unroll
         for (int o = 1; o < 64; o *= 2) {
@@ -157,7 +156,7 @@ __device__ __forceinline__ Units units_of(const DecodeArgs& d, int unit, int b) 
             u.b = b0 + l;
             u.first = at + __builtin_amdgcn_readlane(inc - cnt, l);
             u.count = __builtin_amdgcn_readlane(cnt, l);
-            u.end = __builtin_amdgcn_readlane(mine, l);
+            u.rows = lane_rows(mine, l);
             break;
         }
         at += __builtin_amdgcn_readlane(inc, 63);
@@ -339,14 +338,12 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     const int b = un.b;
     if (b < 0) return;
     const int G = a.H / a.c.Hkv;
-    int nrows;
-    const int r0 = paged_rows(a.r, b, nrows);
+    const int r0 = uniform(un.rows.r0), nrows = uniform(un.rows.n), len = uniform(un.rows.len);
     const int nqv = nrows * G, v0 = cg * QV;
     if (v0 >= nqv) return;
-    const int len = paged_len(a.r, b, r0, nrows);
     // the unit's positions that some row of this group reads
     const int kb = (unit - un.first) * un.keys;
-    const int ke = min(min(len - nrows + min(v0 + QV - 1, nqv - 1) / G + 1, un.end), un.count > 1 ? kb + un.keys : INT32_MAX);
+    const int ke = min(min(len - nrows + min(v0 + QV - 1, nqv - 1) / G + 1, seq_end(a, un.rows)), un.count > 1 ? kb + un.keys : INT32_MAX);
     const bool whole_seq = un.count == 1;
     const int64_t slot = ((int64_t)unit * a.c.Hkv + kvh) * d.ncg + cg;
     u4 q[NT][B::NK];
@@ -532,9 +529,7 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
     const Units un = units_of<T>(d, -1, b);
     const int live = un.count;
     if (live == 1) return;
-    int nrows;
-    const int r0 = paged_rows(a.r, b, nrows);
-    const int nqv = nrows * G, v0 = cg * QV, v = v0 + i;
+    const int r0 = un.rows.r0, nqv = un.rows.n * G, v0 = cg * QV, v = v0 + i;
     if (i >= QV || v >= nqv) return;
     // from one unit's partials to the next
     const int64_t slot = ((int64_t)un.first * a.c.Hkv + kvh) * d.ncg + cg, next = (int64_t)a.c.Hkv * d.ncg * QV;
@@ -588,48 +583,60 @@ __device__ __forceinline__ float half_sum(float v) {
 // Workgroup w of a KV head: its sequence (-1: none) and first query vector there.  A sequence's tiles of QV
 // query vectors are numbered from its first row on, and the last tiles of all sequences go first, since
 // they read the most keys.
+struct Tile {
+    int b, v0;
+    SeqRows rows;
+};
 template <int QV>
-__device__ __forceinline__ int prompt_tile(const PagedRows& r, int G, int w, int& v0) {
+__device__ __forceinline__ Tile prompt_tile(const PagedRows& r, int G, int w) {
     const int most = ((int64_t)r.max_rows * G + QV - 1) / QV;  // of a sequence
+    Tile t;
+    t.b = -1;
+    t.v0 = 0;
     if (!r.row_off) {
-        v0 = w < most * r.nseq ? (most - 1 - w / r.nseq) * QV : 0;
-        return w < most * r.nseq ? w % r.nseq : -1;
+        if (w >= most * r.nseq) return t;
+        t.b = w % r.nseq;
+        t.v0 = (most - 1 - w / r.nseq) * QV;
+        t.rows = seq_rows(r, t.b);
+        return t;
     }
     const int lane = threadIdx.x & 63;
-    auto tiles_of = [&](int b) {
-        int n = 0;
-        if (b < r.nseq) paged_rows(r, b, n);
-        return (int)(((int64_t)n * G + QV - 1) / QV);
-    };
-    const int mine = tiles_of(lane);
+    SeqRows mine = lane < r.nseq ? seq_rows(r, lane) : SeqRows{};
+    auto tiles_of = [&](const SeqRows& s) { return (int)(((int64_t)s.n * G + QV - 1) / QV); };
+    auto others = [&](int b) { return tiles_of(b < r.nseq ? seq_rows(r, b) : SeqRows{}); };
+    const int tiles = tiles_of(mine);
     // tiles numbered j or more
     auto from = [&](int j) {
-        int n = max(mine - j, 0);
-        for (int b0 = 64; b0 < r.nseq; b0 += 64) n += max(tiles_of(b0 + lane) - j, 0);
+        int n = max(tiles - j, 0);
+        for (int b0 = 64; b0 < r.nseq; b0 += 64) n += max(others(b0 + lane) - j, 0);
         // (whole numbers that fp32 sums exactly in two halves)
         return ((int)wave_sum_dpp((float)(n >> 12)) << 12) + (int)wave_sum_dpp((float)(n & 4095));
     };
     // the largest j with more than w of them
-    if (from(0) <= w) return -1;
+    if (from(0) <= w) return t;
     int lo = 0, hi = most;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (from(mid) > w) lo = mid;
         else hi = mid;
     }
-    v0 = lo * QV;
+    t.v0 = lo * QV;
     int rank = w - from(lo + 1);  // among the sequences that have a tile lo
     for (int b0 = 0; b0 < r.nseq; b0 += 64) {
-        const bool has = (b0 ? tiles_of(b0 + lane) : mine) > lo;
+        if (b0) mine = b0 + lane < r.nseq ? seq_rows(r, b0 + lane) : SeqRows{};
+        const bool has = tiles_of(mine) > lo;
         const uint64_t m = __ballot(has);
         const int c = __popcll(m);
         if (rank < c) {
-            const bool me = has && __popcll(m & (((uint64_t)1 << lane) - 1)) == rank;
-            return uniform(b0 + (int)__builtin_ctzll(__ballot(me)));
+            const uint64_t me = __ballot(has && __popcll(m & (((uint64_t)1 << lane) - 1)) == rank);
+            const int l = __builtin_ctzll(me);
+            t.b = b0 + l;
+            t.rows = lane_rows(mine, l);
+            break;
         }
         rank -= c;
     }
-    return -1;
+    return t;
 }
 
 // The keys of a tile that workgroup `span` of it reads: of `end` in all, `keys` to each, the same number
@@ -656,14 +663,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
     const int G = a.H / a.c.Hkv;
     // (KV heads lie on XCDs in turn)
     const int kvh = blockIdx.x % a.c.Hkv, span = blockIdx.x / a.c.Hkv % d.nspan, tile = blockIdx.x / a.c.Hkv / d.nspan;
-    int v0 = 0;
-    const int b = prompt_tile<QV>(a.r, G, tile, v0);
+    const Tile tl = prompt_tile<QV>(a.r, G, tile);
+    const int b = uniform(tl.b), v0 = uniform(tl.v0), r0 = uniform(tl.rows.r0), nrows = uniform(tl.rows.n);
     if (b < 0) return;
-    int nrows;
-    const int r0 = paged_rows(a.r, b, nrows);
     const int nqv = nrows * G;
     if (v0 >= nqv) return;
-    const int len = paged_len(a.r, b, r0, nrows), at0 = len - nrows;
+    const int at0 = uniform(tl.rows.len) - nrows;
     const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, span);
     if (span >= sp.live) return;
     const int end = sp.upto;
@@ -758,7 +763,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
             const int key = 8 * (r / 4) + 4 * g + r % 4;
             s[r] = k0 + key <= pos && (hv >> (r / 8) & 1) ? s[r] : -INFINITY;
         }
-        const float mn = fmaxf(m, most(s)), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        const float mx = most(s);
+        if (!__any(mx > m + kLazy)) return;
+        const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
         m = mn;
         l *= f;
 #pragma unroll
@@ -920,14 +927,12 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
     const int n = lane & 31, g = lane >> 5;
     const int G = a.H / a.c.Hkv;
     const int kvh = blockIdx.x % a.c.Hkv, span = blockIdx.x / a.c.Hkv % d.nspan, tile = blockIdx.x / a.c.Hkv / d.nspan;
-    int v0 = 0;
-    const int b = prompt_tile<QV>(a.r, G, tile, v0);
+    const Tile tl = prompt_tile<QV>(a.r, G, tile);
+    const int b = uniform(tl.b), v0 = uniform(tl.v0), r0 = uniform(tl.rows.r0), nrows = uniform(tl.rows.n);
     if (b < 0) return;
-    int nrows;
-    const int r0 = paged_rows(a.r, b, nrows);
     const int nqv = nrows * G;
     if (v0 >= nqv) return;
-    const int len = paged_len(a.r, b, r0, nrows), at0 = len - nrows;
+    const int at0 = uniform(tl.rows.len) - nrows;
     const int wv = v0 + 32 * wave;
     const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, span);
     if (span >= sp.live) return;
@@ -1072,15 +1077,12 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs d) {
     constexpr int PER = 256 / (HD / 4), NBK = QV / PER;
     const PagedAttnArgs& a = d.a;
     const int kvh = blockIdx.x / NBK % a.c.Hkv, tile = blockIdx.x / NBK / a.c.Hkv, G = a.H / a.c.Hkv;
-    int v0 = 0;
-    const int b = prompt_tile<QV>(a.r, G, tile, v0);
-    if (b < 0) return;
-    int nrows;
-    const int r0 = paged_rows(a.r, b, nrows);
-    const int nqv = nrows * G;
+    const Tile tl = prompt_tile<QV>(a.r, G, tile);
+    if (tl.b < 0) return;
+    const int v0 = tl.v0, r0 = tl.rows.r0, nqv = tl.rows.n * G;
     const int i = blockIdx.x % NBK * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4, v = v0 + i;
     if (v >= nqv) return;
-    const int at0 = paged_len(a.r, b, r0, nrows) - nrows;
+    const int at0 = tl.rows.len - tl.rows.n;
     const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, 0);
     if (sp.live == 1) return;
     const int64_t at = ((int64_t)tile * a.c.Hkv + kvh) * d.nspan * QV + i;
