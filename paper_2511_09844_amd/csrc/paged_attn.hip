@@ -674,22 +674,6 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
     const int end = sp.upto;
     const int wv = v0 + 32 * wave;                       // the wave's first query vector
     const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 31, nqv - 1) / G + 1) : 0;
-    u4 q[NS];
-    // (a negative scale turns into the sign of q)
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-    const float c = fabsf(a.scale) * kLog2e;
-    const int v = wv + n, vc = min(v, nqv - 1), pos = at0 + vc / G;
-    {
-        const uint16_t* p = (const uint16_t*)a.q + (r0 + vc / G) * a.q_stride + (kvh * G + vc % G) * HD + 8 * g;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) q[s] = *(const u4*)(p + 16 * s) ^ flip;
-    }
-    f16v o[NC];
-    float m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < NC; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
     // table entries of the KT / 16 groups of keys of a tile, a lane each, and the pages they name (apart: the
     // first test of an entry waits for it, and for all loads before)
     auto look = [&](int k0) {
@@ -699,6 +683,22 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
         return e;
     };
     auto named = [&](int e) { return (uint32_t)e < (uint32_t)a.c.n_pages ? e : -1; };
+    const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
+    int entry = look(t0 * KT), entry1 = look((t0 + 1) * KT);
+    u4 q[NS];
+    const float c = fabsf(a.scale) * kLog2e;
+    const int v = wv + n, vc = min(v, nqv - 1), pos = at0 + vc / G;
+    {
+        const uint16_t* p = (const uint16_t*)a.q + (r0 + vc / G) * a.q_stride + (kvh * G + vc % G) * HD + 8 * g;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) q[s] = *(const u4*)(p + 16 * s);
+    }
+    f16v o[NC];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
     const int mask = (1 << a.c.shift) - 1;
     // This wave's groups of 16 keys of a tile, straight into LDS, 1 KB an instruction: 16-byte unit u of a
     // row at u ^ (row % 8) (K) and u ^ 2 (row % 4) (V).  Rows that do not exist arrive as zeros.
@@ -726,7 +726,6 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
             }
         }
     };
-    const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
     const int nk = (wend + 31) / 32;  // blocks of 32 keys up to the last that this wave computes
     // K: row n of a block, units 2 i + g
     int ka[NS], va[NC];
@@ -823,11 +822,15 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
     };
     const bool late = wave >= NW / 2;
     const int nkw = (end + 31) / 32;  // of the workgroup
-    int pg = named(look(t0 * KT));
+    int pg = named(entry);
     uint64_t have = __ballot(pg >= 0), next = 0;
     load(t0 * KT, pg, t0 & 1);
-    int entry = look((t0 + 1) * KT);
+    entry = entry1;
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    // (a negative scale turns into the sign of q)
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) q[i] ^= flip;
     __syncthreads();
     f16v s;
     u4 x[2][NC];
@@ -894,8 +897,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
     }
     if (!late) meet();
     const float sum = half_sum(l);
-    if (v >= nqv) return;
     if (sp.live > 1) {
+        if (v >= nqv) return;
         const int64_t slot = ((int64_t)tile * a.c.Hkv + kvh) * d.nspan + span;
         float* po = d.part + (slot * QV + wv - v0 + n) * HD + 4 * g;
 #pragma unroll
@@ -905,14 +908,25 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
         if (g == 0) *(f2*)(d.part + d.ml + (slot * QV + wv - v0 + n) * 2) = f2{m, sum};
         return;
     }
+    // the wave's rows through LDS (its own part of what K and V were in, which nobody uses any more), so that
+    // whole rows are stored: 8 bytes a lane to 64 rows took 2 to 4 us
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    constexpr int OB = RB + 16;
+    char* const os = (late ? vs[0] : ks[0]) + wave % (NW / 2) * 32 * OB;
+    static_assert(NW / 2 * 32 * OB <= 2 * KT * RB, "the waves' rows fit");
 #pragma unroll
     for (int i = 0; i < NC; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const float y[4] = {o[i][r] * inv, o[i][r + 1] * inv, o[i][r + 2] * inv, o[i][r + 3] * inv};
-            put<uint16_t, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + 32 * i + 2 * r + 4 * g, y);
-        }
+        for (int r = 0; r < 16; r += 4)
+            *(u2*)(os + n * OB + (32 * i + 2 * r + 4 * g) * 2) = u2{pack_bf16(o[i][r] * inv, o[i][r + 1] * inv), pack_bf16(o[i][r + 2] * inv, o[i][r + 3] * inv)};
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 32 * CH / 64; ++i) {
+        const int row = i * (64 / CH) + lane / CH, w = wv + row;
+        if (w < nqv)
+            *(u4*)((uint16_t*)a.out + (r0 + w / G) * a.out_stride + (kvh * G + w % G) * HD + lane % CH * 8) = *(const u4*)(os + row * OB + lane % CH * 16);
+    }
 }
 
 // The same on fp32 matrix instructions, 32 query vectors per wave and tiles of 32 keys, row by row in LDS
