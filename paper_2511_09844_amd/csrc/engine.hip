@@ -804,8 +804,10 @@ sd2_status sd2_prefill(sd2_handle_t h, int32_t batch, const int32_t* tokens, con
     // several prompts: the rows a chunk has of each are packed, and the launches cover only those
     // (always in pages, whose attention goes by a sequence's last row)
     e->live_off = batch > 1 || e->paged ? e->ws.row_off : nullptr;
-    if (e->paged && (err = launch_prefill_pages(s, *e, batch, lens, max_prompt)) != hipSuccess)
+    if (e->paged && (err = launch_prefill_pages(s, *e, batch, lens, max_prompt)) != hipSuccess) {
+        e->live_off = nullptr;
         return hip_fail(e, err, "prefill pages");
+    }
     for (int c = 0; c < nchunks; ++c) {
         launch_plan_embed(s, *e, e->mv, kPlanPrefill, c, rows, tokens, lens, max_prompt, chunk);
         for (int l = 0; l < e->mv.dm.n_layers; ++l) {

@@ -561,6 +561,8 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
 typedef float f16v __attribute__((ext_vector_type(16)));
 constexpr int kLazy = 8;
 constexpr int kPromptWaves = 8;
+// Keys of a tile in LDS (bf16): 32 KB of K and of V, or 256 of head dim 32.
+constexpr int prompt_keys(int hd) { return hd == 128 ? 128 : 256; }
 
 struct PromptArgs {
     PagedAttnArgs a;
@@ -654,7 +656,7 @@ __device__ __forceinline__ Span prompt_span(int end, int nspan, int keys, int sp
 
 template <int HD>
 __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArgs d) {
-    constexpr int NW = kPromptWaves, KT = 16 * NW * 128 / HD, NB = KT / 32, NS = HD / 16, NC = HD / 32, CH = HD / 8;
+    constexpr int NW = kPromptWaves, KT = prompt_keys(HD), NB = KT / 32, NS = HD / 16, NC = HD / 32, CH = HD / 8;
     constexpr int QV = 32 * NW, RB = HD * 2;
     __shared__ __attribute__((aligned(1024))) char ks[2][KT * RB], vs[2][KT * RB];
     const PagedAttnArgs& a = d.a;
@@ -1118,7 +1120,7 @@ struct PromptPlan {
 // bytes: room for partials.
 PromptPlan prompt_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes) {
     const int QV = bf16 ? kPromptQv<uint16_t> : kPromptQv<float>;
-    const int64_t G = H / c.Hkv, kt = bf16 ? 16 * kPromptWaves * 128 / c.hd : 32, most = (r.max_rows * G + QV - 1) / QV;
+    const int64_t G = H / c.Hkv, kt = bf16 ? prompt_keys(c.hd) : 32, most = (r.max_rows * G + QV - 1) / QV;
     PromptPlan p{};
     p.tiles = r.row_off ? std::min(r.total_rows * G / QV + r.nseq, r.nseq * most) : r.nseq * most;
     // Workgroups for two on every CU (fp32, whose tiles are short: four), of at least two tiles (fp32: four)

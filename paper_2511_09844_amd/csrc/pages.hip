@@ -432,7 +432,8 @@ bool rows_of(const sd2_paged_rows* rows, PagedRows* r) {
         return false;
     if (rows->nseq && !aligned(rows->lens, 4)) return false;
     if (rows->row_off ? !aligned(rows->row_off, 4) : (int64_t)rows->nseq * rows->max_rows != rows->total_rows) return false;
-    *r = PagedRows{rows->nseq, rows->max_rows, rows->total_rows, rows->row_off, rows->lens, nullptr};
+    const int32_t most = rows->row_off ? std::min(rows->max_rows, std::max(rows->total_rows, 1)) : rows->max_rows;
+    *r = PagedRows{rows->nseq, most, rows->total_rows, rows->row_off, rows->lens, nullptr};
     return true;
 }
 

@@ -126,6 +126,73 @@ def test_offsets_out_of_range_stay_inside():
     assert (out[:4] == 3.0).all() and (out[6:9] == 3.0).all() and (out[11] == 3.0).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_more_sequences_than_lanes(dtype):
+    """150 sequences: those of a wave's lanes, and two more rounds of them."""
+    lens = [(37 * b) % 90 for b in range(150)]
+    cache = make_cache(lens, dtype, 2, 64, 16)
+    check(cache, queries(150, 4, 64, dtype), lens, [1] * 150, False)
+    check(cache, queries(150, 4, 64, dtype), lens, [1] * 150, False, max_len=90)
+    check(cache, queries(sum(lens), 4, 64, dtype), lens, lens, True)
+    rows = [min(n, b % 50) for b, n in enumerate(lens)]
+    check(cache, queries(sum(rows), 4, 64, dtype), lens, rows, True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 20, 130])
+@pytest.mark.parametrize("max_len", [1, 700, 4000])
+def test_the_expected_length_decides_nothing_but_the_split(dtype, rows, max_len):
+    lens = [3000, 170, 999]
+    cache = make_cache(lens, dtype, 2, 128, 64, extra_entries=40)
+    check(cache, queries(3 * rows, 6, 128, dtype), lens, [rows] * 3, False, max_len=max_len)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 9, 100])
+def test_lengths_beyond_the_table(dtype, rows):
+    lens = [700, 64 * 5 + 1, 300]
+    cache = make_cache([320, 320, 300], dtype, 2, 64, 64, extra_entries=0)  # five entries
+    check(cache, queries(3 * rows, 4, 64, dtype), lens, [rows] * 3, False)
+    before = [cache.k.clone(), cache.v.clone()]
+    ln, _ = rows_of([700, 640, 5000], [1] * 3, False)
+    cache.append(queries(3, 2, 64, dtype), queries(3, 2, 64, dtype), ln)
+    assert torch.equal(before[0].nan_to_num(), cache.k.nan_to_num()) and torch.equal(before[1].nan_to_num(), cache.v.nan_to_num())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 600])
+@pytest.mark.parametrize("rising", [True, False], ids=["rising", "falling"])
+def test_scores_that_rise_along_the_keys(dtype, rows, rising):
+    """Every few blocks a new maximum, far above the last one, or all but the first block negligible."""
+    lens = [1100]
+    cache = make_cache(lens, dtype, 1, 64, 16)
+    n = lens[0]
+    ramp = torch.linspace(0.05, 12.0, n, device="cuda")
+    ramp = ramp if rising else ramp.flip(0)
+    for j in range(n):
+        p, s = int(cache.table[0, j // 16]), j % 16
+        cache.k[p, 0, 0, s] = ramp[j].to(dtype)
+    q = queries(rows, 2, 64, dtype).abs()
+    check(cache, q, lens, [rows], True)
+
+
+def test_non_finite_values_reach_the_rows_that_read_them():
+    lens = [200, 90]
+    for dtype in (F32, BF16):
+        for rows in (1, 80):
+            cache = make_cache(lens, dtype, 1, 64, 16)
+            for at, what in ((5, float("nan")), (6, float("inf"))):
+                p, s = int(cache.table[0, at // 16]), at % 16
+                cache.v[p, 0, 0, s] = what
+                cache.k[int(cache.table[0, 0]), 0, 0, 7] = 0.0
+            ln, _ = rows_of(lens, [rows] * 2, False)
+            q = queries(2 * rows, 2, 64, dtype)
+            got = cache.attend(q, ln)
+            assert torch.isnan(got[:rows]).all(), "positions 119 .. 199 read it"
+            ref, absv, spread = attend64(cache, q, lens, [rows] * 2)
+            bound = attend_bound(ref, absv, spread, dtype, 200, 64)
+            assert ((got.double() - ref).abs()[rows:] <= bound[rows:]).all(), "the other sequence does not"
+
 @pytest.mark.parametrize("rows", [1, 20, 200])
 def test_far_pages_of_a_large_pool(rows):
     # element offsets beyond 2^32
