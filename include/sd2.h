@@ -390,8 +390,8 @@ sd2_status sd2_paged_append(const sd2_paged_kv* kv, const sd2_paged_rows* rows, 
  * (whole 16-byte units); n_heads a multiple of n_kv_heads, up to 1024.  bf16: scores, softmax and
  * sums in fp32, the softmax's weights rounded to bf16 for their product with v; fp32: fp32 throughout.
  * Memory behind a sequence's last position, and pages it does not name, are not read, or do not count,
- * whatever they hold.  A non-finite value of v may reach the rows of its sequence in this call that
- * lie before it as well as those behind.
+ * whatever they hold; infinities and NaN of a position reach the rows that read it, and no others.
+ * The rows of a sequence times n_heads / n_kv_heads are at most 2^30.
  * max_len: the largest length expected, 1..max_pages * page_size (it decides how the work is split; a longer
  * sequence is computed all the same).
  */

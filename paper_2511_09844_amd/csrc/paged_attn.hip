@@ -219,6 +219,28 @@ struct Acc {
     float m[NT], l[NT];
 };
 
+// Infinities and NaN of v.  A row that does not read a key multiplies the key's values by a weight of 0, which
+// would make NaN of them.  So where rows of a block differ in what they read, such values are looked for; a
+// block with any is multiplied once per position that rows end at, with the values behind it as 0, and only the
+// rows that end there take the product.
+template <typename T>
+__device__ __forceinline__ uint32_t odd_bits(uint32_t x) {  // the sign bit of such a value set
+    return sizeof(T) == 2 ? (x & 0x7f807f80) + 0x00800080 : (x & 0x7f800000) + 0x00800000;
+}
+template <typename T>
+__device__ __forceinline__ bool any_odd(uint32_t bits) {
+    return __any((bits & (sizeof(T) == 2 ? 0x80008000 : 0x80000000)) != 0);
+}
+// A value that the compiler does not know, so that what follows from it is not kept in registers over a loop.
+__device__ __forceinline__ int unknown(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+// Of two bf16 values of neighbouring keys those up to position `upto`.
+__device__ __forceinline__ uint32_t cut_mask(int key, int upto) {
+    return (key <= upto ? 0xffffu : 0u) | (key < upto ? 0xffff0000u : 0u);
+}
+
 // Scores of a block, in units of log2, those that a row does not read at -inf.
 template <typename T, int HD, int NT>
 __device__ __forceinline__ void block_scores(const Block<T, HD>& x, const u4 (&q)[NT][Block<T, HD>::NK],
@@ -257,9 +279,9 @@ __device__ __forceinline__ void block_scores(const Block<T, HD>& x, const u4 (&q
         }
 }
 
-// The block's part of the softmax and of its product with V.
+// The block's part of the softmax: its scores become weights.
 template <typename T, int HD, int NT>
-__device__ __forceinline__ void block_sums(const Block<T, HD>& x, f4 (&sc)[NT][Block<T, HD>::TK], Acc<T, HD, NT>& acc) {
+__device__ __forceinline__ void block_weights(Acc<T, HD, NT>& acc, f4 (&sc)[NT][Block<T, HD>::TK]) {
     using B = Block<T, HD>;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -287,20 +309,35 @@ __device__ __forceinline__ void block_sums(const Block<T, HD>& x, f4 (&sc)[NT][B
             }
         acc.l[j] += sum;
     }
+}
+
+// The weights as bf16, the type of the matrix instruction that v enters as it is: half a step of
+// 2^-8 each, as much as the output's own rounding.
+__device__ __forceinline__ b8 weights_b8(const f4 (&s)[2]) {
+    return __builtin_bit_cast(b8, u4{pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]), pack_bf16(s[1][0], s[1][1]),
+                                     pack_bf16(s[1][2], s[1][3])});
+}
+// Columns 16 i .. 16 i + 15 of a bf16 block's V as an operand.
+template <int HD>
+__device__ __forceinline__ u4 values_b8(const Block<uint16_t, HD>& x, int i, int zero = 0) {
+    u4 w;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+        w[d] = __builtin_amdgcn_perm(x.v[2 * d + 1][0][i / 2], x.v[2 * d][0][i / 2], (i % 2 ? 0x07060302 : 0x05040100) + zero);
+    return w;
+}
+
+// The block's product with V.
+template <typename T, int HD, int NT>
+__device__ __forceinline__ void block_sums(const Block<T, HD>& x, const f4 (&sc)[NT][Block<T, HD>::TK], Acc<T, HD, NT>& acc) {
+    using B = Block<T, HD>;
     if constexpr (B::H) {
-        // the weights as bf16, the type of the matrix instruction that v enters as it is: half a step of
-        // 2^-8 each, as much as the output's own rounding
         b8 p[NT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-            p[j] = __builtin_bit_cast(b8, u4{pack_bf16(sc[j][0][0], sc[j][0][1]), pack_bf16(sc[j][0][2], sc[j][0][3]),
-                                             pack_bf16(sc[j][1][0], sc[j][1][1]), pack_bf16(sc[j][1][2], sc[j][1][3])});
+        for (int j = 0; j < NT; ++j) p[j] = weights_b8(sc[j]);
 #pragma unroll
         for (int i = 0; i < HD / 16; ++i) {
-            u4 w;
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-                w[d] = __builtin_amdgcn_perm(x.v[2 * d + 1][0][i / 2], x.v[2 * d][0][i / 2], i % 2 ? 0x07060302 : 0x05040100);
+            const u4 w = values_b8<HD>(x, i);
 #pragma unroll
             for (int j = 0; j < NT; ++j)
                 acc.o[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, w), p[j], acc.o[j][i], 0, 0, 0);
@@ -317,6 +354,53 @@ __device__ __forceinline__ void block_sums(const Block<T, HD>& x, f4 (&sc)[NT][B
                         acc.o[j][u * B::VW + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[r][u][e]), sc[j][0][r],
                                                                                      acc.o[j][u * B::VW + e], 0, 0, 0);
     }
+}
+
+template <typename T, int HD>
+__device__ __forceinline__ bool block_odd(const Block<T, HD>& x) {
+    using B = Block<T, HD>;
+    uint32_t any = 0;
+#pragma unroll
+    for (int r = 0; r < 4 * B::TK; ++r)
+#pragma unroll
+        for (int u = 0; u < B::VU; ++u)
+#pragma unroll
+            for (int e = 0; e < B::VD; ++e) any |= odd_bits<T>(x.v[r][u][e]);
+    return any_odd<T>(any);
+}
+// block_sums for a block with such values, whose rows end at `from` .. `upto` (or behind).
+template <typename T, int HD, int NT>
+__device__ __forceinline__ void block_sums_odd(const Block<T, HD>& x, const f4 (&sc)[NT][Block<T, HD>::TK], int k0, int from,
+                                               int upto, const int (&pos)[NT], Acc<T, HD, NT>& acc, int lane) {
+    using B = Block<T, HD>;
+#pragma unroll 1
+    for (int at = from; at <= upto; ++at)
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            const int key = unknown(k0 + (lane >> 4) * 4);
+            u4 w = {};
+            if constexpr (B::H) {
+                w = values_b8<HD>(x, i, unknown(0));
+#pragma unroll
+                for (int d = 0; d < 4; ++d) w[d] &= cut_mask(key + 16 * (d / 2) + d % 2 * 2, at);
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                f4 c = {0.f, 0.f, 0.f, 0.f};
+                if constexpr (B::H) {
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, w), weights_b8(sc[j]), c, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        c = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                            key + r <= at ? __uint_as_float(x.v[r][i / B::VW][i % B::VW]) : 0.f, sc[j][0][r], c, 0, 0, 0);
+                }
+                const bool mine = min(pos[j], upto) == at;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc.o[j][i][r] += mine ? c[r] : 0.f;
+            }
+        }
 }
 
 // Query vector v of a sequence and KV head: row v / G of the sequence, head kvh * G + v % G.
@@ -390,6 +474,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
             page[1][t] = page[2][t];
         }
     };
+    // whether rows differ in what they read of a block; such blocks come last
+    auto mixed = [&](int k) { return min(k + BK, ke) - 1 > first; };
+    bool odd = false;
     if constexpr (NT == 1) {
         // the next block is requested before this one is used
         Block<T, HD> x[2];
@@ -401,23 +488,43 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
                 if (k >= ke) break;
                 look(k + 2 * step, page[2]);
                 load_block<T, HD, kLoadK | kLoadV>(x[1 - i], a.c, kvh, page[1], k + step, ke, lane);
+                if (mixed(k) && block_odd<T, HD>(x[i])) {
+                    odd = true;
+                    k0 = k;
+                    break;
+                }
                 block_scores<T, HD, NT>(x[i], q, sc, page[0], k, pos, whole(k), scale, lane);
+                block_weights<T, HD, NT>(acc, sc);
                 block_sums<T, HD, NT>(x[i], sc, acc);
                 shift();
             }
+            if (odd) break;
         }
     } else {
         // registers for one block: its K is replaced when the scores are there, its V when the sums are
         Block<T, HD> x;
         load_block<T, HD, kLoadK | kLoadV>(x, a.c, kvh, page[0], k0, ke, lane);
-        for (; k0 < ke; k0 += step) {
+        for (; k0 < ke && !(mixed(k0) && block_odd<T, HD>(x)); k0 += step) {
             look(k0 + 2 * step, page[2]);
             block_scores<T, HD, NT>(x, q, sc, page[0], k0, pos, whole(k0), scale, lane);
             load_block<T, HD, kLoadK>(x, a.c, kvh, page[1], k0 + step, ke, lane);
+            block_weights<T, HD, NT>(acc, sc);
             block_sums<T, HD, NT>(x, sc, acc);
             load_block<T, HD, kLoadV>(x, a.c, kvh, page[1], k0 + step, ke, lane);
             shift();
         }
+    }
+    // from a block with infinities or NaN on one by one, apart so that it costs the others no registers
+#pragma unroll 1
+    for (; k0 < ke; k0 += step) {
+        Block<T, HD> x;
+        const int lane = unknown(threadIdx.x) & 63;
+        look(k0, page[0]);
+        load_block<T, HD, kLoadK>(x, a.c, kvh, page[0], k0, ke, lane);
+        block_scores<T, HD, NT>(x, q, sc, page[0], k0, pos, false, scale, lane);
+        block_weights<T, HD, NT>(acc, sc);
+        load_block<T, HD, kLoadV>(x, a.c, kvh, page[0], k0, ke, lane);
+        block_sums_odd<T, HD, NT>(x, sc, k0, max(first, k0), min(k0 + BK, ke) - 1, pos, acc, lane);
     }
     // the waves' parts on one maximum, then added
 #pragma unroll
@@ -510,7 +617,8 @@ __device__ __forceinline__ f4 join_parts(const float* po, const float* pm, int l
         m = mn;
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-            const float w = s0 + s < live ? __builtin_amdgcn_exp2f(ml[s][0] - base) : 0.f;
+            if (s0 + s >= live) break;
+            const float w = __builtin_amdgcn_exp2f(ml[s][0] - base);
             l += w * ml[s][1];
             o += w * x[s];
         }
@@ -688,7 +796,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
     const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
     int entry = look(t0 * KT), entry1 = look((t0 + 1) * KT);
     u4 q[NS];
-    const float c = fabsf(a.scale) * kLog2e;
+    const float c = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
     const int v = wv + n, vc = min(v, nqv - 1), pos = at0 + vc / G;
     {
         const uint16_t* p = (const uint16_t*)a.q + (r0 + vc / G) * a.q_stride + (kvh * G + vc % G) * HD + 8 * g;
@@ -815,6 +923,36 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
             for (int i = 0; i < NC; ++i)
                 o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, x[u][i]), __builtin_bit_cast(b8, p[u]), o[i], 0, 0, 0);
     };
+    // (as block_odd; the block's V is 0 afterwards)
+    auto odd = [&](const u4 (&p)[2], u4 (&x)[2][NC], int k) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < 8 * NC; ++i) any |= odd_bits<uint16_t>(x[i / 4 % 2][i / 8][i % 4]);
+        if (!any_odd<uint16_t>(any)) return;
+        const int upto = min(32 * k + 32, end) - 1;
+#pragma unroll 1
+        for (int at = max(wfirst, 32 * k); at <= upto; ++at)
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int key = unknown(32 * k + 4 * g);
+                f16v w = {};
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    u4 y;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) y[d] = x[u][i][d] & cut_mask(key + 16 * u + 8 * (d / 2) + d % 2 * 2, at);
+                    w = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, y), __builtin_bit_cast(b8, p[u]), w, 0, 0, 0);
+                }
+                const bool mine = min(pos, upto) == at;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[i][r] += mine ? w[r] : 0.f;
+            }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < NC; ++i) x[u][i] = u4{};
+    };
     auto meet = [] {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
@@ -829,10 +967,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
     load(t0 * KT, pg, t0 & 1);
     entry = entry1;
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-    // (a negative scale turns into the sign of q)
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    // (a negative scale turns into the sign of q, and 0 into q = 0: scores that do not count are -inf before
+    // they are scaled)
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = a.scale != 0.f ? ~0u : 0u;
 #pragma unroll
-    for (int i = 0; i < NS; ++i) q[i] ^= flip;
+    for (int i = 0; i < NS; ++i) q[i] = (q[i] ^ flip) & keep;
     __syncthreads();
     f16v s;
     u4 x[2][NC];
@@ -868,6 +1007,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArg
                     settle(s, k, hv);
                     sum = weights(s, p);
                     begun = !__any(m == -INFINITY);
+                    if (32 * k + 31 > wfirst) odd(p, x, k);
                 }
                 l += sum;
             }
@@ -997,75 +1137,117 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
         }
     };
     const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
-    int pg[2], nx[2];
-    look(t0 * KT, pg);
-    look((t0 + 1) * KT, nx);
-    load(t0 * KT, pg);
-    store(t0 & 1);
-    for (int t = t0; t < nt; ++t) {
-        __syncthreads();
-        const int k0 = t * KT;
-        const bool whole = k0 + 31 <= wfirst && pg[0] >= 0 && pg[1] >= 0;
-        const bool have[2] = {pg[0] >= 0, pg[1] >= 0};
-        if (t + 1 < nt) {
-            pg[0] = nx[0];
-            pg[1] = nx[1];
-            load(k0 + KT, pg);
-            look(k0 + 2 * KT, nx);
-        }
-        const float *kf = ks[t & 1], *vf = vs[t & 1];
-        if (k0 < wend) {
-            f16v s, s1;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = s1[r] = 0.f;
-#pragma unroll
-            for (int i = 0; i < HD / 8; ++i) {
-                const f4 x = *(const f4*)(kf + n * KL + 8 * i + 4 * g);
-#pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[i][e], s, 0, 0, 0);
-                    s1 = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e + 1], q[i][e + 1], s1, 0, 0, 0);
-                }
+    auto values = [&](const float* vf, int r, float (&x)[VW]) {
+        const float* p = vf + (8 * (r / 4) + 4 * g + r % 4) * HD + n * VW;
+        if constexpr (VW == 4) *(f4*)x = *(const f4*)p;
+        else if constexpr (VW == 2) *(f2*)x = *(const f2*)p;
+        else x[0] = *p;
+    };
+    // Tiles from `from` on.  The first whose V holds infinities or NaN that some rows only read (see odd_bits)
+    // and those behind are left to a second, careful pass, apart so that it costs the first no registers.
+    int todo = INT32_MAX;
+    auto pass = [&](auto careful, int from) {
+        constexpr bool kCareful = decltype(careful)::value;
+        int pg[2], nx[2];
+        look(from * KT, pg);
+        look((from + 1) * KT, nx);
+        load(from * KT, pg);
+        store(from & 1);
+        for (int t = from; t < nt; ++t) {
+            __syncthreads();
+            const int k0 = t * KT;
+            const bool whole = k0 + 31 <= wfirst && pg[0] >= 0 && pg[1] >= 0;
+            const bool have[2] = {pg[0] >= 0, pg[1] >= 0};
+            if (t + 1 < nt) {
+                pg[0] = nx[0];
+                pg[1] = nx[1];
+                load(k0 + KT, pg);
+                look(k0 + 2 * KT, nx);
             }
-            s += s1;
-            if (!whole)
+            const float *kf = ks[t & 1], *vf = vs[t & 1];
+            if (!kCareful && k0 < wend && k0 + 31 > wfirst && t < todo) {
+                uint32_t any = 0;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int key = 8 * (r / 4) + 4 * g + r % 4;
-                    s[r] = k0 + key <= pos && have[r / 8] ? s[r] : -INFINITY;
+                    float x[VW];
+                    values(vf, r, x);
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) any |= odd_bits<float>(__float_as_uint(x[i]));
                 }
-            float mx = s[0];
-#pragma unroll
-            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-            mx = half_max(mx);
-            if (__any(mx > m + kLazy)) {
-                const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-                m = mn;
-                l *= f;
-#pragma unroll
-                for (int i = 0; i < VW; ++i) o[i] *= f;
+                if (any_odd<float>(any)) todo = t;
             }
-            const float base = m == -INFINITY ? 0.f : m;
-            float sum = 0.f;
+            if (k0 < wend && (kCareful ? t >= todo : t < todo)) {
+                f16v s, s1;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = __builtin_amdgcn_exp2f(s[r] - base);
-                sum += s[r];
+                for (int r = 0; r < 16; ++r) s[r] = s1[r] = 0.f;
+#pragma unroll
+                for (int i = 0; i < HD / 8; ++i) {
+                    const f4 x = *(const f4*)(kf + n * KL + 8 * i + 4 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[i][e], s, 0, 0, 0);
+                        s1 = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e + 1], q[i][e + 1], s1, 0, 0, 0);
+                    }
+                }
+                s += s1;
+                if (!whole)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int key = 8 * (r / 4) + 4 * g + r % 4;
+                        s[r] = k0 + key <= pos && have[r / 8] ? s[r] : -INFINITY;
+                    }
+                float mx = s[0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+                mx = half_max(mx);
+                if (__any(mx > m + kLazy)) {
+                    const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+                    m = mn;
+                    l *= f;
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) o[i] *= f;
+                }
+                const float base = m == -INFINITY ? 0.f : m;
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = __builtin_amdgcn_exp2f(s[r] - base);
+                    sum += s[r];
+                }
+                l += sum;
+                if constexpr (!kCareful) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        float x[VW];
+                        values(vf, r, x);
+#pragma unroll
+                        for (int i = 0; i < VW; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], s[r], o[i], 0, 0, 0);
+                    }
+                } else {
+                    const int upto = min(k0 + 32, end) - 1;
+#pragma unroll 1
+                    for (int at = max(wfirst, k0); at <= upto; ++at)
+#pragma unroll
+                        for (int i = 0; i < VW; ++i) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            const int key = unknown(4 * g), left = at - k0 - key;
+                            f16v w = {};
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) {
+                                const float x = vf[(key + 8 * (r / 4) + r % 4) * HD + n * VW + i];
+                                w = __builtin_amdgcn_mfma_f32_32x32x2f32(8 * (r / 4) + r % 4 <= left ? x : 0.f, s[r], w, 0, 0, 0);
+                            }
+                            const bool mine = min(pos, upto) == at;
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) o[i][r] += mine ? w[r] : 0.f;
+                        }
+                }
             }
-            l += sum;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float* p = vf + (8 * (r / 4) + 4 * g + r % 4) * HD + n * VW;
-                float x[VW];
-                if constexpr (VW == 4) *(f4*)x = *(const f4*)p;
-                else if constexpr (VW == 2) *(f2*)x = *(const f2*)p;
-                else x[0] = *p;
-#pragma unroll
-                for (int i = 0; i < VW; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], s[r], o[i], 0, 0, 0);
-            }
+            if (t + 1 < nt) store((t + 1) & 1);
         }
-        if (t + 1 < nt) store((t + 1) & 1);
-    }
+    };
+    pass(std::false_type{}, t0);
+    if (__syncthreads_or(todo != INT32_MAX)) pass(std::true_type{}, max(t0, (at0 + v0 / G) / KT));
     const float sum = half_sum(l), inv = sp.live > 1 ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
     if (v >= nqv) return;
     const int64_t at = (((int64_t)tile * a.c.Hkv + kvh) * d.nspan + span) * QV + wv - v0 + n;
@@ -1141,7 +1323,8 @@ PromptPlan prompt_plan(const PagedView& c, const PagedRows& r, int H, bool bf16,
 template <typename T, int HD>
 hipError_t prompt(hipStream_t s, const PagedAttnArgs& a, const PromptPlan& p, float* ws) {
     const int64_t groups = p.tiles * a.c.Hkv, nj = kPromptQv<T> * (HD / 4) / 256;
-    if (groups * std::max<int64_t>(p.nspan, nj) > INT32_MAX) return hipErrorInvalidValue;
+    // (a launch has fewer than 2^32 threads)
+    if (groups * std::max<int64_t>(p.nspan, nj) > UINT32_MAX / (64 * kPromptWaves)) return hipErrorInvalidValue;
     const PromptArgs d{a, (int)p.tiles, p.nspan, p.keys, ws, p.ml};
     hipError_t err;
     if constexpr (sizeof(T) == 2) err = launch(k_pprompt_bf16<HD>, dim3((unsigned)(groups * p.nspan)), dim3(64 * kPromptWaves), s, d);
@@ -1187,7 +1370,7 @@ template <typename T, int HD, int NT>
 hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p, float* ws) {
     const DecodeArgs d{a, p.ncg, p.target, kDecodeWaves * kBlockKeys<T>, p.units, ws, p.ml};
     const int64_t per = ((int64_t)p.units * a.c.Hkv + 7) / 8 * 8;
-    if (per * p.ncg > INT32_MAX) return hipErrorInvalidValue;
+    if (per * p.ncg > UINT32_MAX / (64 * kDecodeWaves)) return hipErrorInvalidValue;  // (a launch has fewer than 2^32 threads)
     const hipError_t err = launch(k_pdecode<T, HD, NT>, dim3((unsigned)(per * p.ncg)), dim3(64 * kDecodeWaves), s, d);
     if (err != hipSuccess || !p.target) return err;
     constexpr int q = 256 / (HD / 4), nb = (16 * NT + q - 1) / q;

@@ -23,27 +23,31 @@ struct AppendArgs {
     int64_t k_stride, v_stride;  // bytes
     int lc;                      // 16-byte units of a head's row: a power of two, 1 << lc
 };
+constexpr int kAppendBlocks = 1 << 22;  // (of 256 threads: a launch may have fewer than 2^32)
 
 __global__ __launch_bounds__(256) void k_paged_append(AppendArgs a) {
     const int lane = threadIdx.x & 63;
-    const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    if (row >= a.r.total_rows) return;
-    const int b = paged_seq(a.r, row);
-    int n;
-    const int r0 = paged_rows(a.r, b, n);
-    if (row < r0 || row >= r0 + n) return;
-    const int pos = a.r.row_pos ? a.r.row_pos[row] : paged_len(a.r, b, r0, n) - n + (row - r0);
-    if (pos < 0) return;
-    const int page = paged_page(a.c, b, pos >> a.c.shift);
-    if (page < 0) return;
-    const int slot = pos & ((1 << a.c.shift) - 1), unit = 16 << a.lc;
-    const int64_t base = (int64_t)page * a.c.page_stride * (unit / a.c.hd);
-    for (int i = lane; i < a.c.Hkv << a.lc; i += 64) {
-        const int h = i >> a.lc, u = i & ((1 << a.lc) - 1);
-        const int64_t at = base + (((int64_t)h << a.c.shift) + slot) * unit + 16 * u;
-        const uint4 x = *(const uint4*)(a.k + row * a.k_stride + 16 * i), y = *(const uint4*)(a.v + row * a.v_stride + 16 * i);
-        *(uint4*)((char*)a.c.k + at) = x;
-        *(uint4*)((char*)a.c.v + at) = y;
+    // (a wave has one row, but where there are more than kAppendBlocks workgroups of them)
+    for (int64_t at_row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); at_row < a.r.total_rows;
+         at_row += (int64_t)gridDim.x * 4) {
+        const int row = (int)at_row;
+        const int b = paged_seq(a.r, row);
+        int n;
+        const int r0 = paged_rows(a.r, b, n);
+        if (row < r0 || row >= r0 + n) continue;
+        const int pos = a.r.row_pos ? a.r.row_pos[row] : paged_len(a.r, b, r0, n) - n + (row - r0);
+        if (pos < 0) continue;
+        const int page = paged_page(a.c, b, pos >> a.c.shift);
+        if (page < 0) continue;
+        const int slot = pos & ((1 << a.c.shift) - 1), unit = 16 << a.lc;
+        const int64_t base = (int64_t)page * a.c.page_stride * (unit / a.c.hd);
+        for (int i = lane; i < a.c.Hkv << a.lc; i += 64) {
+            const int h = i >> a.lc, u = i & ((1 << a.lc) - 1);
+            const int64_t at = base + (((int64_t)h << a.c.shift) + slot) * unit + 16 * u;
+            const uint4 x = *(const uint4*)(a.k + row * a.k_stride + 16 * i), y = *(const uint4*)(a.v + row * a.v_stride + 16 * i);
+            *(uint4*)((char*)a.c.k + at) = x;
+            *(uint4*)((char*)a.c.v + at) = y;
+        }
     }
 }
 
@@ -390,7 +394,7 @@ hipError_t paged_append(hipStream_t s, const PagedView& c, const PagedRows& r, c
     if (!r.total_rows || !r.nseq) return hipSuccess;
     AppendArgs a{c, r, (const char*)k, (const char*)v, k_stride * size, v_stride * size, 0};
     while (16 << a.lc < c.hd * size) ++a.lc;
-    return launch(k_paged_append, dim3((r.total_rows + 3) / 4), dim3(256), s, a);
+    return launch(k_paged_append, dim3((unsigned)std::min<int64_t>(((int64_t)r.total_rows + 3) / 4, kAppendBlocks)), dim3(256), s, a);
 }
 
 namespace {
@@ -432,7 +436,7 @@ bool rows_of(const sd2_paged_rows* rows, PagedRows* r) {
         return false;
     if (rows->nseq && !aligned(rows->lens, 4)) return false;
     if (rows->row_off ? !aligned(rows->row_off, 4) : (int64_t)rows->nseq * rows->max_rows != rows->total_rows) return false;
-    const int32_t most = rows->row_off ? std::min(rows->max_rows, std::max(rows->total_rows, 1)) : rows->max_rows;
+    const int32_t most = std::min(rows->max_rows, std::max(rows->total_rows, 1));
     *r = PagedRows{rows->nseq, most, rows->total_rows, rows->row_off, rows->lens, nullptr};
     return true;
 }
@@ -516,6 +520,7 @@ size_t sd2_paged_attn_workspace_bytes(const sd2_paged_kv* kv, const sd2_paged_ro
     PagedRows r;
     int size;
     if (!view_of(kv, &c, &size) || !rows_of(rows, &r) || n_heads < 1 || n_heads > 1024 || n_heads % c.Hkv) return 0;
+    if ((int64_t)r.max_rows * (n_heads / c.Hkv) > 1 << 30) return 0;
     if (max_len < 1 || max_len > (int64_t)c.max_pages << c.shift) return 0;
     return paged_attn_bytes(c, r, n_heads, size == 2, max_len);
 }
@@ -528,6 +533,7 @@ sd2_status sd2_paged_attn(const sd2_paged_kv* kv, const sd2_paged_rows* rows, co
     if (!view_of(kv, &a.c, &size) || !rows_of(rows, &a.r)) return SD2_ERR_INVALID_ARG;
     if (n_heads < 1 || n_heads > 1024 || n_heads % a.c.Hkv || !(scale >= -1e30f && scale <= 1e30f)) return SD2_ERR_INVALID_ARG;
     if (max_len < 1 || max_len > (int64_t)a.c.max_pages << a.c.shift) return SD2_ERR_INVALID_ARG;
+    if ((int64_t)a.r.max_rows * (n_heads / a.c.Hkv) > 1 << 30) return SD2_ERR_INVALID_ARG;
     if (!a.r.nseq || !a.r.total_rows) return SD2_OK;
     const int64_t width = (int64_t)n_heads * a.c.hd;
     if (!strided(q, q_stride, width, size) || !strided(out, out_stride, width, size)) return SD2_ERR_INVALID_ARG;

@@ -87,6 +87,7 @@ class PagedCache:
         """A tensor [rows][heads][head_dim] whose rows may be apart: its row stride."""
         _need(isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == self.dtype and t.dim() == 3 and
               t.shape[2] == self.head_dim, f"{what}: [rows][heads][head_dim] of the cache's type, on its device")
+        _need(not t.requires_grad or not torch.is_grad_enabled(), f"{what}: no gradients here (torch.no_grad(), or detach it)")
         if t.numel():
             _need(t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == self.head_dim),
                   f"{what}: heads and head dimension have to be contiguous")
@@ -190,6 +191,7 @@ class PagedCache:
         ints)."""
         src, dst = list(src), list(dst)
         _need(len(src) == len(dst), "fork: as many src as dst")
+        _need(all(0 <= b < self.max_seqs for b in src + dst), f"fork: the table has {self.max_seqs} sequences")
         n = len(src)
         arr = ctypes.c_int32 * max(n, 1)
         self._call(self.lib.sd2_pages_fork, ctypes.byref(self._pages), n, arr(*src), arr(*dst))

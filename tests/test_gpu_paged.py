@@ -193,6 +193,58 @@ def test_non_finite_values_reach_the_rows_that_read_them():
             bound = attend_bound(ref, absv, spread, dtype, 200, 64)
             assert ((got.double() - ref).abs()[rows:] <= bound[rows:]).all(), "the other sequence does not"
 
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("hkv,hd", [(2, 32), (1, 64), (2, 128)])
+@pytest.mark.parametrize("rows", [3, 9, 21, 33, 70, 600])
+@pytest.mark.parametrize("before", [0, 2, 1500])
+def test_non_finite_values_of_later_rows_do_not_count(dtype, hkv, hd, rows, before):
+    """v of one of the call's own positions: NaN in one column, infinities in others, a NaN in a later position's
+    k.  The rows before are as if neither were there, and so are the other columns of those between."""
+    heads = 2 * hkv
+    lens = [before + rows, before + rows]
+    cache = make_cache(lens, dtype, hkv, hd, 16)
+    q = queries(2 * rows, heads, hd, dtype)
+    ref, absv, spread = attend64(cache, q, lens, [rows] * 2)
+    bound = attend_bound(ref, absv, spread, dtype, lens[0], hd)
+    bad, last = before + rows // 2, before + rows - 1
+
+    def slot(at):
+        return int(cache.table[0, at // 16]), 0, slice(None), at % 16
+
+    v = cache.v[slot(bad)]
+    v[:, 3], v[:, 5], v[:, 8], v[:, hd - 1] = float("nan"), float("inf"), -float("inf"), float("inf")
+    cache.v[slot(bad)] = v
+    v = cache.v[slot(bad + 1 if bad < last else bad)]
+    if bad < last:
+        v[:, hd - 1] = -float("inf")  # both signs: NaN
+        cache.v[slot(bad + 1)] = v
+    k = cache.k[slot(last)]
+    k[:, 0] = float("nan")
+    cache.k[slot(last)] = k
+    ln, _ = rows_of(lens, [rows] * 2, False)
+    got = cache.attend(q, ln).double()
+    ok = (got - ref).abs() <= bound
+    first = bad - before  # row of the first one
+    assert ok[rows:].all(), "another sequence"
+    assert ok[:first].all(), "rows before"
+    assert torch.isnan(got[rows - 1]).all(), "the row that reads the key"
+    mid = slice(first, rows - 1)
+    plain = [c for c in range(hd) if c not in (3, 5, 8, hd - 1)]
+    assert ok[mid][:, :, plain].all(), "columns without"
+    assert torch.isnan(got[mid][:, :, 3]).all()
+    assert (got[mid][:, :, 5] == float("inf")).all() and (got[mid][:, :, 8] == -float("inf")).all()
+    assert torch.isnan(got[first + 1: rows - 1][:, :, hd - 1]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 5, 40, 300])
+def test_scale_zero_is_a_mean(dtype, rows):
+    lens = [rows + 130, rows]
+    cache = make_cache(lens, dtype, 2, 64, 16)
+    check(cache, queries(2 * rows, 4, 64, dtype), lens, [rows] * 2, False, scale=0.0)
+
+
 @pytest.mark.parametrize("rows", [1, 20, 200])
 def test_far_pages_of_a_large_pool(rows):
     # element offsets beyond 2^32
@@ -273,6 +325,13 @@ def test_refusals_of_the_binding():
         PagedCache(cache.k, cache.v, cache.table, cache.refs[:-1])
     with pytest.raises(Sd2Error):
         PagedCache.empty(4, 24, 1, 1, 64, 1, 1)
+    grad = q.clone().requires_grad_()
+    for call in (lambda: cache.attend(grad, ln), lambda: cache.append(grad[:, :2], q[:, :2], ln),
+                 lambda: cache.fork([2 ** 32], [1])):
+        with pytest.raises(Sd2Error):
+            call()
+    with torch.no_grad():
+        cache.attend(grad, ln)
     # nothing to do is no error
     cache.fork([], [])
     none = torch.zeros(0, dtype=torch.int32, device="cuda")

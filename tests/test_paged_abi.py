@@ -112,6 +112,10 @@ def test_attn_and_append_arguments_refused():
                dict(heads=6), dict(heads=1028), dict(scale=float("nan")), dict(scale=float("inf")), dict(max_len=0),
                dict(max_len=65), dict(ws=None), dict(ws=AT + 64), dict(n=0)]:
         assert attn(lib, c, r, **kw) == -1, kw
+    # more query vectors of one sequence and KV head than 2^30
+    many = rows(total_rows=(1 << 29) + 1, max_rows=1 << 30, row_off=AT)
+    assert attn(lib, c, many) == -1
+    assert lib.sd2_paged_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(many), 8, 64) == 0
     for args in [(None, 256, AT, 256), (AT, 248, AT, 256), (AT, 256, AT + 4, 256), (AT, 256, AT, 260)]:
         assert lib.sd2_paged_append(ctypes.byref(c), ctypes.byref(r), *args, None) == -1, args
     # nothing to do is no error
