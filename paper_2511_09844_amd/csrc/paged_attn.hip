@@ -617,10 +617,11 @@ __device__ __forceinline__ f4 join_parts(const float* po, const float* pm, int l
         m = mn;
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-            if (s0 + s >= live) break;
-            const float w = __builtin_amdgcn_exp2f(ml[s][0] - base);
+            const bool on = s0 + s < live;  // (a select: 0 times an infinity is NaN)
+            const float w = on ? __builtin_amdgcn_exp2f(ml[s][0] - base) : 0.f;
             l += w * ml[s][1];
-            o += w * x[s];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] += on ? w * x[s][i] : 0.f;
         }
     }
     return o * (l > 0.f ? 1.f / l : 0.f);
@@ -763,7 +764,7 @@ __device__ __forceinline__ Span prompt_span(int end, int nspan, int keys, int sp
 }
 
 template <int HD>
-__global__ __launch_bounds__(64 * kPromptWaves, 2) void k_pprompt_bf16(PromptArgs d) {
+__global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt_bf16(PromptArgs d) {
     constexpr int NW = kPromptWaves, KT = prompt_keys(HD), NB = KT / 32, NS = HD / 16, NC = HD / 32, CH = HD / 8;
     constexpr int QV = 32 * NW, RB = HD * 2;
     __shared__ __attribute__((aligned(1024))) char ks[2][KT * RB], vs[2][KT * RB];
