@@ -51,6 +51,21 @@ __device__ __forceinline__ float col_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// Sum over a wave.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int v) {
+    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_total(int v) {
+    v = dpp_add<0xB1, 0xf>(v);   // quad_perm [1,0,3,2]
+    v = dpp_add<0x4E, 0xf>(v);   // quad_perm [2,3,0,1]
+    v = dpp_add<0x141, 0xf>(v);  // row_half_mirror
+    v = dpp_add<0x140, 0xf>(v);  // row_mirror
+    v = dpp_add<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
+    v = dpp_add<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
     const f2 v = {x, y};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
@@ -422,11 +437,23 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     const int b = un.b;
     if (b < 0) return;
     const int G = a.H / a.c.Hkv;
+    // the first two blocks' table entries, which need no length (a sequence that is one unit has been asked
+    // for nothing else yet, and one round trip to memory is saved)
+    constexpr int step = kDecodeWaves * BK;
+    const int kb = (unit - un.first) * un.keys;
+    int k0 = kb + wave * BK;
+    int entry[2][B::TK];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < B::TK; ++t) {
+            const int j = (k0 + i * step + 16 * t) >> a.c.shift;
+            entry[i][t] = j < a.c.max_pages ? a.c.table[(int64_t)b * a.c.max_pages + j] : -1;
+        }
     const int r0 = uniform(un.rows.r0), nrows = uniform(un.rows.n), len = uniform(un.rows.len);
     const int nqv = nrows * G, v0 = cg * QV;
     if (v0 >= nqv) return;
     // the unit's positions that some row of this group reads
-    const int kb = (unit - un.first) * un.keys;
     const int ke = min(min(len - nrows + min(v0 + QV - 1, nqv - 1) / G + 1, seq_end(a, un.rows)), un.count > 1 ? kb + un.keys : INT32_MAX);
     const bool whole_seq = un.count == 1;
     const int64_t slot = ((int64_t)unit * a.c.Hkv + kvh) * d.ncg + cg;
@@ -455,11 +482,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
         for (int t = 0; t < B::TK; ++t)
             page[t] = k0 + 16 * t < ke ? __builtin_amdgcn_readfirstlane(paged_page(a.c, b, (k0 + 16 * t) >> a.c.shift)) : -1;
     };
-    constexpr int step = kDecodeWaves * BK;
-    int k0 = kb + wave * BK;
     int page[3][B::TK];
-    look(k0, page[0]);
-    look(k0 + step, page[1]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < B::TK; ++t) {
+            const int p = uniform(entry[i][t]);
+            page[i][t] = k0 + i * step + 16 * t < ke && (uint32_t)p < (uint32_t)a.c.n_pages ? p : -1;
+        }
     f4 sc[NT][B::TK];
     auto whole = [&](int k) {
         bool w = k + BK - 1 <= min(first, ke - 1);
@@ -720,8 +750,7 @@ __device__ __forceinline__ Tile prompt_tile(const PagedRows& r, int G, int w) {
     auto from = [&](int j) {
         int n = max(tiles - j, 0);
         for (int b0 = 64; b0 < r.nseq; b0 += 64) n += max(others(b0 + lane) - j, 0);
-        // (whole numbers that fp32 sums exactly in two halves)
-        return ((int)wave_sum_dpp((float)(n >> 12)) << 12) + (int)wave_sum_dpp((float)(n & 4095));
+        return wave_total(n);
     };
     // the largest j with more than w of them
     if (from(0) <= w) return t;
@@ -779,31 +808,38 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
     if (b < 0) return;
     const int nqv = nrows * G;
     if (v0 >= nqv) return;
-    const int at0 = uniform(tl.rows.len) - nrows;
-    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, span);
-    if (span >= sp.live) return;
-    const int end = sp.upto;
-    const int wv = v0 + 32 * wave;                       // the wave's first query vector
-    const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 31, nqv - 1) / G + 1) : 0;
     // table entries of the KT / 16 groups of keys of a tile, a lane each, and the pages they name (apart: the
-    // first test of an entry waits for it, and for all loads before)
-    auto look = [&](int k0) {
-        const int key = k0 + 16 * lane;
+    // first test of an entry waits for it, and for all loads before).  Those of the first two tiles, and q, are
+    // requested before the length is there.
+    auto ask = [&](int key) {
         int e = -1;
-        if (lane < KT / 16 && key < end) e = a.c.table[(int64_t)b * a.c.max_pages + (key >> a.c.shift)];
+        if (lane < KT / 16 && key >> a.c.shift < a.c.max_pages) e = a.c.table[(int64_t)b * a.c.max_pages + (key >> a.c.shift)];
         return e;
     };
-    auto named = [&](int e) { return (uint32_t)e < (uint32_t)a.c.n_pages ? e : -1; };
-    const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
-    int entry = look(t0 * KT), entry1 = look((t0 + 1) * KT);
+    const int span0 = d.nspan > 1 ? span * d.keys : 0;  // (as prompt_span, for a span that has keys)
+    int entry = ask(span0 + 16 * lane), entry1 = ask(span0 + KT + 16 * lane);
+    const int wv = v0 + 32 * wave;  // the wave's first query vector
     u4 q[NS];
-    const float c = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
-    const int v = wv + n, vc = min(v, nqv - 1), pos = at0 + vc / G;
+    const int v = wv + n, vc = min(v, nqv - 1);
     {
         const uint16_t* p = (const uint16_t*)a.q + (r0 + vc / G) * a.q_stride + (kvh * G + vc % G) * HD + 8 * g;
 #pragma unroll
         for (int s = 0; s < NS; ++s) q[s] = *(const u4*)(p + 16 * s);
     }
+    const int at0 = uniform(tl.rows.len) - nrows, pos = at0 + vc / G;
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, span);
+    if (span >= sp.live) return;
+    const int end = sp.upto;
+    const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 31, nqv - 1) / G + 1) : 0;
+    auto look = [&](int k0) {
+        const int key = k0 + 16 * lane;
+        return key < end ? ask(key) : -1;
+    };
+    auto named = [&](int e) { return (uint32_t)e < (uint32_t)a.c.n_pages ? e : -1; };
+    const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
+    if (span0 + 16 * lane >= end) entry = -1;
+    if (span0 + KT + 16 * lane >= end) entry1 = -1;
+    const float c = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
     f16v o[NC];
     float m = -INFINITY, l = 0.f;
 #pragma unroll
