@@ -16,6 +16,11 @@
 // those keys go through one buffer descriptor, whose size says how many of the 16 rows exist: rows behind
 // the last position and pages that are missing read as zeros, whatever lies there, and nothing
 // outside a page is ever addressed.
+//
+// Few rows are bound by the bytes of K and V: on MI355X one token of 16 fp32 sequences (152 MB) takes 37 us with
+// its join, one of a bf16 batch of 905 MB 165 (5.5 TB/s), eight rows of 16 fp32 sequences 50 (155 MB, and
+// 16 us of fp32 matrix instructions that overlap with the loads in part); one short sequence is
+// bound by round trips to memory in a row, 6.9 us.  Prompts are bound by the matrix cores, see k_pprompt_bf16.
 #include <math.h>
 
 #include <algorithm>
@@ -105,6 +110,8 @@ __device__ __forceinline__ void put(const PagedAttnArgs& a, int row, int c, cons
 // The keys a workgroup of k_pdecode takes at a time, 16 or 32 per wave.
 template <typename T>
 constexpr int kBlockKeys = sizeof(T) == 2 ? 32 : 16;
+// Waves of a workgroup: with 8 the one-token calls of 16 fp32 sequences take 42.5 us, not 36.5, and blocks of eight
+// rows 57, not 49 (larger units, and one more join of the waves' sums).
 constexpr int kDecodeWaves = 4;
 
 struct DecodeArgs {
@@ -690,7 +697,11 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
 // The two waves of a SIMD take turns: while one computes weights (vector instructions) the other has the
 // matrix cores and LDS (its sums with V, then the next block's scores, the operands of both read
 // meanwhile); a barrier after each turn keeps them apart.  Unsynchronised, both tended to want the same unit:
-// 8192 positions, 32/8 heads of 128, took 660 us that way, 570 in turns.
+// 8192 positions, 32/8 heads of 128, took 660 us that way, 570 in turns, and 510 to 540 (1.05 PFLOP/s; a large
+// matrix product of torch reaches 1.16) since the waves' turns are balanced (about 700 cycles of softmax
+// and 660 of matrix work in a slot of 945) and rows are stored whole.  Besides, a workgroup takes 6 to 8 thousand
+// cycles until its first scores and 5 for its rows, which short prompts show: 24 of 1 to 2001 positions reach
+// 0.7 PFLOP/s.
 //
 // The running maximum is raised only when a weight exceeds 2^kLazy: until then the sums need no
 // rescaling, and a block's scores no maximum, since large weights show in their bits.
@@ -1108,7 +1119,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
     }
 }
 
-// The same on fp32 matrix instructions, 32 query vectors per wave and tiles of 32 keys, row by row in LDS
+// The same on fp32 matrix instructions (115 TFLOP/s at 4096 positions, 32/8 heads of 128; a large product of torch
+// reaches 154), 32 query vectors per wave and tiles of 32 keys, row by row in LDS
 // (rows of K four words apart from whole bank rounds).  A lane reads a row of K, or HD / 32 neighbouring
 // columns of its keys of V, at a time.
 template <int HD>
@@ -1342,9 +1354,13 @@ PromptPlan prompt_plan(const PagedView& c, const PagedRows& r, int H, bool bf16,
     const int64_t G = H / c.Hkv, kt = bf16 ? prompt_keys(c.hd) : 32, most = (r.max_rows * G + QV - 1) / QV;
     PromptPlan p{};
     p.tiles = r.row_off ? std::min(r.total_rows * G / QV + r.nseq, r.nseq * most) : r.nseq * most;
-    // Workgroups for two on every CU (fp32, whose tiles are short: four), of at least two tiles (fp32: four)
+    // Workgroups for two rounds of what the CUs hold, one each (head dim 32: two), of at least two tiles; fp32,
+    // whose tiles are short: four on each CU, of at least four tiles.  bf16, 4096 positions, 256 / 512 / 1024
+    // workgroups: head dim 64 (32/8 heads) 109 / 109 / 168 us, head dim 32 (16 heads) 87 / 74 / 68; fp32, chunks of
+    // five sequences, 12 heads of 64, 512 / 768 / 1024 / 1536 / 2048: 74 / 62 / 58 / 56 / 63, but 4096 positions of 32/8
+    // heads of 128 take 1195 us with 1024 and 1611 with 2048
     const int64_t groups = std::max<int64_t>(1, p.tiles * c.Hkv), least = kt * (bf16 ? 2 : 4);
-    int64_t want = std::max<int64_t>(1, (bf16 ? 512 : 1024) / groups);
+    int64_t want = std::max<int64_t>(1, (bf16 && c.hd > 32 ? 512 : 1024) / groups);
     const size_t per = (size_t)groups * QV * (c.hd + 2) * sizeof(float);
     if (want > 1) want = std::min<int64_t>(want, std::max<size_t>(1, bytes / per));
     const int64_t keys = std::max(least, ((max_len + want - 1) / want + kt - 1) / kt * kt);
@@ -1370,13 +1386,17 @@ hipError_t prompt(hipStream_t s, const PagedAttnArgs& a, const PromptPlan& p, fl
     return launch(k_prompt_join<T, HD, kPromptQv<T>>, dim3((unsigned)(groups * nj)), dim3(256), s, d);
 }
 
-// Whether a call goes to k_pprompt.
-bool many_rows(const PagedView& c, const PagedRows& r, int H) {
-    return (int64_t)std::min(r.max_rows, r.total_rows) * (H / c.Hkv) > 64;
+// Whether a call goes to k_pprompt: by the query vectors of a sequence and KV head that share keys.  k_pdecode reads
+// the keys once per 32 of them, k_pprompt once per 256 (fp32: 128) and computes whole tiles.  32/8 heads of
+// 128, 16 sequences of 2000 positions / one of 20000, us in k_pdecode and in k_pprompt:
+//   bf16:  48: 49 and 49 / 32 and 36    68: 75 and 51 / 37 and 38    132: 82 and 61 / 50 and 46
+//   fp32: 128: 184 and 195 / 112 and 130    192: 239 and 310 / 212 and 203    224: 306 and 319 / 252 and 207
+bool many_rows(const PagedView& c, const PagedRows& r, int H, bool bf16) {
+    return (int64_t)r.max_rows * (H / c.Hkv) > (bf16 ? 64 : 192);
 }
 
 // Up to kDirect workgroup steps of expected positions a sequence is one unit, which writes its rows itself:
-// 517 positions of 8 KV heads take 9.7 us that way, and 7.3 and 3.5 in two launches.
+// 517 positions of 8 KV heads take 7.8 us that way, and 7.3 and 3.5 in two launches.
 constexpr int kDirect = 6;
 
 struct DecodePlan {
@@ -1389,10 +1409,12 @@ struct DecodePlan {
 DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes) {
     DecodePlan p;
     const int qv = std::min<int64_t>((int64_t)r.max_rows * (H / c.Hkv), 1 << 20);
+    // (blocks of 32 query vectors as two groups that read the keys once each: 62 us, not 49)
     p.nt = qv <= 16 ? 1 : 2;
     p.ncg = (qv + 16 * p.nt - 1) / (16 * p.nt);
     const int64_t groups = (int64_t)c.Hkv * p.ncg;
-    // two workgroups per CU, or as many units again as sequences
+    // two workgroups per CU, or as many units again as sequences (for 384 / 512 / 768 workgroups 16 fp32 sequences
+    // of 256 to 2048 take 41.4 / 36.4 / 44.6 us, and the 905 MB batch 171 / 159 / 161)
     int64_t target = max_len <= kDirect * kDecodeWaves * (bf16 ? 32 : 16) ? 0 : std::max<int64_t>((512 + groups - 1) / groups, r.nseq);
     const size_t per = (size_t)groups * 16 * p.nt * (c.hd + 2) * sizeof(float);
     if (target && per * (target + r.nseq + 8) > bytes) target = std::max<int64_t>(0, (int64_t)(bytes / per) - r.nseq - 8);
@@ -1416,7 +1438,7 @@ hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p
 
 template <typename T, int HD>
 hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws, size_t bytes) {
-    if (many_rows(a.c, a.r, a.H)) return prompt<T, HD>(s, a, prompt_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, bytes), ws);
+    if (many_rows(a.c, a.r, a.H, sizeof(T) == 2)) return prompt<T, HD>(s, a, prompt_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, bytes), ws);
     const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, bytes);
     return p.nt == 1 ? run_decode<T, HD, 1>(s, a, p, ws) : run_decode<T, HD, 2>(s, a, p, ws);
 }
@@ -1424,7 +1446,7 @@ hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float*
 }  // namespace
 
 size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
-    if (many_rows(c, r, H)) return std::max<size_t>(prompt_plan(c, r, H, bf16, max_len, SIZE_MAX).bytes, 256);
+    if (many_rows(c, r, H, bf16)) return std::max<size_t>(prompt_plan(c, r, H, bf16, max_len, SIZE_MAX).bytes, 256);
     const DecodePlan p = decode_plan(c, r, H, bf16, max_len, SIZE_MAX);
     return std::max<size_t>(p.bytes, 256);
 }
