@@ -634,3 +634,79 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for i in (0, 1):
         assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("most", [30, 300])
+def test_captured_packed_rows_follow_offsets_and_lengths(dtype, most):
+    """One captured call of packed rows, replayed for other divisions of them: chunks, single rows, none."""
+    total, entries = 2 * most + 5, 60
+    cache = make_cache([900, 900, 900], dtype, 2, 64, 16, extra_entries=4)
+    q = queries(total, 8, 64, dtype)
+    ln = torch.tensor([900, 900, 900], dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda")
+    out = torch.empty(total, 8, 64, dtype=dtype, device="cuda")
+    graph, _ = _capture(lambda: cache.attend(q, ln, row_off=off, max_rows=most, max_len=16 * entries, out=out))
+    for rows, lens in [([most, most, 5], [900, 811, 5]), ([1, 0, most], [1, 17, 900]), ([0, 0, 0], [900, 3, 0]), ([7, most, 1], [640, most, 333])]:
+        off.copy_(torch.tensor([0, rows[0], rows[0] + rows[1], sum(rows)], dtype=torch.int32))
+        ln.copy_(torch.tensor(lens, dtype=torch.int32))
+        q.copy_(queries(total, 8, 64, dtype, 50 + sum(rows)))
+        out.fill_(3.0)
+        graph.replay()
+        n = sum(rows)
+        ref, absv, spread = attend64(cache, q[:n], lens, rows)
+        assert ((out[:n].double() - ref).abs() <= attend_bound(ref, absv, spread, dtype, 900, 64)).all()
+        assert (out[n:] == 3.0).all(), "rows of no sequence"
+        again = out.clone()
+        graph.replay()
+        assert torch.equal(again, out)
+        torch.cuda.synchronize()
+
+
+def test_two_graphs_of_one_cache():
+    """Two captured calls, each with a workspace of its own, replayed in turn with eager calls between."""
+    lens = [2000, 700]
+    cache = make_cache(lens, BF16, 2, 128, 64)
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    one, many = queries(2, 8, 128, BF16, 1), queries(400, 8, 128, BF16, 2)
+    a, out_a = _capture(lambda: cache.attend(one, ln))
+    b, out_b = _capture(lambda: cache.attend(many, ln))
+    for i in range(4):
+        one.copy_(queries(2, 8, 128, BF16, 20 + i))
+        many.copy_(queries(400, 8, 128, BF16, 30 + i))
+        a.replay()
+        b.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out_a, cache.attend(one, ln)) and torch.equal(out_b, cache.attend(many, ln))
+
+
+def test_rows_kept_in_copies():
+    """keep: how much of a shared page its copy has to hold, whatever is written next."""
+    t = Tagged(20, 16, 4, 4)
+    t.reserve([0], [60])
+    t.write(0, 0, 60)
+    t.fork([0, 0, 0], [1, 2, 3])
+    t.reserve([0, 20, 33, 16], [0, 60, 34, 48], [0, 60, 40, 0])
+    t.check()
+    t.write(1, 20, 60)
+    t.check()
+    t.reserve([0, 0], [60, 60], [1000, -5])
+    t.check()
+
+
+def test_operands_out_of_alignment_are_refused():
+    from paper_2511_09844_amd.binding import Sd2Error
+    cache = make_cache([40, 50], BF16, 2, 64, 16)
+    ln = torch.tensor([40, 50], dtype=torch.int32, device="cuda")
+    flat = torch.zeros(2 * 4 * 64 + 8, dtype=BF16, device="cuda")
+    q = flat[4: 4 + 2 * 4 * 64].view(2, 4, 64)            # 8 bytes off
+    with pytest.raises(Sd2Error):
+        cache.attend(q, ln)
+    with pytest.raises(Sd2Error):
+        cache.append(q[:, :2], q[:, 2:], ln)
+    far = torch.zeros(2, 4 * 64 + 4, dtype=BF16, device="cuda")[:, :256].unflatten(1, (4, 64))  # rows 520 bytes apart
+    with pytest.raises(Sd2Error):
+        cache.attend(far, ln)
+    good = queries(2, 4, 64, BF16)
+    with pytest.raises(Sd2Error):
+        cache.attend(good, ln, out=q)
