@@ -392,8 +392,8 @@ sd2_status sd2_paged_append(const sd2_paged_kv* kv, const sd2_paged_rows* rows, 
  * Memory behind a sequence's last position, and pages it does not name, are not read, or do not count,
  * whatever they hold; infinities and NaN of a position reach the rows that read it, and no others.
  * The rows of a sequence times n_heads / n_kv_heads are at most 2^30.
- * max_len: the largest length expected, 1..max_pages * page_size (it decides how the work is split; a longer
- * sequence is computed all the same).
+ * max_len: the largest length expected, 1..max_pages * page_size (it decides into how many parts the work may be
+ * split, and the workspace; a longer sequence is computed all the same).
  */
 size_t sd2_paged_attn_workspace_bytes(const sd2_paged_kv* kv, const sd2_paged_rows* rows, int32_t n_heads,
                                       int32_t max_len);

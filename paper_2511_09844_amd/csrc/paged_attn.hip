@@ -70,6 +70,15 @@ __device__ __forceinline__ int wave_total(int v) {
     v = dpp_add<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
     return __builtin_amdgcn_readlane(v, 63);
 }
+// Maximum over a wave of values that are not negative.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_max(int v) {
+    return max(v, __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ int wave_most(int v) {
+    v = dpp_max<0x142, 0xa>(dpp_max<0x140, 0xf>(dpp_max<0x141, 0xf>(dpp_max<0x4E, 0xf>(dpp_max<0xB1, 0xf>(v)))));
+    return __builtin_amdgcn_readlane(dpp_max<0x143, 0xc>(v), 63);
+}
 
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
     const f2 v = {x, y};
@@ -717,7 +726,7 @@ constexpr int prompt_keys(int hd) { return hd == 128 ? 128 : 256; }
 struct PromptArgs {
     PagedAttnArgs a;
     int tiles;    // workgroups of a KV head and span
-    int nspan, keys;  // spans at most, keys of one
+    int nspan, least;  // spans at most, keys of one at least
     float* part;  // partials: [tile][KV head][span] of [QV][HD] sums, then of [QV] (maximum, sum)
     int64_t ml;   // floats of the first
 };
@@ -790,8 +799,25 @@ __device__ __forceinline__ Tile prompt_tile(const PagedRows& r, int G, int w) {
     return t;
 }
 
-// The keys of a tile that workgroup `span` of it reads: of `end` in all, `keys` to each, the same number
-// for all tiles, so that the workgroups' work is alike; the last span takes what is left.
+// Keys of a span, the same number for all tiles, so that the workgroups' work is alike: the longest sequence's in
+// nspan parts, which the lengths on the device say.  What the call expects may be far more: with spans of that
+// length 512 bf16 rows of 20000 positions, of 150000 that the table holds, took 459 us, not 186, and 64 fp32
+// rows of four sequences of 2000 527, not 109; with the length known, parts from the device cost up to 1.5 us.
+// For whole waves; mine: the tile's sequence.
+__device__ __forceinline__ int span_keys(const PromptArgs& d, int kt, const SeqRows& mine) {
+    if (d.nspan == 1) return 1 << 30;
+    int longest = seq_end(d.a, mine);
+    if (d.a.r.nseq > 1) {
+        for (int b0 = 0; b0 < d.a.r.nseq; b0 += 64) {
+            const int b = b0 + (threadIdx.x & 63);
+            if (b < d.a.r.nseq) longest = max(longest, seq_end(d.a, seq_rows(d.a.r, b)));
+        }
+        longest = wave_most(longest);
+    }
+    return max(((longest + d.nspan - 1) / d.nspan + kt - 1) / kt * kt, d.least);
+}
+// The keys of a tile that workgroup `span` of it reads: of `end` in all, `keys` to each; the last span takes
+// what is left.
 struct Span {
     int from, upto, live;  // spans that have keys
 };
@@ -827,8 +853,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
         if (lane < KT / 16 && key >> a.c.shift < a.c.max_pages) e = a.c.table[(int64_t)b * a.c.max_pages + (key >> a.c.shift)];
         return e;
     };
-    const int span0 = d.nspan > 1 ? span * d.keys : 0;  // (as prompt_span, for a span that has keys)
-    int entry = ask(span0 + 16 * lane), entry1 = ask(span0 + KT + 16 * lane);
+    // (Where keys are split, the first one's position follows from the lengths.)
+    int entry = -1, entry1 = -1;
+    if (d.nspan == 1) {
+        entry = ask(16 * lane);
+        entry1 = ask(KT + 16 * lane);
+    }
     const int wv = v0 + 32 * wave;  // the wave's first query vector
     u4 q[NS];
     const int v = wv + n, vc = min(v, nqv - 1);
@@ -838,7 +868,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
         for (int s = 0; s < NS; ++s) q[s] = *(const u4*)(p + 16 * s);
     }
     const int at0 = uniform(tl.rows.len) - nrows, pos = at0 + vc / G;
-    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, span);
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, span_keys(d, KT, tl.rows), span);
     if (span >= sp.live) return;
     const int end = sp.upto;
     const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 31, nqv - 1) / G + 1) : 0;
@@ -848,8 +878,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
     };
     auto named = [&](int e) { return (uint32_t)e < (uint32_t)a.c.n_pages ? e : -1; };
     const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
-    if (span0 + 16 * lane >= end) entry = -1;
-    if (span0 + KT + 16 * lane >= end) entry1 = -1;
+    if (d.nspan > 1) {
+        entry = look(t0 * KT);
+        entry1 = look((t0 + 1) * KT);
+    } else {
+        if (16 * lane >= end) entry = -1;
+        if (KT + 16 * lane >= end) entry1 = -1;
+    }
     const float c = a.scale != 0.f ? fabsf(a.scale) * kLog2e : 1.f;
     f16v o[NC];
     float m = -INFINITY, l = 0.f;
@@ -1139,7 +1174,7 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
     if (v0 >= nqv) return;
     const int at0 = uniform(tl.rows.len) - nrows;
     const int wv = v0 + 32 * wave;
-    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, span);
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, span_keys(d, KT, tl.rows), span);
     if (span >= sp.live) return;
     const int end = sp.upto;
     const int wfirst = at0 + wv / G, wend = wv < nqv ? min(end, at0 + min(wv + 31, nqv - 1) / G + 1) : 0;
@@ -1319,18 +1354,19 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
 }
 
 // The spans of k_pprompt's tiles joined: a thread per query vector and 4 columns.
-template <typename T, int HD, int QV>
+template <typename T, int HD, int QV, int KT>
 __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs d) {
     constexpr int PER = 256 / (HD / 4), NBK = QV / PER;
     const PagedAttnArgs& a = d.a;
     const int kvh = blockIdx.x / NBK % a.c.Hkv, tile = blockIdx.x / NBK / a.c.Hkv, G = a.H / a.c.Hkv;
     const Tile tl = prompt_tile<QV>(a.r, G, tile);
     if (tl.b < 0) return;
+    const int keys = span_keys(d, KT, tl.rows);  // (by whole waves)
     const int v0 = tl.v0, r0 = tl.rows.r0, nqv = tl.rows.n * G;
     const int i = blockIdx.x % NBK * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4, v = v0 + i;
     if (v >= nqv) return;
     const int at0 = tl.rows.len - tl.rows.n;
-    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, d.keys, 0);
+    const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, keys, 0);
     if (sp.live == 1) return;
     const int64_t at = ((int64_t)tile * a.c.Hkv + kvh) * d.nspan * QV + i;
     const f4 o = join_parts(d.part + at * HD + c, d.part + d.ml + at * 2, sp.live, QV, HD);
@@ -1343,7 +1379,7 @@ constexpr int kPromptQv = sizeof(T) == 2 ? 32 * kPromptWaves : 128;
 
 struct PromptPlan {
     int64_t tiles;
-    int nspan, keys;
+    int nspan, least;
     int64_t ml;
     size_t bytes;
 };
@@ -1363,9 +1399,8 @@ PromptPlan prompt_plan(const PagedView& c, const PagedRows& r, int H, bool bf16,
     int64_t want = std::max<int64_t>(1, (bf16 && c.hd > 32 ? 512 : 1024) / groups);
     const size_t per = (size_t)groups * QV * (c.hd + 2) * sizeof(float);
     if (want > 1) want = std::min<int64_t>(want, std::max<size_t>(1, bytes / per));
-    const int64_t keys = std::max(least, ((max_len + want - 1) / want + kt - 1) / kt * kt);
-    p.nspan = (int)((max_len + keys - 1) / keys);
-    p.keys = (int)std::min<int64_t>(keys, 1 << 30);
+    p.nspan = (int)std::min(want, (max_len + least - 1) / least);
+    p.least = (int)least;
     if (p.nspan > 1) {
         p.ml = groups * p.nspan * QV * c.hd;
         p.bytes = per * p.nspan;
@@ -1378,12 +1413,12 @@ hipError_t prompt(hipStream_t s, const PagedAttnArgs& a, const PromptPlan& p, fl
     const int64_t groups = p.tiles * a.c.Hkv, nj = kPromptQv<T> * (HD / 4) / 256;
     // (a launch has fewer than 2^32 threads)
     if (groups * std::max<int64_t>(p.nspan, nj) > UINT32_MAX / (64 * kPromptWaves)) return hipErrorInvalidValue;
-    const PromptArgs d{a, (int)p.tiles, p.nspan, p.keys, ws, p.ml};
+    const PromptArgs d{a, (int)p.tiles, p.nspan, p.least, ws, p.ml};
     hipError_t err;
     if constexpr (sizeof(T) == 2) err = launch(k_pprompt_bf16<HD>, dim3((unsigned)(groups * p.nspan)), dim3(64 * kPromptWaves), s, d);
     else err = launch(k_pprompt_f32<HD>, dim3((unsigned)(groups * p.nspan)), dim3(256), s, d);
     if (err != hipSuccess || p.nspan == 1) return err;
-    return launch(k_prompt_join<T, HD, kPromptQv<T>>, dim3((unsigned)(groups * nj)), dim3(256), s, d);
+    return launch(k_prompt_join<T, HD, kPromptQv<T>, sizeof(T) == 2 ? prompt_keys(HD) : 32>, dim3((unsigned)(groups * nj)), dim3(256), s, d);
 }
 
 // Whether a call goes to k_pprompt: by the query vectors of a sequence and KV head that share keys.  k_pdecode reads
