@@ -139,6 +139,19 @@ def test_more_sequences_than_lanes(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("longest", [3, 69])
+def test_split_keys_of_more_sequences_than_lanes(dtype, longest):
+    """70 sequences, one far longer than the others, whose rows are split over its keys."""
+    lens = [5 + b for b in range(70)]
+    rows = [b % 3 for b in range(70)]
+    lens[longest], rows[longest] = 1500, 300
+    cache = make_cache(lens, dtype, 1, 64, 16, extra_entries=60)
+    q = queries(sum(rows), 2, 64, dtype)
+    check(cache, q, lens, rows, True, max_rows=300)
+    check(cache, q, lens, rows, True, max_len=1500)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("rows", [1, 20, 130])
 @pytest.mark.parametrize("max_len", [1, 700, 4000])
 def test_the_expected_length_decides_nothing_but_the_split(dtype, rows, max_len):
