@@ -104,7 +104,7 @@ struct Workspace {
     float* cond_b;          // conditional bias: [2 max_batch][F_D] one layer's bias of the drafter rows
     // paged caches (sd2_create_paged; else null)
     int32_t *pg_table, *pg_refs;  // [max_batch][max_pages], [n_pages]
-    int32_t *pg_first, *pg_last, *pg_granted, *pg_trim;  // [max_batch] arguments of the page calls
+    int32_t *pg_first, *pg_last, *pg_keep, *pg_granted, *pg_trim;  // [max_batch] arguments of the page calls
     int32_t* steer_out;     // [max_batch] row that a sequence's steering goes to: its own, or -1 (keep the old one)
     void* pg_ws;
 };

@@ -317,6 +317,7 @@ size_t carve(const sd2_config& c, char* base, Workspace* ws, ModelDev* mv, Model
         w.pg_refs = p.refs = cv.take<int32_t>(p.n_pages);
         w.pg_first = cv.take<int32_t>(B);
         w.pg_last = cv.take<int32_t>(B);
+        w.pg_keep = cv.take<int32_t>(B);
         w.pg_granted = cv.take<int32_t>(B);
         w.pg_trim = cv.take<int32_t>(B);
         w.steer_out = cv.take<int32_t>(B);

@@ -613,14 +613,17 @@ hipError_t launch_prefill_pages(hipStream_t s, Engine& e, int batch, const int32
                                                    e.ws.pg_granted, e.ws.pg_ws);
 }
 
-// Positions min(len_v, len_d) .. t + k - 1 are what a round writes; finished sequences give up their pages.
+// Positions min(len_v, len_d) .. t + k - 1 are what a round writes, in one model or both; what either holds already,
+// up to max(len_v, len_d), is kept when a shared page is copied (after a round that accepted every draft the
+// verifier holds a position that the drafter has yet to write).  Finished sequences give up their pages.
 __global__ void k_round_pages(int batch, int k, int cap, const int32_t* t, const int32_t* len_v, const int32_t* len_d,
-                              const int32_t* done, int32_t* first, int32_t* last, int32_t* trim) {
+                              const int32_t* done, int32_t* first, int32_t* last, int32_t* keep, int32_t* trim) {
     const int b = threadIdx.x;
     if (b >= batch) return;
     const bool over = done[b] == 1;
     first[b] = over ? 0 : min(len_v[b], len_d[b]);
     last[b] = over ? 0 : min(t[b] + k, cap);
+    keep[b] = max(len_v[b], len_d[b]);
     trim[b] = over ? 0 : -1;
 }
 // done = 2: no pages for this round; such a sequence keeps its steering and is tried again next time.
@@ -635,10 +638,11 @@ hipError_t launch_round_pages(hipStream_t s, Engine& e) {
     static_assert(SD2_PAGED_MAX_SEQS >= 256, "a handle's sequences fit");
     Workspace& w = e.ws;
     prof_begin(&e, kProfOther, 0.0);
-    k_round_pages<<<1, 256, 0, s>>>(e.batch, e.cfg.k, e.cap, w.t, w.len_v, w.len_d, w.done, w.pg_first, w.pg_last, w.pg_trim);
+    k_round_pages<<<1, 256, 0, s>>>(e.batch, e.cfg.k, e.cap, w.t, w.len_v, w.len_d, w.done, w.pg_first, w.pg_last, w.pg_keep,
+                                     w.pg_trim);
     hipError_t err = pages_trim(s, e.pages, e.batch, w.pg_trim);
     if (err == hipSuccess)
-        err = pages_reserve(s, e.pages, e.batch, w.pg_first, w.pg_last, nullptr, w.pg_granted, w.pg_ws);
+        err = pages_reserve(s, e.pages, e.batch, w.pg_first, w.pg_last, w.pg_keep, w.pg_granted, w.pg_ws);
     if (err == hipSuccess) k_round_stall<<<1, 256, 0, s>>>(e.batch, w.pg_last, w.pg_granted, w.done, w.steer_out);
     prof_end(&e);
     return err;

@@ -1,0 +1,91 @@
+"""Paged handles where sequences share pages that a round is about to write, and where the pool is short: against
+contiguous handles of the same history.
+
+Both hold the same fp32 rows and differ in how attention sums them and in how many rows a projection takes at
+once, so logits of equal histories agree to 1e-4 (fp32 weights) and 1e-3 (bf16, as the plane projections'
+tests derive)."""
+import numpy as np
+import pytest
+import torch
+
+import sd2_inputs as si
+from sd2_inputs.configs import Dims, Workload
+from paper_2511_09844_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TOL = {"f32": 1e-4, "bf16": 1e-3}
+BF16 = Workload(name="paged-handles", verifier=Dims(1, 768, 12, 4, 1280, 1008, 5e5),
+                drafter=Dims(1, 512, 16, 4, 768, 1008, 5e5), dtype="bf16", k=4, batch=4, prompt=(40, 40), new_tokens=30,
+                temperature=0.0, seed=5)
+F32 = si.TINY.with_(name="paged-handles", batch=4, prompt=(40, 40), new_tokens=30, temperature=0.0, seed=5)
+
+
+class Model:
+    """Weights of a workload on the GPU, for several handles."""
+
+    def __init__(self, wl):
+        import gpu_harness
+        self.wl = wl
+        self.dv, self.dd = gpu_harness.device_model(wl, 0), gpu_harness.device_model(wl, 1)
+        self.ws = B.to_device(si.steer_weights(wl))
+
+    def engine(self, paging=None):
+        return B.Engine(B.config_of(self.wl), self.dv, self.dd, self.ws, paging=paging)
+
+
+def prompts(n, length, seed=3):
+    return torch.randint(0, 1000, (n, length), generator=torch.Generator().manual_seed(seed), dtype=torch.int32)
+
+
+def prefill(eng, toks, lens=None):
+    lens = [toks.shape[1]] * toks.shape[0] if lens is None else lens
+    eng.prefill(toks.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), toks.shape[1])
+
+
+def close(a, b, tol):
+    for name in (B.DBG_LOGITS_V, B.DBG_LOGITS_D, B.DBG_STEER):
+        err = np.abs(a.debug(name) - b.debug(name)).max(axis=tuple(range(1, a.debug(name).ndim)))
+        assert (err <= tol).all(), (name, err)
+
+
+def decisions(accepted, k, seed):
+    """What a round is forced to: drafts, how many of them are accepted, the token after."""
+    g = torch.Generator().manual_seed(seed)
+    rows = torch.randint(0, 1000, (len(accepted), k + 2), generator=g, dtype=torch.int32)
+    rows[:, k] = torch.tensor(accepted, dtype=torch.int32)
+    return rows
+
+
+def advance(eng, forced):
+    out, cnt = eng.round(forced.cuda())
+    return out.cpu().tolist(), cnt.cpu().tolist()
+
+
+@pytest.mark.parametrize("wl", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("length,slot", [(13, 0), (20, 7), (12, 15)], ids=["first", "middle", "last"])
+@pytest.mark.parametrize("accepted", [4, 3, 0])
+def test_fork_after_a_round(wl, length, slot, accepted):
+    """With every draft accepted the verifier holds one position more than the drafter, on a page that the fork
+    shares: that row belongs to what is copied, whatever slot it lies in."""
+    m = Model(wl.with_(prompt=(length, length)))
+    plain, paged = m.engine(), m.engine(paging=(16, 40))
+    toks = prompts(1, length)
+    prefill(plain, toks.expand(4, -1).contiguous())
+    prefill(paged, toks)
+    first = decisions([accepted], wl.k, 1)
+    advance(plain, first.expand(4, -1).contiguous())
+    advance(paged, first)
+    state = paged.state()[0]
+    assert state["len_v"] == length + accepted and state["len_d"] == state["len_v"] - (accepted == wl.k)
+    if accepted == wl.k:
+        assert state["len_d"] % 16 == slot
+    paged.fork(0)
+    paged.fork(1, 2)
+    for r in range(3):
+        forced = decisions([[4, 0, 2, 4], [1, 4, 4, 0], [2, 2, 0, 1]][r], wl.k, 10 + r)
+        assert advance(plain, forced) == advance(paged, forced)
+        close(plain, paged, TOL[wl.dtype])
+        assert plain.state() == paged.state()
+        refs, table = paged.debug(B.DBG_REFS), paged.debug(B.DBG_TABLE)
+        assert all((table == p).sum() == n for p, n in enumerate(refs))
