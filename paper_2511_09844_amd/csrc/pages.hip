@@ -92,18 +92,19 @@ struct BookArgs {
 };
 
 // Sum of x over the threads before this one; total: over all.
-__device__ int block_before(int x, int* red, int& total) {
+template <typename T>
+__device__ T block_before(T x, T* red, T& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int inc = x;
+    T inc = x;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-        const int y = __shfl_up(inc, d, 64);
+        const T y = __shfl_up(inc, d, 64);
         if (lane >= d) inc += y;
     }
     __syncthreads();
     if (lane == 63) red[wave] = inc;
     __syncthreads();
-    int before = 0;
+    T before = 0;
     total = 0;
 #pragma unroll
     for (int w = 0; w < kBookWaves; ++w) {
@@ -131,8 +132,12 @@ __device__ __forceinline__ bool asks(const BookArgs& a, int b, int j, int& page)
     return page < 0 || a.refs[page] > 1;
 }
 
+// What all sequences together ask for is counted in 64 bits: up to 4096 times 2^26 entries.  Pages are at most 2^24, so
+// a sequence that has more than kBehind entries before it gets none, however many they are.
+constexpr int kBehind = 1 << 30;
 __global__ __launch_bounds__(kBookThreads) void k_pages_reserve(BookArgs a) {
     __shared__ int red[kBookWaves];
+    __shared__ int64_t sums[kBookWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int b = wave; b < a.nseq; b += kBookWaves) {
         const Want w = window(a, b);
@@ -146,14 +151,15 @@ __global__ __launch_bounds__(kBookThreads) void k_pages_reserve(BookArgs a) {
         if (lane == 0) a.l.need[b] = n;
     }
     __syncthreads();
-    int want = 0;
+    int64_t asked = 0;
     for (int b0 = 0; b0 < a.nseq; b0 += kBookThreads) {
         const int b = b0 + tid;
-        int n;
-        const int before = want + block_before(b < a.nseq ? a.l.need[b] : 0, red, n);
-        if (b < a.nseq) a.l.need[b] = before;
-        want += n;
+        int64_t n;
+        const int64_t before = asked + block_before<int64_t>(b < a.nseq ? a.l.need[b] : 0, sums, n);
+        if (b < a.nseq) a.l.need[b] = min(before, (int64_t)kBehind);
+        asked += n;
     }
+    const int want = min(asked, (int64_t)a.n_pages);
     // the first `want` free pages, ascending
     int found = 0;
     for (int p0 = 0; p0 < a.n_pages && found < want; p0 += 4 * kBookThreads) {
@@ -216,7 +222,7 @@ __global__ __launch_bounds__(kBookThreads) void k_pages_compact(BookArgs a) {
         const bool used = p < a.n_pages && a.refs[p] > 0;
         const bool s = used && p >= live, d = !used && p < live;
         int ts, td;
-        const int is = ns + block_before(s, red, ts), id = nd + block_before(d, red, td);
+        const int is = ns + block_before<int>(s, red, ts), id = nd + block_before<int>(d, red, td);
         if (s) a.l.src[is] = p;
         else if (p >= live && p < a.n_pages) a.l.name[p] = p;  // (an entry that names a free page keeps it)
         if (d) a.l.dst[id] = p;
