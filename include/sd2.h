@@ -187,10 +187,10 @@ sd2_status sd2_create_mlp(const sd2_config* cfg, const sd2_weights* verifier, co
  * pages in use together.  cfg->steering must be SD2_STEER_INPUT or SD2_STEER_NONE; rounds run one kernel per
  * operation; everything else is as sd2_create, with sd2_create_paged_bytes for sd2_workspace_bytes.
  * sd2_prefill returns SD2_ERR_CAPACITY when batch * ceil((max_prompt - 1) / page_size) exceeds n_pages.
- * A sequence that the pool cannot give the pages of a round sits it out: its out_counts entry is 0, its
- * state is kept (SD2_DBG_STATE: done = 2), and it goes on in a later round that finds pages, which finished
- * sequences have left; when none can go on, the caller has to release one.  sd2_train_loss returns
- * SD2_ERR_UNSUPPORTED.
+ * A sequence that the pool cannot give all the pages of a round takes none and sits it out: its out_counts
+ * entry is 0, its state is kept (SD2_DBG_STATE: done = 2), and it goes on in a later round that finds pages,
+ * which finished sequences have left; when none can go on, the caller has to release one.  sd2_train_loss
+ * returns SD2_ERR_UNSUPPORTED.
  */
 typedef struct {
     int32_t page_size;  /* 16, 32, 64, 128, 256, 512 or 1024 */

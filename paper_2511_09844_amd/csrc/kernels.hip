@@ -642,7 +642,7 @@ hipError_t launch_round_pages(hipStream_t s, Engine& e) {
                                      w.pg_trim);
     hipError_t err = pages_trim(s, e.pages, e.batch, w.pg_trim);
     if (err == hipSuccess)
-        err = pages_reserve(s, e.pages, e.batch, w.pg_first, w.pg_last, w.pg_keep, w.pg_granted, w.pg_ws);
+        err = pages_reserve(s, e.pages, e.batch, w.pg_first, w.pg_last, w.pg_keep, w.pg_granted, w.pg_ws, true);
     if (err == hipSuccess) k_round_stall<<<1, 256, 0, s>>>(e.batch, w.pg_last, w.pg_granted, w.done, w.steer_out);
     prof_end(&e);
     return err;

@@ -51,8 +51,10 @@ hipError_t paged_append(hipStream_t s, const PagedView& c, const PagedRows& r, c
 
 bool pages_ok(const sd2_pages* p);
 size_t pages_bytes(const sd2_pages& p);
+// whole: a sequence that the pool cannot give every page it asks for gets none of them, and those behind it are
+// served all the same.
 hipError_t pages_reserve(hipStream_t s, const sd2_pages& p, int nseq, const int32_t* first, const int32_t* last,
-                         const int32_t* keep, int32_t* granted, void* ws);
+                         const int32_t* keep, int32_t* granted, void* ws, bool whole = false);
 hipError_t pages_fork(hipStream_t s, const sd2_pages& p, int n, const int32_t* src, const int32_t* dst);
 hipError_t pages_trim(hipStream_t s, const sd2_pages& p, int nseq, const int32_t* lens);
 hipError_t pages_compact(hipStream_t s, const sd2_pages& p, int32_t* live, void* ws);

@@ -88,6 +88,7 @@ struct BookArgs {
     int32_t n_pages, max_pages, shift, nseq, max_seqs;
     const int32_t *first, *last, *keep;
     int32_t *granted, *live;
+    bool whole;  // reserve: a sequence gets all it asks for, or nothing
     PageList l;
 };
 
@@ -138,6 +139,7 @@ constexpr int kBehind = 1 << 30;
 __global__ __launch_bounds__(kBookThreads) void k_pages_reserve(BookArgs a) {
     __shared__ int red[kBookWaves];
     __shared__ int64_t sums[kBookWaves];
+    __shared__ int taken;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int b = wave; b < a.nseq; b += kBookWaves) {
         const Want w = window(a, b);
@@ -180,6 +182,28 @@ __global__ __launch_bounds__(kBookThreads) void k_pages_reserve(BookArgs a) {
     }
     found = min(found, want);
     __syncthreads();
+    if (a.whole && found < asked) {
+        // in the sequences' order, those that fit into what is left, the others passed over
+        if (wave == 0) {
+            int given = 0;
+            for (int b0 = 0; b0 < a.nseq; b0 += 64) {
+                const int b = b0 + lane;
+                const int64_t behind = b + 1 < a.nseq ? a.l.need[b + 1] : min(asked, (int64_t)kBehind);
+                const int mine = b < a.nseq ? (int)behind - a.l.need[b] : 0;
+                int at = kBehind;
+                for (int l = 0; l < 64; ++l) {
+                    const int n = __builtin_amdgcn_readlane(mine, l);
+                    if (n > found - given) continue;
+                    if (lane == l) at = given;
+                    given += n;
+                }
+                if (b < a.nseq) a.l.need[b] = at;
+            }
+            if (lane == 0) taken = given;
+        }
+        __syncthreads();
+        found = taken;
+    }
     for (int b = wave; b < a.nseq; b += kBookWaves) {
         const Want w = window(a, b);
         const int keep = a.keep ? max(a.keep[b], 0) : w.from;
@@ -367,9 +391,9 @@ bool pages_ok(const sd2_pages* p) {
 size_t pages_bytes(const sd2_pages& p) { return list_carve(p, nullptr, nullptr); }
 
 hipError_t pages_reserve(hipStream_t s, const sd2_pages& p, int nseq, const int32_t* first, const int32_t* last,
-                         const int32_t* keep, int32_t* granted, void* ws) {
+                         const int32_t* keep, int32_t* granted, void* ws, bool whole) {
     BookArgs a = book(p, ws);
-    a.nseq = nseq; a.first = first; a.last = last; a.keep = keep; a.granted = granted;
+    a.nseq = nseq; a.first = first; a.last = last; a.keep = keep; a.granted = granted; a.whole = whole;
     const hipError_t err = launch(k_pages_reserve, dim3(1), dim3(kBookThreads), s, a);
     return err != hipSuccess ? err : copy_listed(s, p, a.l, false);
 }

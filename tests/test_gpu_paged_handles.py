@@ -89,3 +89,40 @@ def test_fork_after_a_round(wl, length, slot, accepted):
         assert plain.state() == paged.state()
         refs, table = paged.debug(B.DBG_REFS), paged.debug(B.DBG_TABLE)
         assert all((table == p).sum() == n for p, n in enumerate(refs))
+
+
+def generate(eng, n, limit=300):
+    """Tokens per sequence until all are done, and how often each sat out a round (which changes nothing of it)."""
+    got, waited = [[] for _ in range(n)], [0] * n
+    for _ in range(limit):
+        before, steer = eng.state(), eng.debug(B.DBG_STEER)
+        out, cnt = eng.round()
+        out, cnt, after, kept = out.cpu(), cnt.cpu(), eng.state(), eng.debug(B.DBG_STEER)
+        for b in range(n):
+            if after[b]["done"] == 2:
+                waited[b] += 1
+                assert int(cnt[b]) == 0 and (out[b] == -1).all() and (kept[b] == steer[b]).all()
+                assert {**after[b], "done": 0} == {**before[b], "done": 0}
+            got[b] += out[b, : int(cnt[b])].tolist()
+        if all(s["done"] == 1 for s in after):
+            return got, waited
+    raise AssertionError("sequences that cannot go on")
+
+
+@pytest.mark.parametrize("wl", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[17, 18], [18, 17], [17, 18, 18], [18, 17, 18], [17] + 19 * [18], 69 * [18] + [17]], ids=len)
+def test_a_sequence_takes_no_pages_of_a_round_it_cannot_run(wl, lens):
+    """One free page.  A block of 17 positions that begins a page takes two of 16, any other here one: a sequence that
+    needs one goes on, whichever comes first, and the others when it has finished."""
+    n = len(lens)
+    wl = wl.with_(k=16, new_tokens=10, batch=n, prompt=(17, 18))
+    m = Model(wl)
+    plain, paged = m.engine(), m.engine(paging=(16, 2 * n))
+    toks = prompts(n, 18)
+    prefill(plain, toks, lens)
+    want, _ = generate(plain, n)
+    prefill(paged, toks, lens)
+    assert (paged.debug(B.DBG_REFS) == 0).sum() == 1
+    got, waited = generate(paged, n)
+    assert got == want
+    assert waited[lens.index(18)] == 0 and sum(w > 0 for w in waited) == n - 1
