@@ -391,7 +391,9 @@ sd2_status sd2_paged_append(const sd2_paged_kv* kv, const sd2_paged_rows* rows, 
  * sums in fp32, the softmax's weights rounded to bf16 for their product with v; fp32: fp32 throughout.
  * Memory behind a sequence's last position, and pages it does not name, are not read, or do not count,
  * whatever they hold; infinities and NaN of a position reach the rows that read it, and no others.
- * The rows of a sequence times n_heads / n_kv_heads are at most 2^30.
+ * The rows of a sequence times n_heads / n_kv_heads are at most 2^30.  Sizes that together make a launch of 2^32
+ * threads or more are refused (workspace 0): that takes beyond 8 million workgroups, one for each sequence, KV head
+ * and 16 query vectors at least.
  * max_len: the largest length expected, 1..max_pages * page_size (it decides into how many parts the work may be
  * split, and the workspace; a longer sequence is computed all the same).
  */

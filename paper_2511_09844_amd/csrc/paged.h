@@ -39,8 +39,8 @@ struct PagedAttnArgs {
     float scale;
 };
 
-// Workspace of a call, and the call.  max_len: the largest length expected.  bf16: of q, the cache
-// and out (else fp32).
+// Workspace of a call (0: more than can be launched), and the call.  max_len: the largest length expected.  bf16: of
+// q, the cache and out (else fp32).
 size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len);
 // With less than that the keys are split less.
 hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t ws_bytes);

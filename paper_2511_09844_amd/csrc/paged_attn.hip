@@ -1411,8 +1411,6 @@ PromptPlan prompt_plan(const PagedView& c, const PagedRows& r, int H, bool bf16,
 template <typename T, int HD>
 hipError_t prompt(hipStream_t s, const PagedAttnArgs& a, const PromptPlan& p, float* ws) {
     const int64_t groups = p.tiles * a.c.Hkv, nj = kPromptQv<T> * (HD / 4) / 256;
-    // (a launch has fewer than 2^32 threads)
-    if (groups * std::max<int64_t>(p.nspan, nj) > UINT32_MAX / (64 * kPromptWaves)) return hipErrorInvalidValue;
     const PromptArgs d{a, (int)p.tiles, p.nspan, p.least, ws, p.ml};
     hipError_t err;
     if constexpr (sizeof(T) == 2) err = launch(k_pprompt_bf16<HD>, dim3((unsigned)(groups * p.nspan)), dim3(64 * kPromptWaves), s, d);
@@ -1460,14 +1458,26 @@ DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16,
     return p;
 }
 
+// Workgroups of k_pjoin for a group of 16 nt query vectors.
+constexpr int join_blocks(int hd, int nt) { return (16 * nt + 1024 / hd - 1) / (1024 / hd); }
+
+// Whether both launches of a plan have fewer than 2^32 threads, which is what one may have.
+bool fits(const PagedView& c, const PagedRows&, bool bf16, const PromptPlan& p) {
+    const int64_t groups = p.tiles * c.Hkv, nj = (bf16 ? kPromptQv<uint16_t> : kPromptQv<float>) * (c.hd / 4) / 256;
+    return std::max(groups * p.nspan * (bf16 ? 64 * kPromptWaves : 256), p.nspan > 1 ? groups * nj * 256 : 0) <= UINT32_MAX;
+}
+bool fits(const PagedView& c, const PagedRows& r, bool, const DecodePlan& p) {
+    const int64_t per = ((int64_t)p.units * c.Hkv + 7) / 8 * 8, join = p.target ? (int64_t)r.nseq * c.Hkv * join_blocks(c.hd, p.nt) : 0;
+    return std::max(per, join) * p.ncg <= UINT32_MAX / 256;
+}
+
 template <typename T, int HD, int NT>
 hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p, float* ws) {
     const DecodeArgs d{a, p.ncg, p.target, kDecodeWaves * kBlockKeys<T>, p.units, ws, p.ml};
     const int64_t per = ((int64_t)p.units * a.c.Hkv + 7) / 8 * 8;
-    if (per * p.ncg > UINT32_MAX / (64 * kDecodeWaves)) return hipErrorInvalidValue;  // (a launch has fewer than 2^32 threads)
     const hipError_t err = launch(k_pdecode<T, HD, NT>, dim3((unsigned)(per * p.ncg)), dim3(64 * kDecodeWaves), s, d);
     if (err != hipSuccess || !p.target) return err;
-    constexpr int q = 256 / (HD / 4), nb = (16 * NT + q - 1) / q;
+    constexpr int nb = join_blocks(HD, NT);
     return launch(k_pjoin<T, HD, NT>, dim3((unsigned)(a.r.nseq * a.c.Hkv * p.ncg * nb)), dim3(256), s, d);
 }
 
@@ -1481,9 +1491,12 @@ hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float*
 }  // namespace
 
 size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
-    if (many_rows(c, r, H, bf16)) return std::max<size_t>(prompt_plan(c, r, H, bf16, max_len, SIZE_MAX).bytes, 256);
+    if (many_rows(c, r, H, bf16)) {
+        const PromptPlan p = prompt_plan(c, r, H, bf16, max_len, SIZE_MAX);
+        return fits(c, r, bf16, p) ? std::max<size_t>(p.bytes, 256) : 0;
+    }
     const DecodePlan p = decode_plan(c, r, H, bf16, max_len, SIZE_MAX);
-    return std::max<size_t>(p.bytes, 256);
+    return fits(c, r, bf16, p) ? std::max<size_t>(p.bytes, 256) : 0;
 }
 
 hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t ws_bytes) {

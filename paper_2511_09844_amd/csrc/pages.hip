@@ -571,8 +571,8 @@ sd2_status sd2_paged_attn(const sd2_paged_kv* kv, const sd2_paged_rows* rows, co
     if (!a.r.nseq || !a.r.total_rows) return SD2_OK;
     const int64_t width = (int64_t)n_heads * a.c.hd;
     if (!strided(q, q_stride, width, size) || !strided(out, out_stride, width, size)) return SD2_ERR_INVALID_ARG;
-    if (!aligned(workspace, 256) || workspace_bytes < paged_attn_bytes(a.c, a.r, n_heads, size == 2, max_len))
-        return SD2_ERR_INVALID_ARG;
+    const size_t need = paged_attn_bytes(a.c, a.r, n_heads, size == 2, max_len);
+    if (!need || !aligned(workspace, 256) || workspace_bytes < need) return SD2_ERR_INVALID_ARG;
     const sd2_status st = device_ok();
     if (st != SD2_OK) return st;
     a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.H = n_heads; a.scale = scale;
