@@ -385,7 +385,8 @@ sd2_status sd2_paged_append(const sd2_paged_kv* kv, const sd2_paged_rows* rows, 
 /*
  * Causal grouped-query attention of the rows over their sequences' pages: row at position p, head h:
  *   out = sum_j softmax_j(scale * q . k_j) v_j   over the positions j <= p that have a page,
- * KV head h / (n_heads / n_kv_heads); zeros when there is none (a negative position, no page).
+ * KV head h / (n_heads / n_kv_heads); zeros when there is none (a negative position, no page), NaN where all
+ * their scores are -infinity.
  * q, out: device [total_rows][n_heads][head_dim], q_stride and out_stride elements from one row to the next
  * (whole 16-byte units); n_heads a multiple of n_kv_heads, up to 1024.  bf16: scores, softmax and
  * sums in fp32, the softmax's weights rounded to bf16 for their product with v; fp32: fp32 throughout.

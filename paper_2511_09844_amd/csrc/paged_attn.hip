@@ -116,6 +116,24 @@ __device__ __forceinline__ void put(const PagedAttnArgs& a, int row, int c, cons
     }
 }
 
+// What a row's sums are multiplied by.  A sum of weights of 0 is that of a row that reads nothing, which gives zeros, or
+// of one whose every score is -inf, which gives NaN; only such waves look which it is, in the table: at the first
+// position that has a page, up to `upto`.  For whole waves, of one sequence.
+__device__ __forceinline__ float inverse(const PagedView& c, int b, float sum, int pos, int upto) {
+    const float inv = 1.f / sum;
+    if (!__any(!(sum > 0.f))) return inv;
+    const int lane = threadIdx.x & 63, n = min((upto >> c.shift) + 1, c.max_pages);
+    int first = INT32_MAX;
+    for (int j = 0; j < n; j += 64) {
+        const uint64_t there = __ballot(j + lane < n && paged_page(c, b, j + lane) >= 0);
+        if (there) {
+            first = (j + (int)__builtin_ctzll(there)) << c.shift;
+            break;
+        }
+    }
+    return sum > 0.f ? inv : pos < first ? 0.f : NAN;
+}
+
 // The keys a workgroup of k_pdecode takes at a time, 16 or 32 per wave.
 template <typename T>
 constexpr int kBlockKeys = sizeof(T) == 2 ? 32 : 16;
@@ -617,7 +635,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int v = v0 + 16 * j + n;
-        const float inv = !whole_seq ? 1.f : lt[j] > 0.f ? 1.f / lt[j] : 0.f;
+        const float inv = !whole_seq ? 1.f : inverse(a.c, b, lt[j], pos[j], len - nrows + min(v0 + QV - 1, nqv - 1) / G);
 #pragma unroll
         for (int u = 0; u < B::VU; ++u) {
             float y[4 * B::VW];
@@ -641,9 +659,10 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     }
 }
 
-// `live` partials, `next` query vectors apart, joined: 4 columns of one.
-__device__ __forceinline__ f4 join_parts(const float* po, const float* pm, int live, int64_t next, int hd) {
-    float m = -INFINITY, l = 0.f;
+// `live` partials, `next` query vectors apart, joined: 4 columns of one, and its sum of weights.
+__device__ __forceinline__ f4 join_parts(const float* po, const float* pm, int live, int64_t next, int hd, float& l) {
+    float m = -INFINITY;
+    l = 0.f;
     f4 o = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < live; s0 += 8) {
         f2 ml[8];
@@ -670,7 +689,7 @@ __device__ __forceinline__ f4 join_parts(const float* po, const float* pm, int l
             for (int i = 0; i < 4; ++i) o[i] += on ? w * x[s][i] : 0.f;
         }
     }
-    return o * (l > 0.f ? 1.f / l : 0.f);
+    return o;
 }
 
 // The units of a sequence joined: a thread per query vector and 4 columns.
@@ -684,15 +703,19 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
     const Units un = units_of<T>(d, -1, b);
     const int live = un.count;
     if (live == 1) return;
-    const int r0 = un.rows.r0, nqv = un.rows.n * G, v0 = cg * QV, v = v0 + i;
-    if (i >= QV || v >= nqv) return;
+    const int r0 = un.rows.r0, nqv = un.rows.n * G, v0 = cg * QV, n = min(QV, nqv - v0);
+    if (!__any(i < n)) return;
+    const int at = min(i, n - 1), v = v0 + at;  // (lanes without a query vector go along with the last one)
     // from one unit's partials to the next
     const int64_t slot = ((int64_t)un.first * a.c.Hkv + kvh) * d.ncg + cg, next = (int64_t)a.c.Hkv * d.ncg * QV;
-    const float* po = d.part + (slot * QV + i) * HD + c;
-    const float* pm = d.part + d.ml + (slot * QV + i) * 2;
-    const f4 o = join_parts(po, pm, live, next, HD);
+    const float* po = d.part + (slot * QV + at) * HD + c;
+    const float* pm = d.part + d.ml + (slot * QV + at) * 2;
+    float sum;
+    const f4 parts = join_parts(po, pm, live, next, HD, sum);
+    const int at0 = un.rows.len - un.rows.n;
+    const f4 o = parts * inverse(a.c, b, sum, at0 + v / G, at0 + (v0 + n - 1) / G);
     const float y[4] = {o[0], o[1], o[2], o[3]};
-    put<T, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
+    if (i < n) put<T, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1135,7 +1158,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
     }
     // the wave's rows through LDS (its own part of what K and V were in, which nobody uses any more), so that
     // whole rows are stored: 8 bytes a lane to 64 rows took 2 to 4 us
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float inv = inverse(a.c, b, sum, pos, at0 + min(wv + 31, nqv - 1) / G);
     constexpr int OB = RB + 16;
     char* const os = (late ? vs[0] : ks[0]) + wave % (NW / 2) * 32 * OB;
     static_assert(NW / 2 * 32 * OB <= 2 * KT * RB, "the waves' rows fit");
@@ -1332,7 +1355,7 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
     };
     pass(std::false_type{}, t0);
     if (__syncthreads_or(todo != INT32_MAX)) pass(std::true_type{}, max(t0, (at0 + v0 / G) / KT));
-    const float sum = half_sum(l), inv = sp.live > 1 ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
+    const float sum = half_sum(l), inv = sp.live > 1 ? 1.f : inverse(a.c, b, sum, pos, at0 + min(wv + 31, nqv - 1) / G);
     if (v >= nqv) return;
     const int64_t at = (((int64_t)tile * a.c.Hkv + kvh) * d.nspan + span) * QV + wv - v0 + n;
 #pragma unroll
@@ -1363,15 +1386,18 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs d) {
     if (tl.b < 0) return;
     const int keys = span_keys(d, KT, tl.rows);  // (by whole waves)
     const int v0 = tl.v0, r0 = tl.rows.r0, nqv = tl.rows.n * G;
-    const int i = blockIdx.x % NBK * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4, v = v0 + i;
-    if (v >= nqv) return;
+    const int i = blockIdx.x % NBK * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4;
+    if (!__any(v0 + i < nqv)) return;
+    const int v = min(v0 + i, nqv - 1);  // (as in k_pjoin)
     const int at0 = tl.rows.len - tl.rows.n;
     const Span sp = prompt_span(max(min(at0 + min(v0 + QV - 1, nqv - 1) / G + 1, (int64_t)a.c.max_pages << a.c.shift), 0), d.nspan, keys, 0);
     if (sp.live == 1) return;
-    const int64_t at = ((int64_t)tile * a.c.Hkv + kvh) * d.nspan * QV + i;
-    const f4 o = join_parts(d.part + at * HD + c, d.part + d.ml + at * 2, sp.live, QV, HD);
+    const int64_t at = ((int64_t)tile * a.c.Hkv + kvh) * d.nspan * QV + v - v0;
+    float sum;
+    const f4 parts = join_parts(d.part + at * HD + c, d.part + d.ml + at * 2, sp.live, QV, HD, sum);
+    const f4 o = parts * inverse(a.c, tl.b, sum, at0 + v / G, at0 + min(v0 + QV - 1, nqv - 1) / G);
     const float y[4] = {o[0], o[1], o[2], o[3]};
-    put<T, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
+    if (v0 + i < nqv) put<T, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
 }
 
 template <typename T>

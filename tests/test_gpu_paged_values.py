@@ -1,0 +1,72 @@
+"""Paged attention on values at the edge of the definition, and how exact its sums are."""
+import math
+
+import pytest
+import torch
+
+from paged_ref import attend64, attend_bound, make_cache, rows_of
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+DTYPES = pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+
+
+def queries(n, heads, hd, dtype, seed=1):
+    return torch.randn(n, heads, hd, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+
+
+def set_rows(pool, cache, b, positions, value):
+    """Column 0 of these positions of sequence b."""
+    table = cache.table[b].tolist()
+    for j in positions:
+        pool[table[j // cache.page_size], 0, :, j % cache.page_size, 0] = value
+
+
+@DTYPES
+@pytest.mark.parametrize("hkv,heads,hd", [(1, 2, 32), (2, 4, 64), (2, 2, 128)])
+@pytest.mark.parametrize("rows", [1, 9, 40, 300])
+@pytest.mark.parametrize("before", [0, 2500], ids=["short", "split"])
+def test_scores_of_minus_infinity(dtype, hkv, heads, hd, rows, before):
+    """Four sequences.  All scores -inf: the softmax of that is NaN, as in the definition, not the zeros of a row that
+    reads nothing.  All but one, or all but the later half: those alone count.  No page: zeros."""
+    n = before + rows
+    cache = make_cache([n] * 4, dtype, hkv, hd, 16)
+    ln, _ = rows_of([n] * 4, [rows] * 4, False)
+    q = queries(4 * rows, heads, hd, dtype)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    set_rows(cache.k, cache, 0, range(n), -math.inf)
+    set_rows(cache.k, cache, 1, range(1, n), -math.inf)
+    set_rows(cache.k, cache, 2, range((n + 1) // 2), -math.inf)
+    cache.table[3] = -1
+    got = cache.attend(q, ln, max_len=n).double().view(4, rows, heads, hd)
+    ref, absv, spread = attend64(cache, q, [n] * 4, [rows] * 4)
+    ref, absv = ref.view(4, rows, heads, hd), absv.view(4, rows, heads, hd)
+    assert torch.isnan(got[0]).all()
+    first = cache.v[int(cache.table[1, 0]), 0, :, 0].double().repeat_interleave(heads // hkv, 0)
+    assert (got[1] == first).all()
+    assert (got[3] == 0).all()
+    reads = before + torch.arange(rows, device="cuda") >= (n + 1) // 2
+    assert torch.isnan(got[2][~reads]).all()
+    # (the sums of magnitudes that the bound goes by, without the infinite ones)
+    plain = make_cache([n] * 4, dtype, hkv, hd, 16)
+    spread = attend64(plain, q, [n] * 4, [rows] * 4)[2]
+    assert ((got[2] - ref[2]).abs() <= attend_bound(ref[2], absv[2], spread, dtype, n, hd))[reads].all()
+
+
+@DTYPES
+@pytest.mark.parametrize("rows", [1, 33, 300])
+@pytest.mark.parametrize("max_len", [None, 64], ids=["split", "whole"])
+def test_minus_infinity_behind_missing_pages(dtype, rows, max_len):
+    """The first page that is there begins at position 1600, which half of the rows reach, and its keys score -inf: zeros for
+    the rows before it, which read nothing, and NaN for the others."""
+    hkv, heads, hd, n = 2, 4, 64, 1600 + (rows + 1) // 2
+    cache = make_cache([n, n], dtype, hkv, hd, 16)
+    set_rows(cache.k, cache, 0, range(n), -math.inf)
+    cache.table[0, :100] = -1
+    cache.table[0, 7] = cache.n_pages  # (no page either)
+    ln, _ = rows_of([n, n], [rows] * 2, False)
+    q = queries(2 * rows, heads, hd, dtype)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    got = cache.attend(q, ln, max_len=max_len)[:rows]
+    reads = n - rows + torch.arange(rows, device="cuda") >= 1600
+    assert torch.isnan(got[reads]).all() and (got[~reads] == 0).all() and reads.any()
