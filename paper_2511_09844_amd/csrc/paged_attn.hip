@@ -1073,11 +1073,16 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
     load(t0 * KT, pg, t0 & 1);
     entry = entry1;
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-    // (a negative scale turns into the sign of q, and 0 into q = 0: scores that do not count are -inf before
-    // they are scaled)
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = a.scale != 0.f ? ~0u : 0u;
+    // (a negative scale turns into the sign of q, and 0 into q = 0, NaN where it is no finite number: scores that do
+    // not count are -inf before they are scaled)
+    if (a.scale != 0.f) {
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-    for (int i = 0; i < NS; ++i) q[i] = (q[i] ^ flip) & keep;
+        for (int i = 0; i < NS; ++i) q[i] ^= flip;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4 * NS; ++i) q[i / 4][i % 4] = (odd_bits<uint16_t>(q[i / 4][i % 4]) >> 15 & 0x00010001) * 0x7fc0;
+    }
     __syncthreads();
     f16v s;
     u4 x[2][NC];

@@ -70,3 +70,22 @@ def test_minus_infinity_behind_missing_pages(dtype, rows, max_len):
     got = cache.attend(q, ln, max_len=max_len)[:rows]
     reads = n - rows + torch.arange(rows, device="cuda") >= 1600
     assert torch.isnan(got[reads]).all() and (got[~reads] == 0).all() and reads.any()
+
+
+@DTYPES
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("rows", [3, 100])
+def test_scale_zero_and_queries_that_are_no_numbers(dtype, hd, rows):
+    """0 times an infinity or NaN is NaN; every other row is a mean."""
+    n = rows + 70
+    cache = make_cache([n], dtype, 2, hd, 16)
+    q = queries(rows, 4, hd, dtype)
+    q[0, 1, 3], q[2, 0, hd - 1], q[2, 3, 0] = math.nan, math.inf, -math.inf
+    ln, _ = rows_of([n], [rows], False)
+    got = cache.attend(q, ln, scale=0.0)
+    odd = torch.zeros(rows, 4, dtype=torch.bool, device="cuda")
+    odd[0, 1] = odd[2, 0] = odd[2, 3] = True
+    assert torch.isnan(got[odd]).all()
+    q[odd] = 0
+    ref, absv, spread = attend64(cache, q, [n], [rows], scale=0.0)
+    assert ((got.double() - ref).abs() <= attend_bound(ref, absv, spread, dtype, n, hd))[~odd].all()
