@@ -16,6 +16,7 @@ import ctypes
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as B
 
@@ -28,6 +29,11 @@ _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: 
 def _need(ok, msg):
     if not ok:
         raise B.Sd2Error(msg)
+
+
+def _tangent(t):
+    """Whether t carries a forward-mode tangent (outside a dual level, which is quick to see, none does)."""
+    return getattr(forward_ad, "_current_level", 0) >= 0 and forward_ad.unpack_dual(t).tangent is not None
 
 
 class PagedCache:
@@ -88,6 +94,7 @@ class PagedCache:
         _need(isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == self.dtype and t.dim() == 3 and
               t.shape[2] == self.head_dim, f"{what}: [rows][heads][head_dim] of the cache's type, on its device")
         _need(not t.requires_grad or not torch.is_grad_enabled(), f"{what}: no gradients here (torch.no_grad(), or detach it)")
+        _need(not _tangent(t), f"{what}: no forward-mode tangents here (take its primal)")
         if t.numel():
             _need(t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == self.head_dim),
                   f"{what}: heads and head dimension have to be contiguous")

@@ -1,0 +1,36 @@
+"""What PagedCache refuses beside sizes and types: gradients that would be lost, and operands that lie in one another."""
+import pytest
+import torch
+import torch.autograd.forward_ad as forward_ad
+
+from paged_ref import attend64, attend_bound, make_cache
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def setup():
+    cache = make_cache([40, 50], BF16, 2, 64, 16)
+    ln = torch.tensor([40, 50], dtype=torch.int32, device="cuda")
+    q = torch.randn(2, 4, 64, generator=torch.Generator().manual_seed(1)).to(BF16).cuda()
+    return cache, ln, q
+
+
+def refused(call):
+    from paper_2511_09844_amd.binding import Sd2Error
+    with pytest.raises(Sd2Error):
+        call()
+
+
+def test_forward_mode_tangents_are_refused():
+    cache, ln, q = setup()
+    kv = q[:, :2].contiguous()
+    with forward_ad.dual_level():
+        dual, rows = forward_ad.make_dual(q, torch.ones_like(q)), forward_ad.make_dual(kv, torch.ones_like(kv))
+        refused(lambda: cache.attend(dual, ln))
+        refused(lambda: cache.append(rows, kv, ln))
+        refused(lambda: cache.append(kv, rows, ln))
+        with torch.no_grad():  # (which does not stop forward mode)
+            refused(lambda: cache.attend(dual, ln))
+        plain = cache.attend(q, ln)  # no tangent, no refusal
+    assert torch.equal(plain, cache.attend(forward_ad.unpack_dual(dual).primal, ln))
