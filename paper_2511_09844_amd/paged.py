@@ -46,6 +46,7 @@ class PagedCache:
               "[n_pages][n_layers][n_kv_heads][page_size][head_dim]")
         _need(v.shape == k.shape and v.dtype == k.dtype and v.device == k.device, "v has to be like k")
         _need(k.is_contiguous() and v.is_contiguous(), "k and v have to be contiguous")
+        _need(not any(t.requires_grad or _tangent(t) for t in (k, v)), "k and v: no gradients here (detach them)")
         self._int32(table, 2, "table", k.device)
         self._int32(refs, 1, "refs", k.device)
         n_pages, n_layers, n_kv, page, hd = k.shape

@@ -34,3 +34,16 @@ def test_forward_mode_tangents_are_refused():
             refused(lambda: cache.attend(dual, ln))
         plain = cache.attend(q, ln)  # no tangent, no refusal
     assert torch.equal(plain, cache.attend(forward_ad.unpack_dual(dual).primal, ln))
+
+
+def test_pools_that_want_gradients_are_refused():
+    from paper_2511_09844_amd.paged import PagedCache
+    cache, ln, q = setup()
+    for k, v in ((cache.k.clone().requires_grad_(), cache.v), (cache.k, cache.v.clone().requires_grad_())):
+        refused(lambda: PagedCache(k, v, cache.table, cache.refs))
+        with torch.no_grad():
+            refused(lambda: PagedCache(k, v, cache.table, cache.refs))  # (it may be used outside)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(cache.k, torch.ones_like(cache.k))
+        refused(lambda: PagedCache(dual, cache.v, cache.table, cache.refs))
+    assert torch.equal(PagedCache(cache.k, cache.v, cache.table, cache.refs).attend(q, ln), cache.attend(q, ln))
