@@ -938,7 +938,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
                 // (no builtin: with it every read of LDS waits for what is still on its way to the other buffers;
                 // `meet` below says who waits for what)
                 asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                             :: "s"(to + i * 1024), "v"(off), "s"(rs) : "memory", "m0");
+                             :: "s"(to + i * 1024), "v"(off), "s"(rs) : "memory");
             }
         }
     };
