@@ -480,6 +480,16 @@ bool strided(const void* p, int64_t stride, int64_t width, int size) {
     return aligned(p, 16) && stride >= width && stride % (16 / size) == 0 && stride <= (int64_t)1 << 40;
 }
 
+// Whether two such operands of n rows share an element.  Rows of one stride may lie in one another's gaps; of others
+// it is enough that their extents meet.
+bool overlap(const void* p, int64_t ps, const void* q, int64_t qs, int64_t n, int64_t width, int size) {
+    const __int128 d = ((__int128)(uintptr_t)q - (__int128)(uintptr_t)p) / size;  // (16-byte aligned)
+    if (d >= (n - 1) * (__int128)ps + width || -d >= (n - 1) * (__int128)qs + width) return false;
+    if (ps != qs || n == 1) return true;
+    const int64_t gap = (int64_t)((d % ps + ps) % ps);
+    return gap < width || gap > ps - width;
+}
+
 }  // namespace
 
 }  // namespace sd2
@@ -570,7 +580,9 @@ sd2_status sd2_paged_attn(const sd2_paged_kv* kv, const sd2_paged_rows* rows, co
     if ((int64_t)a.r.max_rows * (n_heads / a.c.Hkv) > 1 << 30) return SD2_ERR_INVALID_ARG;
     if (!a.r.nseq || !a.r.total_rows) return SD2_OK;
     const int64_t width = (int64_t)n_heads * a.c.hd;
-    if (!strided(q, q_stride, width, size) || !strided(out, out_stride, width, size)) return SD2_ERR_INVALID_ARG;
+    if (!strided(q, q_stride, width, size) || !strided(out, out_stride, width, size) ||
+        overlap(q, q_stride, out, out_stride, a.r.total_rows, width, size))
+        return SD2_ERR_INVALID_ARG;
     const size_t need = paged_attn_bytes(a.c, a.r, n_heads, size == 2, max_len);
     if (!need || !aligned(workspace, 256) || workspace_bytes < need) return SD2_ERR_INVALID_ARG;
     const sd2_status st = device_ok();

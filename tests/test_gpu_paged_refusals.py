@@ -47,3 +47,24 @@ def test_pools_that_want_gradients_are_refused():
         dual = forward_ad.make_dual(cache.k, torch.ones_like(cache.k))
         refused(lambda: PagedCache(dual, cache.v, cache.table, cache.refs))
     assert torch.equal(PagedCache(cache.k, cache.v, cache.table, cache.refs).attend(q, ln), cache.attend(q, ln))
+
+
+@pytest.mark.parametrize("rows", [1, 70])
+def test_q_and_out_that_share_elements_are_refused(rows):
+    """Columns of one buffer: heads 0-3 are q; out beside them is computed, out over them refused."""
+    cache = make_cache([rows + 40, rows + 9], BF16, 2, 64, 16)
+    ln = torch.tensor([rows + 40, rows + 9], dtype=torch.int32, device="cuda")
+    wide = torch.randn(2 * rows, 12, 64, generator=torch.Generator().manual_seed(1)).to(BF16).cuda()
+    q = wide[:, 4:8]
+    want = cache.attend(q, ln)
+    ref, absv, spread = attend64(cache, q, [rows + 40, rows + 9], [rows] * 2)
+    assert ((want.double() - ref).abs() <= attend_bound(ref, absv, spread, BF16, rows + 40, 64)).all()
+    for first in (1, 2, 3, 4, 5, 7):
+        refused(lambda: cache.attend(q, ln, out=wide[:, first: first + 4]))
+    for first in (0, 8):
+        assert torch.equal(cache.attend(q, ln, out=wide[:, first: first + 4]), want)
+    assert torch.equal(cache.attend(q, ln), want)
+    flat = torch.empty(4 * rows, 4, 64, dtype=BF16, device="cuda")  # one behind the other
+    flat[: 2 * rows] = q
+    assert torch.equal(cache.attend(flat[: 2 * rows], ln, out=flat[2 * rows:]), want)
+    refused(lambda: cache.attend(flat[: 2 * rows], ln, out=flat[2 * rows - 1: 4 * rows - 1]))
