@@ -361,7 +361,9 @@ __device__ __forceinline__ void block_weights(Acc<T, HD, NT>& acc, f4 (&sc)[NT][
 }
 
 // The weights as bf16, the type of the matrix instruction that v enters as it is: half a step of
-// 2^-8 each, as much as the output's own rounding.
+// 2^-8 each, as much as the output's own rounding.  The largest error of 64 sequences of up to 4000 is 2.2e-3 that way and
+// 1.8e-3, the output's rounding alone, with the weights as two bf16 numbers each; those cost 0.3 us of 6.9 for one short
+// sequence, 3 % for blocks of eight rows and 9 % for 64 query vectors of head dim 32, and nothing in long batches.
 __device__ __forceinline__ b8 weights_b8(const f4 (&s)[2]) {
     return __builtin_bit_cast(b8, u4{pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]), pack_bf16(s[1][0], s[1][1]),
                                      pack_bf16(s[1][2], s[1][3])});

@@ -1,4 +1,4 @@
-"""Paged attention on values at the edge of the definition, and how exact its sums are."""
+"""Paged attention on values at the edge of the definition."""
 import math
 
 import pytest
@@ -89,3 +89,26 @@ def test_scale_zero_and_queries_that_are_no_numbers(dtype, hd, rows):
     q[odd] = 0
     ref, absv, spread = attend64(cache, q, [n], [rows], scale=0.0)
     assert ((got.double() - ref).abs() <= attend_bound(ref, absv, spread, dtype, n, hd))[~odd].all()
+
+
+@DTYPES
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("rows", [1, 6, 40, 200])
+def test_infinite_values_stay_infinite(dtype, hd, rows):
+    """Infinities of v that every row reads, beside weights of all sizes, 1 among them (a row that reads one key)."""
+    lens = [rows + 150, rows]
+    cache = make_cache(lens, dtype, 1, hd, 16)
+    table = cache.table.tolist()
+    for b, at in ((0, 7), (0, 100), (1, 0)):
+        cache.v[table[b][at // 16], 0, :, at % 16, 1] = math.inf
+        cache.v[table[b][at // 16], 0, :, at % 16, 2] = -math.inf
+    cache.v[table[0][0], 0, :, 3, 2] = math.inf  # both signs
+    ln, _ = rows_of(lens, [rows] * 2, False)
+    q = queries(2 * rows, 3, hd, dtype)
+    got = cache.attend(q, ln)
+    assert (got[..., 1] == math.inf).all()
+    assert torch.isnan(got[:rows, :, 2]).all() and (got[rows:, :, 2] == -math.inf).all()
+    other = [c for c in range(hd) if c not in (1, 2)]
+    ref, absv, spread = attend64(cache, q, lens, [rows] * 2)
+    bound = attend_bound(ref, absv, spread, dtype, max(lens), hd)
+    assert ((got.double() - ref).abs() <= bound)[..., other].all()
