@@ -65,9 +65,18 @@ def advance(eng, forced):
 @pytest.mark.parametrize("wl", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("length,slot", [(13, 0), (20, 7), (12, 15)], ids=["first", "middle", "last"])
 @pytest.mark.parametrize("accepted", [4, 3, 0])
-def test_fork_after_a_round(wl, length, slot, accepted):
+@pytest.mark.parametrize("stream", [False, True], ids=["default", "graphs"])
+def test_fork_after_a_round(wl, length, slot, accepted, stream):
     """With every draft accepted the verifier holds one position more than the drafter, on a page that the fork
-    shares: that row belongs to what is copied, whatever slot it lies in."""
+    shares: that row belongs to what is copied, whatever slot it lies in.  (On a stream of its own rounds are replayed
+    from graphs.)"""
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream() if stream else torch.cuda.current_stream()):
+        fork_after_a_round(wl, length, slot, accepted)
+    torch.cuda.synchronize()
+
+
+def fork_after_a_round(wl, length, slot, accepted):
     m = Model(wl.with_(prompt=(length, length)))
     plain, paged = m.engine(), m.engine(paging=(16, 40))
     toks = prompts(1, length)
