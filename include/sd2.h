@@ -390,7 +390,8 @@ sd2_status sd2_paged_append(const sd2_paged_kv* kv, const sd2_paged_rows* rows, 
  * q, out: device [total_rows][n_heads][head_dim], q_stride and out_stride elements from one row to the next
  * (whole 16-byte units); n_heads a multiple of n_kv_heads, up to 1024.  q and out may be columns of one buffer, but
  * share no element (SD2_ERR_INVALID_ARG; of different strides: their extents must not meet).  bf16: scores,
- * softmax and sums in fp32, the softmax's weights rounded to bf16 for their product with v; fp32: fp32 throughout.
+ * softmax and sums in fp32, the softmax's weights rounded to bf16 for their product with v (up to 64 query vectors
+ * of a sequence and KV head: to two bf16 numbers each, 2^-15 of the weight); fp32: fp32 throughout.
  * Memory behind a sequence's last position, and pages it does not name, are not read, or do not count,
  * whatever they hold; infinities and NaN of a position reach the rows that read it, and no others.
  * The rows of a sequence times n_heads / n_kv_heads are at most 2^30.  Sizes that together make a launch of 2^32

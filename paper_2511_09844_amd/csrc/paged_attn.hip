@@ -20,7 +20,7 @@
 // Few rows are bound by the bytes of K and V: on MI355X one token of 16 fp32 sequences (152 MB) takes 37 us with
 // its join, one of a bf16 batch of 905 MB 165 (5.5 TB/s), eight rows of 16 fp32 sequences 50 (155 MB, and
 // 16 us of fp32 matrix instructions that overlap with the loads in part); one short sequence is
-// bound by round trips to memory in a row, 6.9 us.  Prompts are bound by the matrix cores, see k_pprompt_bf16.
+// bound by round trips to memory in a row, 7.1 us.  Prompts are bound by the matrix cores, see k_pprompt_bf16.
 #include <math.h>
 
 #include <algorithm>
@@ -360,13 +360,29 @@ __device__ __forceinline__ void block_weights(Acc<T, HD, NT>& acc, f4 (&sc)[NT][
     }
 }
 
-// The weights as bf16, the type of the matrix instruction that v enters as it is: half a step of
-// 2^-8 each, as much as the output's own rounding.  The largest error of 64 sequences of up to 4000 is 2.2e-3 that way and
-// 1.8e-3, the output's rounding alone, with the weights as two bf16 numbers each; those cost 0.3 us of 6.9 for one short
-// sequence, 3 % for blocks of eight rows and 9 % for 64 query vectors of head dim 32, and nothing in long batches.
-__device__ __forceinline__ b8 weights_b8(const f4 (&s)[2]) {
-    return __builtin_bit_cast(b8, u4{pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]), pack_bf16(s[1][0], s[1][1]),
-                                     pack_bf16(s[1][2], s[1][3])});
+// The weights in the type of the matrix instruction that v enters as it is, bf16, as the sum of two: the leading
+// digits (less than the weight by up to 2^-7 of it), and what they left out rounded (half a step, 2^-8 of that).  Neither
+// is 0 or negative unless the weight is 0, so that an infinity of v stays what it is.  The largest error of 64
+// sequences of up to 4000 is 1.8e-3, the output's own rounding, and 2.2e-3 with the weights rounded once.  That would save
+// 0.2 us of 7.1 for one short sequence, 3 % for blocks of eight rows, 7 % for 64 query vectors of head dim 32, and
+// nothing in long batches, whose matrix cores wait for bytes.
+struct Split {
+    u4 hi, lo;
+};
+__device__ __forceinline__ Split split_b8(const f4 (&s)[2]) {
+    Split w;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const float x = s[d / 2][d % 2 * 2], y = s[d / 2][d % 2 * 2 + 1];
+        const uint32_t a = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u) & 0xffff0000,
+                       b = __builtin_elementwise_sub_sat(__float_as_uint(y), 1u) & 0xffff0000;
+        w.hi[d] = __builtin_amdgcn_perm(b, a, 0x07060302);
+        w.lo[d] = pack_bf16(x - __uint_as_float(a), y - __uint_as_float(b));
+    }
+    return w;
+}
+__device__ __forceinline__ f4 mfma_b8(u4 v, u4 w, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, v), __builtin_bit_cast(b8, w), c, 0, 0, 0);
 }
 // Columns 16 i .. 16 i + 15 of a bf16 block's V as an operand.
 template <int HD>
@@ -383,15 +399,25 @@ template <typename T, int HD, int NT>
 __device__ __forceinline__ void block_sums(const Block<T, HD>& x, const f4 (&sc)[NT][Block<T, HD>::TK], Acc<T, HD, NT>& acc) {
     using B = Block<T, HD>;
     if constexpr (B::H) {
-        b8 p[NT];
+        Split p[NT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) p[j] = weights_b8(sc[j]);
+        for (int j = 0; j < NT; ++j) p[j] = split_b8(sc[j]);
+        // (all of the leading digits' products first, where registers hold the operands meanwhile: 7.07 and 7.19 us for
+        // one short sequence)
+        constexpr int W = NT == 1 || HD < 128 ? HD / 16 : 1;
 #pragma unroll
-        for (int i = 0; i < HD / 16; ++i) {
-            const u4 w = values_b8<HD>(x, i);
+        for (int i0 = 0; i0 < HD / 16; i0 += W) {
+            u4 w[W];
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                acc.o[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, w), p[j], acc.o[j][i], 0, 0, 0);
+            for (int i = 0; i < W; ++i) {
+                w[i] = values_b8<HD>(x, i0 + i);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc.o[j][i0 + i] = mfma_b8(w[i], p[j].hi, acc.o[j][i0 + i]);
+            }
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc.o[j][i0 + i] = mfma_b8(w[i], p[j].lo, acc.o[j][i0 + i]);
         }
     } else {
 #pragma unroll
@@ -440,7 +466,8 @@ __device__ __forceinline__ void block_sums_odd(const Block<T, HD>& x, const f4 (
             for (int j = 0; j < NT; ++j) {
                 f4 c = {0.f, 0.f, 0.f, 0.f};
                 if constexpr (B::H) {
-                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, w), weights_b8(sc[j]), c, 0, 0, 0);
+                    const Split p = split_b8(sc[j]);
+                    c = mfma_b8(w, p.hi, mfma_b8(w, p.lo, c));
                 } else {
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
@@ -988,7 +1015,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
 #pragma unroll
         for (int i = 0; i < NC; ++i) o[i] *= f;
     };
-    // (bf16, see block_sums; their sum from before the rounding)
+    // (bf16, half a step of 2^-8 each, as much as the output's own rounding; their sum from before it.  As two numbers
+    // each, see split_b8, they take half as many matrix instructions again: 8192 positions 718 us, not 526)
     auto weights = [&](const f16v& s, u4 (&p)[2]) {
         const float base = m == -INFINITY ? 0.f : m;
         float sum[2] = {0.f, 0.f};

@@ -1,4 +1,4 @@
-"""Paged attention on values at the edge of the definition."""
+"""Paged attention on values at the edge of the definition, and how exact its sums are."""
 import math
 
 import pytest
@@ -89,6 +89,32 @@ def test_scale_zero_and_queries_that_are_no_numbers(dtype, hd, rows):
     q[odd] = 0
     ref, absv, spread = attend64(cache, q, [n], [rows], scale=0.0)
     assert ((got.double() - ref).abs() <= attend_bound(ref, absv, spread, dtype, n, hd))[~odd].all()
+
+
+@pytest.mark.parametrize("hkv,heads,hd", [(2, 4, 32), (2, 6, 64), (1, 8, 128), (2, 32, 64)])
+@pytest.mark.parametrize("rows", [1, 2, 4])
+@pytest.mark.parametrize("odd", [False, True], ids=["plain", "odd"])
+def test_weights_of_few_bf16_rows(hkv, heads, hd, rows, odd):
+    """The softmax's weights enter their product with v as two bf16 numbers each: the second, up to 2^-7 of the weight, is
+    off by half a step of 2^-8, so the weight by 2^-15, and what a row is off by is its fp32 sums and its own
+    rounding.  odd: with a NaN that only the last row reads, which such blocks are computed another way for."""
+    lens = [20, 33, 64, 90, 300]
+    cache = make_cache(lens, BF16, hkv, hd, 16)
+    q = queries(rows * len(lens), heads, hd, BF16)
+    ref, absv, spread = attend64(cache, q, lens, [rows] * len(lens))
+    sums = attend_bound(ref, absv, spread, F32, max(lens), hd) + 2.0 ** -15 * absv
+    bound = sums + 2.0 ** -8 * (ref.abs() + sums)
+    if odd:
+        for b, n in enumerate(lens):
+            cache.v[int(cache.table[b, (n - 1) // 16]), 0, :, (n - 1) % 16, 0] = math.nan
+    ln, _ = rows_of(lens, [rows] * len(lens), False)
+    for max_len in (None, 64):  # split, and not
+        err = (cache.attend(q, ln, max_len=max_len).double() - ref).abs()
+        ok = err <= bound
+        if odd:
+            ok = ok.view(len(lens), rows, heads, hd)
+            ok[:, -1, :, 0] = True
+        assert ok.all(), float((err / bound).nan_to_num().max())
 
 
 @DTYPES
