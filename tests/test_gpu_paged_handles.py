@@ -135,3 +135,69 @@ def test_a_sequence_takes_no_pages_of_a_round_it_cannot_run(wl, lens):
     got, waited = generate(paged, n)
     assert got == want
     assert waited[lens.index(18)] == 0 and sum(w > 0 for w in waited) == n - 1
+
+
+@pytest.mark.parametrize("own", [False, True], ids=["drafter", "itself"])
+@pytest.mark.parametrize("page,n_pages", [(16, 17), (32, 12)])
+@pytest.mark.parametrize("seed", [0, 1, 2])
+def test_random_forks_releases_and_compactions(own, page, n_pages, seed):
+    """Two prompts and greedy decoding, over a pool that is short at times.  Whatever is forked, released and moved between
+    the rounds, each sequence goes on with the tokens of the prompt it comes from.  itself: the verifier drafts, so
+    that nearly every draft is accepted."""
+    g = torch.Generator().manual_seed(seed)
+
+    def pick(n):
+        return int(torch.randint(0, n, (1,), generator=g))
+
+    wl = F32.with_(batch=7, new_tokens=40, prompt=(30, 45))
+    if own:
+        wl = wl.with_(drafter=wl.verifier)
+    m = Model(wl)
+    if own:
+        m.dd = m.dv
+    cfg = B.config_of(wl, steering=B.STEER_NONE) if own else B.config_of(wl)
+    ws = None if own else m.ws
+    plain, paged = B.Engine(cfg, m.dv, m.dd, ws), B.Engine(cfg, m.dv, m.dd, ws, paging=(page, n_pages))
+    toks, lens = prompts(2, 45, seed), [45, 30]
+    prefill(plain, toks, lens)
+    want, _ = generate(plain, 2)
+    prefill(paged, toks, lens)
+    origin, got, over, full = [0, 1], [[], []], set(), 0
+    for _ in range(200):
+        state = paged.state()
+        what = pick(6)
+        if what == 0 and len(origin) < 7:
+            b, count = pick(len(origin)), 1 + pick(min(2, 7 - len(origin)))
+            paged.fork(b, count)
+            origin += [origin[b]] * count
+            got += [list(got[b]) for _ in range(count)]
+            if state[b]["done"] == 1:
+                over |= set(range(len(origin) - count, len(origin)))
+        elif what == 1:
+            paged.compact()
+        elif what == 2 and len(origin) > 3:
+            b = 2 + pick(len(origin) - 2)
+            paged.release(b)
+            over.add(b)
+        before = paged.state()
+        out, cnt = (x.cpu().tolist() for x in paged.round())
+        after = paged.state()
+        for b in range(len(origin)):
+            got[b] += out[b][: cnt[b]]
+            full += cnt[b] == wl.k + 1
+            assert got[b] == want[origin[b]][: len(got[b])], b
+            if after[b]["done"] == 1 and b not in over:
+                assert got[b] == want[origin[b]]
+                over.add(b)
+            if before[b]["done"] == 1:
+                assert cnt[b] == 0
+        refs, table = paged.debug(B.DBG_REFS), paged.debug(B.DBG_TABLE)
+        assert all((table == p).sum() == n for p, n in enumerate(refs))
+        if len(over) == len(origin):
+            break
+        if all(s["done"] for s in after):
+            b = max(b for b in range(len(origin)) if b not in over)
+            paged.release(b)
+            over.add(b)
+    assert len(over) == len(origin)
+    assert not own or full > 8
