@@ -292,11 +292,13 @@ sd2_status sd2_train_loss(sd2_handle_t h, const int32_t* tokens, const int32_t* 
 #define SD2_PAGED_MAX_SEQS 4096
 
 /* One array of a cache: page p is blocks * page_size rows of row_bytes bytes, page after page.  A block
- * (a layer and KV head, say) is the page's positions in order. */
+ * (a layer and KV head, say) is the page's positions in order.  With a negative row_bytes it has no rows: page p is
+ * blocks records of -row_bytes bytes (the scales of a layer, say), which go along whole where any row of the page is
+ * copied. */
 typedef struct {
     void* data;         /* device, 16-byte aligned */
     int32_t blocks;     /* 1..65536 */
-    int32_t row_bytes;  /* a multiple of 16, up to 65536 */
+    int32_t row_bytes;  /* a multiple of 16, up to 65536; or minus a multiple of 2, up to 2^20 */
 } sd2_page_array;
 
 typedef struct {
@@ -341,6 +343,14 @@ sd2_status sd2_pages_fork(const sd2_pages* pages, int32_t n, const int32_t* src,
  * and give up the others; lens[b] = 0 frees a sequence, a negative one leaves it as it is.
  */
 sd2_status sd2_pages_trim(const sd2_pages* pages, int32_t nseq, const int32_t* lens, void* hip_stream);
+
+/*
+ * Sequences b = 0 .. nseq - 1 give up the pages that their next rows, from position lens[b] on, do not read under a
+ * window (see sd2_paged_attn_window): those whose positions are all at least sinks and at most lens[b] - window.
+ * lens: device int32 [nseq]; a negative one leaves its sequence as it is.  window: 1..2^30; sinks: 0..2^30.
+ */
+sd2_status sd2_pages_slide(const sd2_pages* pages, int32_t nseq, const int32_t* lens, int32_t window, int32_t sinks,
+                           void* hip_stream);
 
 /*
  * Move the pages in use (refs above 0) to 0 .. live - 1: those behind, in ascending order, into the
@@ -405,6 +415,55 @@ size_t sd2_paged_attn_workspace_bytes(const sd2_paged_kv* kv, const sd2_paged_ro
 sd2_status sd2_paged_attn(const sd2_paged_kv* kv, const sd2_paged_rows* rows, const void* q, int64_t q_stride,
                           void* out, int64_t out_stride, int32_t n_heads, float scale, int32_t max_len,
                           void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * sd2_paged_attn under a window: the row at position p reads the positions j <= p with p - j < window (its own and
+ * the window - 1 before it) or j < sinks, of those that have a page.  window: 1..2^30, or 0 for every j <= p;
+ * sinks: 0..2^30.  Positions that no row of a sequence reads cost nothing, and need no pages (sd2_pages_slide).
+ * Everything else is as with sd2_paged_attn; the workspace is that of the same window and sinks.
+ */
+size_t sd2_paged_attn_window_workspace_bytes(const sd2_paged_kv* kv, const sd2_paged_rows* rows, int32_t n_heads,
+                                             int32_t max_len, int32_t window, int32_t sinks);
+sd2_status sd2_paged_attn_window(const sd2_paged_kv* kv, const sd2_paged_rows* rows, const void* q, int64_t q_stride,
+                                 void* out, int64_t out_stride, int32_t n_heads, float scale, int32_t max_len,
+                                 int32_t window, int32_t sinks, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * A paged cache that holds 8 bits a value: k and v are e4m3 numbers (4 exponent bits, bias 7; 3 mantissa bits; no
+ * infinities, 0x7f and 0xff are NaN), and each 16 positions of a KV head (slots 16 j .. 16 j + 15 of a page) have a
+ * power of two for k and one for v that their numbers are multiplied by, 2^(byte - 127).  The bytes of KV head h and
+ * j are k's at scales[p * scale_stride + (h * page_size / 16 + j) * 2] for page p, and v's behind it; those that
+ * sd2_paged_append_scaled writes are 27..246, and others give no defined values.  For sd2_pages_* the scales are an array
+ * of their own, of records.
+ */
+typedef struct {
+    sd2_paged_kv kv;       /* dtype: of the rows of a call (new rows, q and out); k, v and page_stride in elements of a byte */
+    void* scales;          /* device, 2-byte aligned */
+    int64_t scale_stride;  /* bytes from one page to the next, even, at least n_kv_heads * page_size / 8 */
+} sd2_paged_scaled;
+
+/*
+ * sd2_paged_append into such a cache.  With a the largest finite magnitude of the new rows in 16 positions of a KV
+ * head (k and v apart), their power 2^e is the least with 448 * 2^e >= a, e in -100..119.  Where the first of the new
+ * rows is not the first of the 16 positions, e is at least what it was before, and when it grows the numbers of the
+ * positions before the first new row are rounded again to the new one.  A value x becomes the e4m3 number nearest to
+ * x / 2^e (ties to even, at most 448 in magnitude); an infinity or NaN becomes NaN.  Positions of the 16 behind the
+ * last new row are not written (and count for nothing until they are).  One sequence's rows of 16 positions are
+ * best brought in one call: what they are rounded to does not depend on it, except below 2^(e - 6), where numbers
+ * that were rounded before e grew are rounded twice.
+ */
+sd2_status sd2_paged_append_scaled(const sd2_paged_scaled* kv, const sd2_paged_rows* rows, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, void* hip_stream);
+
+/*
+ * sd2_paged_attn_window over such a cache (window 0: sd2_paged_attn), for q and out of kv->kv.dtype.  The cache's values enter
+ * both products exactly; q, sums and softmax are as there.
+ */
+size_t sd2_paged_attn_scaled_workspace_bytes(const sd2_paged_scaled* kv, const sd2_paged_rows* rows, int32_t n_heads,
+                                       int32_t max_len, int32_t window, int32_t sinks);
+sd2_status sd2_paged_attn_scaled(const sd2_paged_scaled* kv, const sd2_paged_rows* rows, const void* q, int64_t q_stride,
+                           void* out, int64_t out_stride, int32_t n_heads, float scale, int32_t max_len,
+                           int32_t window, int32_t sinks, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Destroy a handle (NULL is a no-op).  Does not free caller memory. */
 sd2_status sd2_destroy(sd2_handle_t h);

@@ -22,7 +22,9 @@ EXPORTS = ["sd2_workspace_bytes", "sd2_create", "sd2_create_noalloc", "sd2_creat
            "sd2_train_loss_scratch_bytes", "sd2_prefill", "sd2_round", "sd2_round_forced", "sd2_destroy",
            "sd2_status_string", "sd2_last_error", "sd2_debug_read", "sd2_profile", "sd2_profile_read",
            "sd2_pages_workspace_bytes", "sd2_pages_reserve", "sd2_pages_fork", "sd2_pages_trim", "sd2_pages_compact",
-           "sd2_paged_append", "sd2_paged_attn_workspace_bytes", "sd2_paged_attn", "sd2_create_paged_bytes",
+           "sd2_paged_append", "sd2_paged_attn_workspace_bytes", "sd2_paged_attn", "sd2_pages_slide",
+           "sd2_paged_attn_window_workspace_bytes", "sd2_paged_attn_window", "sd2_paged_append_scaled",
+           "sd2_paged_attn_scaled_workspace_bytes", "sd2_paged_attn_scaled", "sd2_create_paged_bytes",
            "sd2_create_paged", "sd2_fork", "sd2_release", "sd2_compact"]
 PROF_GEMV, PROF_ATTN, PROF_SAMPLER, PROF_OTHER, PROF_PROGRAM = 1, 2, 3, 4, 5
 
@@ -73,6 +75,10 @@ class PagedKv(ctypes.Structure):
     _fields_ = [("k", P), ("v", P), ("page_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", P)]
+
+
+class PagedScaled(ctypes.Structure):
+    _fields_ = [("kv", PagedKv), ("scales", P), ("scale_stride", ctypes.c_int64)]
 
 
 class PagedRows(ctypes.Structure):
@@ -142,6 +148,17 @@ def load():
         lib.sd2_paged_attn_workspace_bytes.restype = ctypes.c_size_t
         lib.sd2_paged_attn.argtypes = [kv, rows, P, i64, P, i64, i32, ctypes.c_float, i32, P, ctypes.c_size_t, P]
         lib.sd2_paged_attn.restype = i32
+        scaled = ctypes.POINTER(PagedScaled)
+        lib.sd2_pages_slide.argtypes = [pages, i32, P, i32, i32, P]
+        lib.sd2_pages_slide.restype = i32
+        lib.sd2_paged_append_scaled.argtypes = [scaled, rows, P, i64, P, i64, P]
+        lib.sd2_paged_append_scaled.restype = i32
+        for name, cache in (("sd2_paged_attn_window", kv), ("sd2_paged_attn_scaled", scaled)):
+            size, call = getattr(lib, name + "_workspace_bytes"), getattr(lib, name)
+            size.argtypes = [cache, rows, i32, i32, i32, i32]
+            size.restype = ctypes.c_size_t
+            call.argtypes = [cache, rows, P, i64, P, i64, i32, ctypes.c_float, i32, i32, i32, P, ctypes.c_size_t, P]
+            call.restype = i32
         lib.sd2_create_paged_bytes.argtypes = [ctypes.POINTER(Config), ctypes.POINTER(Paging)]
         lib.sd2_create_paged_bytes.restype = ctypes.c_size_t
         lib.sd2_create_paged.argtypes = [ctypes.POINTER(Config), ctypes.POINTER(Weights), ctypes.POINTER(Weights), P,

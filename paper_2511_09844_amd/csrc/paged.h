@@ -16,6 +16,10 @@ struct PagedView {
     int32_t n_pages, shift, Hkv, hd;  // page_size = 1 << shift
     const int32_t* table;             // [nseq][max_pages]; an entry outside 0 .. n_pages - 1: no page
     int32_t max_pages;
+    // k and v as e4m3 numbers: page p's powers of two for slots 16 j .. 16 j + 15 of KV head h are 2^(byte - 127) of the
+    // two bytes (k's, v's) at p * scale_stride + (h * page_size / 16 + j) * 2; else null
+    uint8_t* scales;
+    int64_t scale_stride;
 };
 
 // The rows a call brings: sequence b has rows row_off[b] .. row_off[b + 1] - 1 (at most max_rows of
@@ -37,17 +41,23 @@ struct PagedAttnArgs {
     int32_t Mp;
     int32_t H;
     float scale;
+    int32_t window, sinks;  // a row at p reads j <= p with p - j < window or j < sinks; window 0: every j <= p
 };
 
 // Workspace of a call (0: more than can be launched), and the call.  max_len: the largest length expected.  bf16: of
-// q, the cache and out (else fp32).
-size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len);
+// q, out and the cache, unless that has scales (else fp32).
+size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, int window = 0, int sinks = 0);
+hipError_t paged_attn_plain(hipStream_t s, const PagedAttnArgs& a, bool bf16);
 // With less than that the keys are split less.
 hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t ws_bytes);
 
 // k, v rows [total_rows][Hkv][hd] (row strides in elements) into their pages; size: bytes of an element.
 hipError_t paged_append(hipStream_t s, const PagedView& c, const PagedRows& r, const void* k, int64_t k_stride,
                         const void* v, int64_t v_stride, int size);
+
+// The same into e4m3 numbers; bf16: of the rows (else fp32).
+hipError_t paged_append8(hipStream_t s, const PagedView& c, const PagedRows& r, const void* k, int64_t k_stride,
+                         const void* v, int64_t v_stride, bool bf16);
 
 bool pages_ok(const sd2_pages* p);
 size_t pages_bytes(const sd2_pages& p);
@@ -57,6 +67,7 @@ hipError_t pages_reserve(hipStream_t s, const sd2_pages& p, int nseq, const int3
                          const int32_t* keep, int32_t* granted, void* ws, bool whole = false);
 hipError_t pages_fork(hipStream_t s, const sd2_pages& p, int n, const int32_t* src, const int32_t* dst);
 hipError_t pages_trim(hipStream_t s, const sd2_pages& p, int nseq, const int32_t* lens);
+hipError_t pages_slide(hipStream_t s, const sd2_pages& p, int nseq, const int32_t* lens, int window, int sinks);
 hipError_t pages_compact(hipStream_t s, const sd2_pages& p, int32_t* live, void* ws);
 
 // A kernel launch whose error is returned and not left behind.

@@ -1551,7 +1551,8 @@ hipError_t decode(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float*
 
 }  // namespace
 
-size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len) {
+size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, int window, int sinks) {
+    if (c.scales || window) return 256;
     if (many_rows(c, r, H, bf16)) {
         const PromptPlan p = prompt_plan(c, r, H, bf16, max_len, SIZE_MAX);
         return fits(c, r, bf16, p) ? std::max<size_t>(p.bytes, 256) : 0;
@@ -1563,6 +1564,7 @@ size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16
 hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t ws_bytes) {
     float* const w = (float*)ws;
     if (!a.r.total_rows || !a.r.nseq) return hipSuccess;
+    if (a.c.scales || a.window) return paged_attn_plain(s, a, bf16);
     switch (a.c.hd) {
         case 32: return bf16 ? decode<uint16_t, 32>(s, a, max_len, w, ws_bytes) : decode<float, 32>(s, a, max_len, w, ws_bytes);
         case 64: return bf16 ? decode<uint16_t, 64>(s, a, max_len, w, ws_bytes) : decode<float, 64>(s, a, max_len, w, ws_bytes);

@@ -276,7 +276,7 @@ __global__ __launch_bounds__(kBookThreads) void k_pages_compact(BookArgs a) {
 
 // Bytes: 2.6 GB read and written in two calls of a long sequence take 460 us, 5.6 TB/s; 32 forked sequences' last pages
 // 25 us.
-// A wave per block of a listed page and array: the first rows[i] rows of the block.  With a table its
+// A wave per block of a listed page and array: the first rows[i] rows of the block, or a record whole.  With a table its
 // entries that name a moved page are renamed as well.
 struct CopyArgs {
     PageList l;
@@ -307,6 +307,16 @@ __global__ __launch_bounds__(256) void k_pages_copy(CopyArgs a) {
         while (blk >= a.blocks[arr]) blk -= a.blocks[arr++];
         const int src = a.l.src[i];
         if (src < 0) continue;
+        if (a.row_bytes[arr] < 0) {  // a record: whole, where anything of the page is kept
+            const int bytes = a.l.rows[i] ? -a.row_bytes[arr] : 0;
+            const char* s = a.data[arr] + ((int64_t)src * a.blocks[arr] + blk) * -a.row_bytes[arr];
+            char* d = a.data[arr] + ((int64_t)a.l.dst[i] * a.blocks[arr] + blk) * -a.row_bytes[arr];
+            if (a.row_bytes[arr] % 16 == 0)
+                for (int x = 16 * lane; x < bytes; x += 1024) *(uint4*)(d + x) = *(const uint4*)(s + x);
+            else
+                for (int x = 2 * lane; x < bytes; x += 128) *(uint16_t*)(d + x) = *(const uint16_t*)(s + x);
+            continue;
+        }
         const int64_t page = (int64_t)a.row_bytes[arr] << a.shift;
         const uint4* s = (const uint4*)(a.data[arr] + ((int64_t)src * a.blocks[arr] + blk) * page);
         uint4* d = (uint4*)(a.data[arr] + ((int64_t)a.l.dst[i] * a.blocks[arr] + blk) * page);
@@ -345,11 +355,30 @@ __global__ __launch_bounds__(256) void k_pages_trim(int32_t* table, int32_t* ref
     }
 }
 
+// Entries lo .. hi - 1 of every sequence whose positions no row at lens[b] or behind reads, and no sink is among: a
+// workgroup per kSlideEntries of them, as long tables hold many that were given up before.
+constexpr int kSlideEntries = 2048, kSlideGroups = 64;
+__global__ __launch_bounds__(256) void k_pages_slide(int32_t* table, int32_t* refs, int n_pages, int max_pages, int shift,
+                                                     const int32_t* lens, int window, int sinks, int groups) {
+    const int b = blockIdx.x / groups, len = lens[b];
+    if (len < 0) return;
+    int32_t* row = table + (int64_t)b * max_pages;
+    const int lo = (sinks + (1 << shift) - 1) >> shift, hi = min((int)max((int64_t)len - window + 1, (int64_t)0) >> shift, max_pages);
+    for (int j = lo + blockIdx.x % groups * 256 + threadIdx.x; j < hi; j += groups * 256) {
+        const int p = row[j];
+        if ((uint32_t)p < (uint32_t)n_pages) atomicSub(refs + p, 1);
+        row[j] = -1;
+    }
+}
+
 int shift_of(int page_size) {
     for (int s = 4; s <= 10; ++s)
         if (page_size == 1 << s) return s;
     return -1;
 }
+
+// Bytes of a record (an array without rows) at most.
+constexpr int32_t kRecordBytes = 1 << 20;
 
 bool aligned(const void* p, size_t n) { return p && (uintptr_t)p % n == 0; }
 
@@ -387,8 +416,8 @@ bool pages_ok(const sd2_pages* p) {
         return false;
     for (int i = 0; i < p->n_arrays; ++i) {
         const sd2_page_array& a = p->arrays[i];
-        if (!aligned(a.data, 16) || a.blocks < 1 || a.blocks > 65536 || a.row_bytes < 16 || a.row_bytes > 65536 ||
-            a.row_bytes % 16)
+        if (!aligned(a.data, 16) || a.blocks < 1 || a.blocks > 65536) return false;
+        if (a.row_bytes < 0 ? a.row_bytes < -kRecordBytes || a.row_bytes % 2 : a.row_bytes < 16 || a.row_bytes > 65536 || a.row_bytes % 16)
             return false;
     }
     return true;
@@ -420,6 +449,12 @@ hipError_t pages_fork(hipStream_t s, const sd2_pages& p, int n, const int32_t* s
 hipError_t pages_trim(hipStream_t s, const sd2_pages& p, int nseq, const int32_t* lens) {
     return launch(k_pages_trim, dim3(nseq), dim3(256), s, p.table, p.refs, (int)p.n_pages, (int)p.max_pages,
                   shift_of(p.page_size), lens);
+}
+
+hipError_t pages_slide(hipStream_t s, const sd2_pages& p, int nseq, const int32_t* lens, int window, int sinks) {
+    const int groups = std::min((p.max_pages + kSlideEntries - 1) / kSlideEntries, kSlideGroups);
+    return launch(k_pages_slide, dim3(nseq * groups), dim3(256), s, p.table, p.refs, (int)p.n_pages, (int)p.max_pages,
+                  shift_of(p.page_size), lens, window, sinks, groups);
 }
 
 hipError_t pages_compact(hipStream_t s, const sd2_pages& p, int32_t* live, void* ws) {
@@ -455,19 +490,29 @@ sd2_status device_ok() {
 
 sd2_status status_of(hipError_t err) { return err == hipSuccess ? SD2_OK : SD2_ERR_HIP; }
 
-bool view_of(const sd2_paged_kv* kv, PagedView* c, int* size) {
+// held: bytes of an element of the cache, where they are not the rows' (0)
+bool view_of(const sd2_paged_kv* kv, PagedView* c, int* size, int held = 0) {
     if (!kv || (kv->dtype != SD2_F32 && kv->dtype != SD2_BF16)) return false;
     *size = kv->dtype == SD2_BF16 ? 2 : 4;
+    if (!held) held = *size;
     const int shift = shift_of(kv->page_size);
     if (shift < 0 || kv->n_pages < 1 || kv->n_pages > 1 << 24 || kv->n_kv_heads < 1 || kv->n_kv_heads > 1024 ||
         (kv->head_dim != 32 && kv->head_dim != 64 && kv->head_dim != 128) || kv->max_pages < 1 ||
         (int64_t)kv->max_pages * kv->page_size > 1 << 30 || !aligned(kv->k, 16) || !aligned(kv->v, 16) ||
         !aligned(kv->table, 4))
         return false;
-    if (kv->page_stride < (int64_t)kv->n_kv_heads * kv->page_size * kv->head_dim || kv->page_stride % (16 / *size) ||
+    if (kv->page_stride < (int64_t)kv->n_kv_heads * kv->page_size * kv->head_dim || kv->page_stride % (16 / held) ||
         kv->page_stride > (int64_t)1 << 40)
         return false;
-    *c = PagedView{kv->k, kv->v, kv->page_stride, kv->n_pages, shift, kv->n_kv_heads, kv->head_dim, kv->table, kv->max_pages};
+    *c = PagedView{kv->k, kv->v, kv->page_stride, kv->n_pages, shift, kv->n_kv_heads, kv->head_dim, kv->table, kv->max_pages, nullptr, 0};
+    return true;
+}
+bool view_of(const sd2_paged_scaled* kv, PagedView* c, int* size) {
+    if (!kv || !view_of(&kv->kv, c, size, 1) || !aligned(kv->scales, 2) || kv->scale_stride % 2 ||
+        kv->scale_stride < (int64_t)c->Hkv << (c->shift - 3) || kv->scale_stride > (int64_t)1 << 40)
+        return false;
+    c->scales = (uint8_t*)kv->scales;
+    c->scale_stride = kv->scale_stride;
     return true;
 }
 
@@ -494,6 +539,45 @@ bool overlap(const void* p, int64_t ps, const void* q, int64_t qs, int64_t n, in
     if (ps != qs || n == 1) return true;
     const int64_t gap = (int64_t)((d % ps + ps) % ps);
     return gap < width || gap > ps - width;
+}
+
+constexpr int32_t kMostPositions = 1 << 30;
+
+// The attention calls, of either kind of cache.
+template <typename KV>
+size_t attn_bytes(const KV* kv, const sd2_paged_rows* rows, int32_t n_heads, int32_t max_len, int32_t window, int32_t sinks) {
+    PagedView c;
+    PagedRows r;
+    int size;
+    if (!view_of(kv, &c, &size) || !rows_of(rows, &r) || n_heads < 1 || n_heads > 1024 || n_heads % c.Hkv) return 0;
+    if ((int64_t)r.max_rows * (n_heads / c.Hkv) > 1 << 30) return 0;
+    if (max_len < 1 || max_len > (int64_t)c.max_pages << c.shift) return 0;
+    if (window < 0 || window > kMostPositions || sinks < 0 || sinks > kMostPositions) return 0;
+    return paged_attn_bytes(c, r, n_heads, size == 2, max_len, window, sinks);
+}
+template <typename KV>
+sd2_status attn_call(const KV* kv, const sd2_paged_rows* rows, const void* q, int64_t q_stride, void* out, int64_t out_stride,
+                     int32_t n_heads, float scale, int32_t max_len, int32_t window, int32_t sinks, void* workspace,
+                     size_t workspace_bytes, void* hip_stream) {
+    PagedAttnArgs a{};
+    int size;
+    if (!view_of(kv, &a.c, &size) || !rows_of(rows, &a.r)) return SD2_ERR_INVALID_ARG;
+    if (n_heads < 1 || n_heads > 1024 || n_heads % a.c.Hkv || !(scale >= -1e30f && scale <= 1e30f)) return SD2_ERR_INVALID_ARG;
+    if (max_len < 1 || max_len > (int64_t)a.c.max_pages << a.c.shift) return SD2_ERR_INVALID_ARG;
+    if (window < 0 || window > kMostPositions || sinks < 0 || sinks > kMostPositions) return SD2_ERR_INVALID_ARG;
+    if ((int64_t)a.r.max_rows * (n_heads / a.c.Hkv) > 1 << 30) return SD2_ERR_INVALID_ARG;
+    if (!a.r.nseq || !a.r.total_rows) return SD2_OK;
+    const int64_t width = (int64_t)n_heads * a.c.hd;
+    if (!strided(q, q_stride, width, size) || !strided(out, out_stride, width, size) ||
+        overlap(q, q_stride, out, out_stride, a.r.total_rows, width, size))
+        return SD2_ERR_INVALID_ARG;
+    const size_t need = paged_attn_bytes(a.c, a.r, n_heads, size == 2, max_len, window, sinks);
+    if (!need || !aligned(workspace, 256) || workspace_bytes < need) return SD2_ERR_INVALID_ARG;
+    const sd2_status st = device_ok();
+    if (st != SD2_OK) return st;
+    a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.H = n_heads; a.scale = scale;
+    a.window = window; a.sinks = sinks;
+    return status_of(paged_attn((hipStream_t)hip_stream, a, size == 2, max_len, workspace, workspace_bytes));
 }
 
 }  // namespace
@@ -566,35 +650,56 @@ sd2_status sd2_paged_append(const sd2_paged_kv* kv, const sd2_paged_rows* rows, 
 
 size_t sd2_paged_attn_workspace_bytes(const sd2_paged_kv* kv, const sd2_paged_rows* rows, int32_t n_heads,
                                       int32_t max_len) {
-    PagedView c;
-    PagedRows r;
-    int size;
-    if (!view_of(kv, &c, &size) || !rows_of(rows, &r) || n_heads < 1 || n_heads > 1024 || n_heads % c.Hkv) return 0;
-    if ((int64_t)r.max_rows * (n_heads / c.Hkv) > 1 << 30) return 0;
-    if (max_len < 1 || max_len > (int64_t)c.max_pages << c.shift) return 0;
-    return paged_attn_bytes(c, r, n_heads, size == 2, max_len);
+    return attn_bytes(kv, rows, n_heads, max_len, 0, 0);
 }
-
 sd2_status sd2_paged_attn(const sd2_paged_kv* kv, const sd2_paged_rows* rows, const void* q, int64_t q_stride,
                           void* out, int64_t out_stride, int32_t n_heads, float scale, int32_t max_len,
                           void* workspace, size_t workspace_bytes, void* hip_stream) {
-    PagedAttnArgs a{};
+    return attn_call(kv, rows, q, q_stride, out, out_stride, n_heads, scale, max_len, 0, 0, workspace, workspace_bytes, hip_stream);
+}
+
+size_t sd2_paged_attn_window_workspace_bytes(const sd2_paged_kv* kv, const sd2_paged_rows* rows, int32_t n_heads,
+                                             int32_t max_len, int32_t window, int32_t sinks) {
+    return attn_bytes(kv, rows, n_heads, max_len, window, sinks);
+}
+sd2_status sd2_paged_attn_window(const sd2_paged_kv* kv, const sd2_paged_rows* rows, const void* q, int64_t q_stride,
+                                 void* out, int64_t out_stride, int32_t n_heads, float scale, int32_t max_len,
+                                 int32_t window, int32_t sinks, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    return attn_call(kv, rows, q, q_stride, out, out_stride, n_heads, scale, max_len, window, sinks, workspace, workspace_bytes, hip_stream);
+}
+
+size_t sd2_paged_attn_scaled_workspace_bytes(const sd2_paged_scaled* kv, const sd2_paged_rows* rows, int32_t n_heads,
+                                       int32_t max_len, int32_t window, int32_t sinks) {
+    return attn_bytes(kv, rows, n_heads, max_len, window, sinks);
+}
+sd2_status sd2_paged_attn_scaled(const sd2_paged_scaled* kv, const sd2_paged_rows* rows, const void* q, int64_t q_stride,
+                           void* out, int64_t out_stride, int32_t n_heads, float scale, int32_t max_len,
+                           int32_t window, int32_t sinks, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    return attn_call(kv, rows, q, q_stride, out, out_stride, n_heads, scale, max_len, window, sinks, workspace, workspace_bytes, hip_stream);
+}
+
+sd2_status sd2_paged_append_scaled(const sd2_paged_scaled* kv, const sd2_paged_rows* rows, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, void* hip_stream) {
+    PagedView c;
+    PagedRows r;
     int size;
-    if (!view_of(kv, &a.c, &size) || !rows_of(rows, &a.r)) return SD2_ERR_INVALID_ARG;
-    if (n_heads < 1 || n_heads > 1024 || n_heads % a.c.Hkv || !(scale >= -1e30f && scale <= 1e30f)) return SD2_ERR_INVALID_ARG;
-    if (max_len < 1 || max_len > (int64_t)a.c.max_pages << a.c.shift) return SD2_ERR_INVALID_ARG;
-    if ((int64_t)a.r.max_rows * (n_heads / a.c.Hkv) > 1 << 30) return SD2_ERR_INVALID_ARG;
-    if (!a.r.nseq || !a.r.total_rows) return SD2_OK;
-    const int64_t width = (int64_t)n_heads * a.c.hd;
-    if (!strided(q, q_stride, width, size) || !strided(out, out_stride, width, size) ||
-        overlap(q, q_stride, out, out_stride, a.r.total_rows, width, size))
-        return SD2_ERR_INVALID_ARG;
-    const size_t need = paged_attn_bytes(a.c, a.r, n_heads, size == 2, max_len);
-    if (!need || !aligned(workspace, 256) || workspace_bytes < need) return SD2_ERR_INVALID_ARG;
+    if (!view_of(kv, &c, &size) || !rows_of(rows, &r)) return SD2_ERR_INVALID_ARG;
+    if (!r.nseq || !r.total_rows) return SD2_OK;
+    const int64_t width = (int64_t)c.Hkv * c.hd;
+    if (!strided(k, k_stride, width, size) || !strided(v, v_stride, width, size)) return SD2_ERR_INVALID_ARG;
     const sd2_status st = device_ok();
     if (st != SD2_OK) return st;
-    a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.H = n_heads; a.scale = scale;
-    return status_of(paged_attn((hipStream_t)hip_stream, a, size == 2, max_len, workspace, workspace_bytes));
+    return status_of(paged_append8((hipStream_t)hip_stream, c, r, k, k_stride, v, v_stride, size == 2));
+}
+
+sd2_status sd2_pages_slide(const sd2_pages* pages, int32_t nseq, const int32_t* lens, int32_t window, int32_t sinks,
+                           void* hip_stream) {
+    if (!pages_ok(pages) || nseq < 0 || nseq > pages->max_seqs || (nseq && !aligned(lens, 4))) return SD2_ERR_INVALID_ARG;
+    if (window < 1 || window > kMostPositions || sinks < 0 || sinks > kMostPositions) return SD2_ERR_INVALID_ARG;
+    if (!nseq) return SD2_OK;
+    const sd2_status st = device_ok();
+    if (st != SD2_OK) return st;
+    return status_of(pages_slide((hipStream_t)hip_stream, *pages, nseq, lens, window, sinks));
 }
 
 }  // extern "C"

@@ -8,6 +8,13 @@
     cache.fork([0], [1])                             # sequence 1 goes on from sequence 0's pages
     cache.trim(lens)                                 # pages behind these lengths become free
 
+A cache of dtype=torch.float8_e4m3fn holds 8 bits a value, with a power of two for every 16 positions of a layer and KV
+head; rows, q and out are then float32 or bfloat16, whichever a call brings.  Under a window a row reads the last
+positions and a few first ones only, and the pages between can be given up:
+
+    out = cache.attend(q, lens, layer=l, window=4096, sinks=4)
+    cache.slide(lens, window=4096, sinks=4)          # pages that no later row reads become free
+
 Sequences are rows of the table; lens, first, last, keep, row_off are int32 tensors on the cache's
 device (their values are not read here: the calls do not wait for the GPU).  Every call runs on the
 current stream of that device.
@@ -21,6 +28,9 @@ from torch.autograd import forward_ad
 from . import binding as B
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+HELD8, SCALES = torch.float8_e4m3fn, torch.float8_e8m0fnu
+BLOCK = 16  # positions that share a power of two
+MOST_POSITIONS = 1 << 30
 # the current stream of a device, as HIP's handle (torch's own shortcut to it where there is one: a
 # microsecond less per call)
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -37,13 +47,15 @@ def _tangent(t):
 
 
 class PagedCache:
-    """k and v: contiguous [n_pages][n_layers][n_kv_heads][page_size][head_dim], float32 or bfloat16;
+    """k and v: contiguous [n_pages][n_layers][n_kv_heads][page_size][head_dim], float32, bfloat16 or float8_e4m3fn;
     table: contiguous int32 [max_seqs][max_pages], -1 where there is no page; refs: int32 [n_pages],
-    the table entries that name each page.  The cache works on these tensors and keeps them."""
+    the table entries that name each page; scales (float8_e4m3fn only): contiguous float8_e8m0fnu
+    [n_pages][n_layers][n_kv_heads][page_size / 16][2], the powers of two of k and of v.  The cache works on these
+    tensors and keeps them."""
 
-    def __init__(self, k, v, table, refs):
-        _need(k.is_cuda and k.dim() == 5 and k.dtype in DTYPES, "k: a float32 or bfloat16 GPU tensor "
-              "[n_pages][n_layers][n_kv_heads][page_size][head_dim]")
+    def __init__(self, k, v, table, refs, scales=None):
+        _need(k.is_cuda and k.dim() == 5 and (k.dtype in DTYPES or k.dtype == HELD8), "k: a float32, bfloat16 or "
+              "float8_e4m3fn GPU tensor [n_pages][n_layers][n_kv_heads][page_size][head_dim]")
         _need(v.shape == k.shape and v.dtype == k.dtype and v.device == k.device, "v has to be like k")
         _need(k.is_contiguous() and v.is_contiguous(), "k and v have to be contiguous")
         _need(not any(t.requires_grad or _tangent(t) for t in (k, v)), "k and v: no gradients here (detach them)")
@@ -51,7 +63,14 @@ class PagedCache:
         self._int32(refs, 1, "refs", k.device)
         n_pages, n_layers, n_kv, page, hd = k.shape
         _need(refs.numel() == n_pages, "refs: one for every page")
-        self.k, self.v, self.table, self.refs = k, v, table, refs
+        self.held8 = k.dtype == HELD8
+        if self.held8:
+            _need(isinstance(scales, torch.Tensor) and scales.dtype == SCALES and scales.device == k.device and
+                  page % BLOCK == 0 and scales.shape == (n_pages, n_layers, n_kv, page // BLOCK, 2) and scales.is_contiguous(),
+                  "scales: a contiguous float8_e8m0fnu tensor [n_pages][n_layers][n_kv_heads][page_size / 16][2] on k's device")
+        else:
+            _need(scales is None, "scales: only float8_e4m3fn caches have them")
+        self.k, self.v, self.table, self.refs, self.scales = k, v, table, refs, scales
         self.device, self.dtype = k.device, k.dtype
         self._index, self._sizes = k.device.index, {}
         self._unused = torch.empty(256, dtype=torch.uint8, device=k.device)  # workspace of calls that need none
@@ -59,26 +78,36 @@ class PagedCache:
         self.max_seqs, self.max_pages = table.shape
         self.lib = B.load()
         size = k.element_size()
-        pages = B.Pages(page, n_pages, self.max_seqs, self.max_pages, table.data_ptr(), refs.data_ptr(), 2)
+        pages = B.Pages(page, n_pages, self.max_seqs, self.max_pages, table.data_ptr(), refs.data_ptr(), 3 if self.held8 else 2)
         for i, pool in enumerate((k, v)):
             pages.arrays[i] = B.PageArray(pool.data_ptr(), n_layers * n_kv, hd * size)
+        record = n_kv * (page // BLOCK) * 2  # bytes of the scales of a page and layer
+        if self.held8:
+            pages.arrays[2] = B.PageArray(scales.data_ptr(), n_layers, -record)
         self._pages = pages
         self._pages_ws = self.lib.sd2_pages_workspace_bytes(ctypes.byref(pages))
         _need(self._pages_ws > 0, "the cache's sizes are outside what sd2_pages takes")
         self._scale = 1.0 / math.sqrt(hd)
         layer = n_kv * page * hd
-        self._kv = [B.PagedKv(k.data_ptr() + l * layer * size, v.data_ptr() + l * layer * size, n_layers * layer,
-                              DTYPES[k.dtype], page, n_pages, n_kv, hd, self.max_pages, table.data_ptr())
-                    for l in range(n_layers)]
+        # for a dtype of a call's rows: a layer's view of the cache
+        self._kv = {t: [B.PagedKv(k.data_ptr() + l * layer * size, v.data_ptr() + l * layer * size, n_layers * layer,
+                                  DTYPES[t], page, n_pages, n_kv, hd, self.max_pages, table.data_ptr())
+                        for l in range(n_layers)] for t in (DTYPES if self.held8 else (k.dtype,))}
+        if self.held8:
+            self._kv = {t: [B.PagedScaled(kv, scales.data_ptr() + l * record, n_layers * record) for l, kv in enumerate(kvs)]
+                        for t, kvs in self._kv.items()}
 
     @classmethod
     def empty(cls, n_pages, page_size, n_layers, n_kv_heads, head_dim, max_seqs, max_pages, dtype=torch.bfloat16,
               device="cuda"):
         """A cache of free pages and no sequences."""
         shape = (n_pages, n_layers, n_kv_heads, page_size, head_dim)
+        scales = None
+        if dtype == HELD8:
+            scales = torch.empty((n_pages, n_layers, n_kv_heads, page_size // BLOCK, 2), dtype=SCALES, device=device)
         return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device),
                    torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device),
-                   torch.zeros(n_pages, dtype=torch.int32, device=device))
+                   torch.zeros(n_pages, dtype=torch.int32, device=device), scales)
 
     # ---- checks ------------------------------------------------------------------------------------
     @staticmethod
@@ -86,14 +115,14 @@ class PagedCache:
         _need(isinstance(t, torch.Tensor) and t.dtype == torch.int32 and t.dim() == dim and t.device == device and
               t.is_contiguous(), f"{what}: a contiguous int32 tensor of {dim} dimension(s) on the cache's device")
 
-    def _layer(self, layer):
+    def _layer(self, layer, like):
         _need(isinstance(layer, int) and 0 <= layer < self.n_layers, f"layer {layer} of {self.n_layers}")
-        return ctypes.byref(self._kv[layer])
+        return ctypes.byref(self._kv[like.dtype][layer])
 
     def _packed(self, t, what):
         """A tensor [rows][heads][head_dim] whose rows may be apart: its row stride."""
-        _need(isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == self.dtype and t.dim() == 3 and
-              t.shape[2] == self.head_dim, f"{what}: [rows][heads][head_dim] of the cache's type, on its device")
+        _need(isinstance(t, torch.Tensor) and t.device == self.device and t.dtype in self._kv and t.dim() == 3 and
+              t.shape[2] == self.head_dim, f"{what}: [rows][heads][head_dim] of the cache's type (float32 or bfloat16 for 8 bits), on its device")
         _need(not t.requires_grad or not torch.is_grad_enabled(), f"{what}: no gradients here (torch.no_grad(), or detach it)")
         _need(not _tangent(t), f"{what}: no forward-mode tangents here (take its primal)")
         if t.numel():
@@ -125,6 +154,11 @@ class PagedCache:
         _need(n <= self.max_seqs, f"{what}: {n} sequences, the table has {self.max_seqs}")
         return n
 
+    @staticmethod
+    def _window(window, sinks):
+        _need(isinstance(window, int) and 1 <= window <= MOST_POSITIONS, f"window {window}: 1 to 2^30 positions")
+        _need(isinstance(sinks, int) and 0 <= sinks <= MOST_POSITIONS, f"sinks {sinks}: 0 to 2^30 positions")
+
     def _workspace(self, nbytes):
         return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
@@ -143,19 +177,22 @@ class PagedCache:
         """Write rows k, v [rows][n_kv_heads][head_dim] to their positions (sd2_paged_append): those of
         sequence b are the last ones of its lens[b] positions, rows row_off[b] .. row_off[b + 1] - 1, or
         without row_off an equal number for every sequence."""
-        kv = self._layer(layer)
         ks, vs = self._packed(k, "k"), self._packed(v, "v")
+        kv = self._layer(layer, k)
+        _need(k.dtype == v.dtype, "k and v: one type")
         _need(k.shape == v.shape and k.shape[1] == self.n_kv_heads, "k and v: [rows][n_kv_heads][head_dim]")
         rows = self._rows(k.shape[0], lens, row_off, max_rows)
-        self._call(self.lib.sd2_paged_append, kv, ctypes.byref(rows), k.data_ptr(), ks, v.data_ptr(), vs)
+        self._call(self.lib.sd2_paged_append_scaled if self.held8 else self.lib.sd2_paged_append, kv, ctypes.byref(rows), k.data_ptr(),
+                   ks, v.data_ptr(), vs)
 
-    def attend(self, q, lens, layer=0, row_off=None, max_rows=None, max_len=None, scale=None, out=None):
+    def attend(self, q, lens, layer=0, row_off=None, max_rows=None, max_len=None, scale=None, out=None, window=None, sinks=0):
         """Causal attention of rows q [rows][heads][head_dim] over their sequences' pages
         (sd2_paged_attn), rows and positions as in append; returns out, like q.  scale: 1 / sqrt(head_dim)
         unless given; max_rows, max_len: the most rows and the largest length, where they are known (they
-        decide how the work is split)."""
-        kv = self._layer(layer)
+        decide how the work is split).  With a window a row reads the last `window` positions up to its own and the
+        first `sinks` ones (sd2_paged_attn_window); caches of 8 bits: sd2_paged_attn_scaled."""
         qs = self._packed(q, "q")
+        kv = self._layer(layer, q)
         heads = q.shape[1]
         _need(heads > 0 and heads % self.n_kv_heads == 0, f"{heads} heads on {self.n_kv_heads} KV heads")
         if out is None:
@@ -165,22 +202,33 @@ class PagedCache:
             _need(isinstance(out, torch.Tensor) and out.shape == q.shape, "out has to be like q")
             _need(not q.numel() or out.data_ptr() != q.data_ptr(), "out must not be q")
             os = self._packed(out, "out")
+            _need(out.dtype == q.dtype, "out has to be like q")
+        if window is None:
+            _need(sinks == 0, "sinks: only with a window")
+            window = 0
+        else:
+            self._window(window, sinks)
         rows = self._rows(q.shape[0], lens, row_off, max_rows)
         if max_len is None:
             max_len = self.max_pages * self.page_size
-        key = (heads, rows.nseq, rows.max_rows, rows.total_rows, row_off is None, max_len)
+        size, call, more = self.lib.sd2_paged_attn_workspace_bytes, self.lib.sd2_paged_attn, ()
+        if self.held8:
+            size, call, more = self.lib.sd2_paged_attn_scaled_workspace_bytes, self.lib.sd2_paged_attn_scaled, (window, sinks)
+        elif window:
+            size, call, more = self.lib.sd2_paged_attn_window_workspace_bytes, self.lib.sd2_paged_attn_window, (window, sinks)
+        key = (heads, rows.nseq, rows.max_rows, rows.total_rows, row_off is None, max_len, q.dtype, *more)
         nbytes = self._sizes.get(key)
         if nbytes is None:
             _need(1 <= max_len <= self.max_pages * self.page_size, f"max_len {max_len} of {self.max_pages} pages")
-            nbytes = self.lib.sd2_paged_attn_workspace_bytes(kv, ctypes.byref(rows), heads, max_len)
+            nbytes = size(kv, ctypes.byref(rows), heads, max_len, *more)
             _need(nbytes > 0, "attend: sizes outside what sd2_paged_attn takes")
             if len(self._sizes) > 1000:
                 self._sizes.clear()
             self._sizes[key] = nbytes
         # (the smallest size is that of calls without partial sums)
         ws = self._unused if nbytes == 256 else self._workspace(nbytes)
-        self._call(self.lib.sd2_paged_attn, kv, ctypes.byref(rows), q.data_ptr(), qs, out.data_ptr(), os, heads,
-                   self._scale if scale is None else scale, max_len, ws.data_ptr(), nbytes)
+        self._call(call, kv, ctypes.byref(rows), q.data_ptr(), qs, out.data_ptr(), os, heads,
+                   self._scale if scale is None else scale, max_len, *more, ws.data_ptr(), nbytes)
         return out
 
     # ---- pages -------------------------------------------------------------------------------------
@@ -209,6 +257,13 @@ class PagedCache:
         a negative length: all)."""
         n = self._seqs("lens", lens)
         self._call(self.lib.sd2_pages_trim, ctypes.byref(self._pages), n, lens.data_ptr())
+
+    def slide(self, lens, window, sinks=0):
+        """Sequences 0 .. len(lens) - 1 give up the pages that, under this window, no row from position lens[b] on
+        reads (sd2_pages_slide; a negative length: none)."""
+        self._window(window, sinks)
+        n = self._seqs("lens", lens)
+        self._call(self.lib.sd2_pages_slide, ctypes.byref(self._pages), n, lens.data_ptr(), window, sinks)
 
     def compact(self):
         """Move the pages in use to the front (sd2_pages_compact); returns their number, int32 [1]."""

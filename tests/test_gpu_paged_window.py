@@ -1,0 +1,251 @@
+"""Attention under a window with first positions that stay visible, pages given up behind it, and the calls of a
+generation that streams on, together."""
+import math
+
+import pytest
+import torch
+
+from paged_ref import make_cache, rows_of
+from paged_scaled_ref import attend64, check, make_scaled
+
+pytestmark = pytest.mark.gpu
+T = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def rand(*shape, dtype, seed, by=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * by).to(dtype).cuda()
+
+
+SHAPES = [(8, 8, 64, 16, [1], 1), (32, 8, 64, 16, [517], 1), (8, 2, 128, 32, [5, 300, 64, 17], 1), (4, 4, 32, 16, [700, 33], 5),
+          (16, 2, 128, 64, [129, 64, 1000], 4), (8, 1, 64, 256, [2000, 1, 255], 8), (6, 2, 32, 32, [200, 90], 33),
+          (8, 1, 128, 16, [150], 40), (16, 2, 64, 64, [300, 65], 0), (4, 2, 128, 16, [513, 40, 1], 0), (3, 1, 32, 128, [300], 0),
+          (8, 8, 128, 64, [600, 450], -1), (2, 1, 64, 64, [1500], 0)]
+
+
+def rows_in(lens, rows):
+    return [min(rows, n) for n in lens] if rows > 0 else list(lens) if rows == 0 else [1 + (n - 1) * (3 + i) // 9 for i, n in enumerate(lens)]
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 16), (50, 4), (129, 17), (300, 0), (7, 400), (5000, 1)])
+@pytest.mark.parametrize("h,hkv,hd,page,lens,rows", SHAPES, ids=str)
+def test_window(dtype, h, hkv, hd, page, lens, rows, window, sinks):
+    cache = make_cache(lens, T[dtype], hkv, hd, page, layers=2, seed=hd + len(lens))
+    rows = rows_in(lens, rows)
+    q = rand(sum(rows), h, hd, dtype=T[dtype], seed=9)
+    dl, off = rows_of(lens, rows, packed=min(rows) < max(rows))
+    got = cache.attend(q, dl, layer=1, row_off=off, window=window, sinks=sinks)
+    check(got, cache, q, lens, rows, layer=1, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("max_len", [3000, 40000])
+def test_window_of_long_sequences_that_are_split(dtype, max_len):
+    lens = [3000, 1, 2500, 777]
+    cache = make_cache(lens, T[dtype], 2, 64, 64, extra_entries=700, seed=1)
+    for window, sinks in ((2000, 5), (900, 70), (64, 0)):
+        for rows in (1, 12, 70):
+            r = [min(rows, n) for n in lens]
+            q = rand(sum(r), 8, 64, dtype=T[dtype], seed=rows)
+            dl, off = rows_of(lens, r, True)
+            check(cache.attend(q, dl, row_off=off, max_len=max_len, window=window, sinks=sinks), cache, q, lens, r, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("rows,g", [(1, 1), (4, 2), (16, 4), (70, 4), (130, 1)])
+@pytest.mark.parametrize("window,sinks", [(20, 2), (33, 0), (3, 100)])
+def test_infinities_and_nan_reach_the_rows_that_read_them(dtype, rows, g, window, sinks):
+    lens = [220, 200]
+    cache = make_cache(lens, T[dtype], 2, 64, 16, seed=8)
+    for n, (j, x) in enumerate([(1, math.inf), (55, math.nan), (140, -math.inf), (150, math.inf), (199, math.nan), (218, math.inf)]):
+        for b in range(2):
+            if j < lens[b]:
+                cache.v[int(cache.table[b, j // 16]), 0, b, j % 16, (7 * n + b) % 64] = x
+    q = rand(2 * rows, 2 * g, 64, dtype=T[dtype], seed=2)
+    dl, _ = rows_of(lens, [rows, rows], False)
+    check(cache.attend(q, dl, window=window, sinks=sinks), cache, q, lens, [rows, rows], window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("rows", [1, 5, 90])
+def test_rows_that_read_nothing_and_rows_whose_scores_are_all_infinite(dtype, rows):
+    lens = [200, 200, 200]
+    cache = make_cache(lens, T[dtype], 1, 32, 16, seed=3)
+    cache.table[0, 2:] = -1   # the pages behind the sinks given up, and the window's missing: sinks only
+    cache.table[1, :] = -1    # nothing: zeros
+    cache.table[2, :4] = -1   # without sinks
+    q = rand(3 * rows, 2, 32, dtype=T[dtype], seed=2)
+    dl, _ = rows_of(lens, [rows] * 3, False)
+    for window, sinks in ((30, 4), (30, 0)):
+        check(cache.attend(q, dl, window=window, sinks=sinks), cache, q, lens, [rows] * 3, window=window, sinks=sinks)
+    # scores of -inf: NaN where a row reads any such position and no other
+    cache.k[:] = 1.0
+    q[:] = -math.inf
+    got = cache.attend(q, dl, window=30, sinks=4).view(3, rows, 2, 32)
+    assert bool(got[0].isnan().all()) and bool((got[1] == 0).all()) and bool(got[2].isnan().all())
+    got = cache.attend(q, dl, window=30, sinks=0).view(3, rows, 2, 32)
+    for i in range(rows):  # sequence 0 has positions 0 .. 31 only
+        assert bool((got[0, i] == 0).all()) == (200 - rows + i - 29 > 31) and bool(got[2, i].isnan().all())
+
+
+def slide_model(table, refs, lens, window, sinks, page):
+    for b, n in enumerate(lens):
+        if n < 0:
+            continue
+        for j, p in enumerate(table[b]):
+            at = range(j * page, j * page + page)
+            if at[0] >= sinks and at[-1] <= n - window:
+                if 0 <= p < len(refs):
+                    refs[p] -= 1
+                table[b][j] = -1
+    return table, refs
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 16), (33, 17), (64, 0), (100, 64), (10 ** 9, 0), (1, 10 ** 9)])
+def test_slide(page, window, sinks):
+    lens = [0, 1, 16, 64, 65, 200, 515]
+    cache = make_cache(lens, torch.bfloat16, 1, 32, page, extra_entries=3, seed=2)
+    cache.table[5, 1], cache.table[6, 2] = -1, 1 << 24
+    ask = [0, 5, -1, 64, 2 ** 31 - 1, 200, 400]
+    want = slide_model(cache.table.tolist(), cache.refs.tolist(), ask, window, sinks, page)
+    k = cache.k.clone()
+    cache.slide(torch.tensor(ask, dtype=torch.int32, device="cuda"), window, sinks)
+    assert (cache.table.tolist(), cache.refs.tolist()) == want
+    assert torch.equal(cache.k.view(torch.int16), k.view(torch.int16))
+    cache.slide(torch.tensor(ask[:3], dtype=torch.int32, device="cuda"), window, sinks)
+    assert (cache.table.tolist(), cache.refs.tolist()) == want
+
+
+def test_slide_of_shared_pages_and_long_tables():
+    cache = make_cache([20000, 0, 0], torch.bfloat16, 1, 32, 16, extra_entries=5000, seed=2)
+    cache.fork([0, 0], [1, 2])
+    want = slide_model(cache.table.tolist(), cache.refs.tolist(), [19000, 20000, -1], 100, 20, 16)
+    cache.slide(torch.tensor([19000, 20000, -1], dtype=torch.int32, device="cuda"), 100, sinks=20)
+    assert (cache.table.tolist(), cache.refs.tolist()) == want
+
+
+@pytest.mark.parametrize("held", ["bf16", "f32", "8"])
+def test_a_generation_streams_on_in_few_pages(held):
+    """slide, reserve, append and attend as a stream of tokens uses them, in a pool that could not hold all of it: each
+    step's rows against attention over everything that was ever written."""
+    from paper_2511_09844_amd.paged import PagedCache
+    dtype = torch.float32 if held == "8" else T[held]
+    pool = torch.float8_e4m3fn if held == "8" else dtype
+    window, sinks, page, hkv, h, hd, seqs = 40, 3, 16, 2, 4, 64, 2
+    # a sequence holds a page of sinks, those of the window and of a step
+    few = PagedCache.empty(seqs * (1 + 4 + 1), page, 1, hkv, hd, seqs, 40, dtype=pool)
+    all_ = PagedCache.empty(seqs * 40, page, 1, hkv, hd, seqs, 40, dtype=pool)
+    lens = [0] * seqs
+
+    def ints(v):
+        return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+    for step, n in enumerate([21, 9, 1, 1, 5, 16, 1, 30, 2, 1, 8, 17, 1, 40, 3] * 2):
+        rows = [n, max(1, n // 2)]
+        new = [a + r for a, r in zip(lens, rows)]
+        k, v, q = (rand(sum(rows), x, hd, dtype=dtype, seed=10 * step + i, by=1 + step % 4) for i, x in enumerate((hkv, hkv, h)))
+        off = ints([0, rows[0], sum(rows)])
+        outs = []
+        for cache in (few, all_):
+            if cache is few:
+                cache.slide(ints(lens), window, sinks)
+            assert cache.reserve(ints(lens), ints(new)).tolist() == new
+            cache.append(k, v, ints(new), row_off=off)
+            outs.append(cache.attend(q, ints(new), row_off=off, window=window, sinks=sinks))
+        lens = new
+        check(outs[0], few, q, lens, rows, window=window, sinks=sinks)
+        check(outs[1], all_, q, lens, rows, window=window, sinks=sinks)
+        # the pages given up change nothing, but for the order of the float64 sums: of hd products in a score, whose
+        # error its exponential takes over, and of up to max(lens) weights above and below the fraction, 2^-53 each
+        (a, absv, spread), (b, _, _) = (attend64(c, q, lens, rows, window=window, sinks=sinks) for c in (few, all_))
+        rel = 4 * ((hd + 4) * 2.0 ** -53 * (spread + 1) + (max(lens) + 8) * 2.0 ** -53)
+        assert bool(((a - b).abs() <= rel * absv).all())
+    assert lens[0] > 300
+
+
+@pytest.mark.parametrize("held", ["bf16", "8"])
+def test_graphs_replay_with_new_lengths(held):
+    """A step captured once: each replay against an eager call, with eager work and synchronisations between."""
+    lens = [300, 40, 170]
+    make = make_scaled if held == "8" else lambda *a, **k: make_cache(a[0], torch.bfloat16, *a[1:], **k)
+    cache, other = (make([400] * 3, 2, 64, 16, extra_entries=4, seed=4) for _ in range(2))
+    one, many = (torch.empty(3, dtype=torch.int32, device="cuda") for _ in range(2))
+    q, k, v = (rand(3, x, 64, dtype=torch.bfloat16, seed=i) for i, x in enumerate((8, 2, 2)))
+    qp, out = rand(3 * 70, 8, 64, dtype=torch.bfloat16, seed=7), torch.empty_like(q)
+    outp = torch.empty_like(qp)
+
+    def step(c, o, op):
+        c.append(k, v, one)
+        c.attend(q, one, window=100, sinks=4, out=o, max_len=400)
+        c.attend(qp, many, window=100, sinks=4, out=op, max_len=400)
+        c.slide(one, 150, 4)
+
+    one.copy_(torch.tensor(lens)), many.copy_(torch.tensor([400, 399, 71]))
+    side = torch.cuda.Stream()
+    table = cache.table.clone()
+    with torch.cuda.stream(side):
+        step(cache, out, outp)
+    side.synchronize()
+    cache.table.copy_(table), cache.refs.copy_(other.refs)
+    for pool in ("k", "v"):
+        getattr(cache, pool).view(torch.uint8).copy_(getattr(other, pool).view(torch.uint8))
+    if held == "8":
+        cache.scales.view(torch.uint8).copy_(other.scales.view(torch.uint8))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cache, out, outp)
+    for i in range(4):
+        one.copy_(torch.tensor([n + 3 * i for n in lens]))
+        many.copy_(torch.tensor([400, 399 - i, 71 + i]))
+        graph.replay()
+        torch.cuda.synchronize()
+        o, op = torch.empty_like(q), torch.empty_like(qp)
+        step(other, o, op)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in ((o, out), (op, outp)))  # (NaN among them)
+        assert torch.equal(cache.table, other.table) and torch.equal(cache.refs, other.refs)
+        assert torch.equal(cache.k.view(torch.uint8), other.k.view(torch.uint8))
+        q.mul_(1.25)
+
+
+def test_calls_on_two_streams_at_once():
+    caches = [make_scaled([900, 31], 2, 128, 32, seed=s) for s in (1, 2)]
+    q = rand(2 * 8, 8, 128, dtype=torch.float32, seed=1)
+    dl, _ = rows_of([900, 31], [8, 8], False)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in caches], [[] for _ in caches]
+    for _ in range(10):
+        for c, s, o in zip(caches, streams, outs):
+            with torch.cuda.stream(s):
+                o.append(c.attend(q, dl, window=500, sinks=4))
+    torch.cuda.synchronize()
+    for c, o in zip(caches, outs):
+        check(o[0], c, q, [900, 31], [8, 8], window=500, sinks=4)
+        assert all(torch.equal(o[0].view(torch.int32), x.view(torch.int32)) for x in o)
+
+
+def test_refusals():
+    from paper_2511_09844_amd import binding as B
+    from paper_2511_09844_amd.paged import PagedCache
+    c = make_scaled([20], 2, 64, 16)
+    plain = make_cache([20], torch.bfloat16, 2, 64, 16)
+    q, kv = rand(1, 4, 64, dtype=torch.bfloat16, seed=1), rand(1, 2, 64, dtype=torch.bfloat16, seed=1)
+    lens = torch.tensor([20], dtype=torch.int32, device="cuda")
+    bad = [lambda: c.attend(q.half(), lens), lambda: c.attend(q, lens, window=0), lambda: c.attend(q, lens, window=-1),
+           lambda: c.attend(q, lens, sinks=1), lambda: c.attend(q, lens, window=5, sinks=-1), lambda: c.attend(q, lens, window=2.0),
+           lambda: c.attend(q, lens, window=2 ** 30 + 1), lambda: c.attend(q, lens, window=1, sinks=2 ** 30 + 1),
+           lambda: c.attend(q, lens, out=torch.empty(1, 4, 64, device="cuda")), lambda: c.append(kv, kv.float(), lens),
+           lambda: c.append(kv.to(torch.float8_e4m3fn), kv.to(torch.float8_e4m3fn), lens), lambda: plain.attend(q.float(), lens),
+           lambda: c.slide(lens, 0), lambda: c.slide(lens, 5, -1), lambda: c.slide(lens.long(), 5), lambda: c.slide(lens, None),
+           lambda: c.attend(q.clone().requires_grad_(), lens, window=4), lambda: plain.slide(lens.cpu(), 5),
+           lambda: PagedCache(c.k, c.v, c.table, c.refs), lambda: PagedCache(c.k, c.v, c.table, c.refs, scales=c.scales.view(torch.uint8)),
+           lambda: PagedCache(c.k, c.v, c.table, c.refs, scales=c.scales[:1]),
+           lambda: PagedCache(plain.k, plain.v, plain.table, plain.refs, scales=c.scales),
+           lambda: PagedCache(c.k, c.k.to(torch.bfloat16), c.table, c.refs, scales=c.scales)]
+    for i, f in enumerate(bad):
+        with pytest.raises(B.Sd2Error):
+            f()
+            print("not refused:", i)
+    c.attend(q, lens, window=2 ** 30, sinks=2 ** 30)
