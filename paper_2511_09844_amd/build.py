@@ -6,7 +6,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 SO = os.path.join(HERE, "libsd2.so")
 SOURCES = ["csrc/kernels.hip", "csrc/wsgemv.hip", "csrc/pgemm.hip", "csrc/attn.hip", "csrc/mk.hip", "csrc/engine.hip",
-           "csrc/paged_attn.hip", "csrc/paged_attn_plain.hip", "csrc/paged_append8.hip", "csrc/pages.hip"]
+           "csrc/paged_attn.hip", "csrc/paged_attn_window.hip", "csrc/paged_attn_scaled_bf16.hip",
+           "csrc/paged_attn_scaled_f32.hip", "csrc/paged_append8.hip", "csrc/pages.hip"]
 # XNACK off: MI355X runs with page-fault replay disabled by default, and code built for that
 # mode forms longer load clauses than the "any" target (0.9 % less time per round measured)
 ARCH = "gfx950:xnack-"

@@ -47,9 +47,12 @@ struct PagedAttnArgs {
 // Workspace of a call (0: more than can be launched), and the call.  max_len: the largest length expected.  bf16: of
 // q, out and the cache, unless that has scales (else fp32).
 size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, int window = 0, int sinks = 0);
-hipError_t paged_attn_plain(hipStream_t s, const PagedAttnArgs& a, bool bf16);
 // With less than that the keys are split less.
 hipError_t paged_attn(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, void* ws, size_t ws_bytes);
+// Its parts: under a window; over caches with scales, for bf16 and fp32 rows.
+hipError_t paged_attn_window(hipStream_t s, const PagedAttnArgs& a, bool bf16, int64_t max_len, float* ws, size_t bytes);
+hipError_t paged_attn_scaled_bf16(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws, size_t bytes);
+hipError_t paged_attn_scaled_f32(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws, size_t bytes);
 
 // k, v rows [total_rows][Hkv][hd] (row strides in elements) into their pages; size: bytes of an element.
 hipError_t paged_append(hipStream_t s, const PagedView& c, const PagedRows& r, const void* k, int64_t k_stride,
