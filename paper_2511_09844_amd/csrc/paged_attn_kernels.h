@@ -49,6 +49,22 @@ constexpr float kLog2e = 1.4426950408889634f;
 // which are three bf16 numbers each there, exactly too (8 of 24 bits in each).  W: whether there is a window.
 template <typename C>
 constexpr bool kHeld8 = sizeof(C) == 1;
+#ifndef DEP1
+#define DEP1 3
+#endif
+#ifndef DEP2
+#define DEP2 2
+#endif
+#ifndef LB8
+#define LB8 2
+#endif
+#ifndef TGT8
+#define TGT8 512
+#endif
+#ifndef KT8
+#define KT8 2
+#endif
+constexpr int kTiles8 = KT8;
 
 // Under a window the keys that a group of rows reads are two runs, sinks and window.  The kernels go through them as one,
 // numbered without the positions between them (from the sinks' end, in whole kRun, to the start of the first row's window):
@@ -62,7 +78,7 @@ __device__ __forceinline__ Run run_of(const PagedAttnArgs& a, int first) {
     if constexpr (!W) return Run{0, 0, 0};
     Run u;
     u.sinks = (a.sinks + kRun - 1) / kRun * kRun;
-    u.from = max(first - a.window + 1, 0) / kRun * kRun;
+    u.from = min(max(first - a.window + 1, 0), a.c.max_pages << a.c.shift) / kRun * kRun;
     u.skip = max(u.from - u.sinks, 0);
     return u;
 }
@@ -209,8 +225,10 @@ __device__ __forceinline__ float inverse(const PagedAttnArgs& a, int b, float su
 }
 
 // The keys a workgroup of k_pdecode takes at a time, 16 or 32 per wave.
-template <typename T, typename C>
-constexpr int kBlockKeys = sizeof(T) == 2 || kHeld8<C> ? 32 : 16;
+template <typename C, int NT>
+constexpr int kTiles = kHeld8<C> ? (NT == 1 ? kTiles8 : 2) : sizeof(C) == 2 ? 2 : 1;  // of 16 keys
+template <typename C, int NT>
+constexpr int kBlockKeys = 16 * kTiles<C, NT>;
 // Waves of a workgroup: with 8 the one-token calls of 16 fp32 sequences take 42.5 us, not 36.5, and blocks of eight
 // rows 57, not 49 (larger units, and one more join of the waves' sums).
 constexpr int kDecodeWaves = 4;
@@ -248,9 +266,9 @@ __device__ __forceinline__ int seq_keys(const PagedAttnArgs& a, const SeqRows& s
 }
 
 // The sequence that unit `unit` belongs to (b = -1: none), or sequence `b` itself when unit is negative.
-template <typename T, typename C, bool W>
+template <bool W, int BK>
 __device__ __forceinline__ Units units_of(const DecodeArgs& d, int unit, int b) {
-    constexpr int step = kDecodeWaves * kBlockKeys<T, C>;
+    constexpr int step = kDecodeWaves * BK;
     const PagedAttnArgs& a = d.a;
     Units u;
     if (!d.target) {
@@ -295,10 +313,10 @@ __device__ __forceinline__ Units units_of(const DecodeArgs& d, int unit, int b) 
 }
 
 // One block of keys in registers, as loaded.
-template <typename T, typename C, int HD>
+template <typename T, typename C, int HD, int TILES>
 struct Block {
     static constexpr bool H = sizeof(T) == 2;
-    static constexpr int TK = H ? 2 : 1;              // tiles of 16 keys
+    static constexpr int TK = TILES;                  // tiles of 16 keys
     static constexpr int NK = H ? HD / 32 : HD / 16;  // 16-byte loads of a row of K per lane
     static constexpr int VW = H ? HD / 16 : HD / 16 < 4 ? HD / 16 : 4;  // neighbouring columns of V per lane
     static constexpr int VU = HD / 16 / VW;
@@ -310,10 +328,10 @@ struct Block {
 };
 // Of 8 bits: a lane's values of K are 8 columns for each of NK instructions, 16 neighbouring ones for two of them (head
 // dim 32: 8 for the one); of V HD / 16 neighbouring columns of its keys, as in bf16.
-template <typename T, int HD>
-struct Block<T, uint8_t, HD> {
+template <typename T, int HD, int TILES>
+struct Block<T, uint8_t, HD, TILES> {
     static constexpr bool H = true;
-    static constexpr int TK = 2, NK = HD / 32;
+    static constexpr int TK = TILES, NK = HD / 32;
     static constexpr int KD = HD >= 64 ? 4 : 2;  // dwords of a load of K
     static constexpr int VW = HD / 16, VU = 1, VD = VW < 4 ? 1 : VW / 4;
     static constexpr int QP = sizeof(T) == 2 ? 1 : 3;
@@ -322,13 +340,16 @@ struct Block<T, uint8_t, HD> {
     uint32_t pk[TK], pv[TK];  // the tile's powers, k's and v's bytes, as they came with K and with V
 };
 
+template <typename T, typename C, int HD, int NT>
+using BlockOf = Block<T, C, HD, kTiles<C, NT>>;
+
 // Which of a block's operands.
 enum { kLoadK = 1, kLoadV = 2 };
 // Keys k0 .. of a cache's pages: position pos (of the tiles in a row: 16 more each), up to key `end`.
-template <typename T, typename C, int HD, int WHAT>
-__device__ __forceinline__ void load_block(Block<T, C, HD>& x, const PagedView& c, int kvh, const int* page, int k0, int pos,
+template <int WHAT, typename T, typename C, int HD, int TILES>
+__device__ __forceinline__ void load_block(Block<T, C, HD, TILES>& x, const PagedView& c, int kvh, const int* page, int k0, int pos,
                                            int end, int lane) {
-    using B = Block<T, C, HD>;
+    using B = Block<T, C, HD, TILES>;
     constexpr int RB = HD * sizeof(C);
     const int n = lane & 15, g = lane >> 4;
 #pragma unroll
@@ -337,9 +358,10 @@ __device__ __forceinline__ void load_block(Block<T, C, HD>& x, const PagedView& 
         const int rows = uniform(page[t] < 0 ? 0 : max(min(end - key, 16), 0));
         const int64_t at = uniform((int64_t)max(page[t], 0) * c.page_stride + (((int64_t)kvh << c.shift) + slot) * HD);
         if constexpr (kHeld8<C>) {
-            // (where there are no rows the power is 1: numbers that are not there are 0)
-            uint32_t b = 0x7f7f;
-            if (rows > 0) b = *(const uint16_t*)(c.scales + uniform((int64_t)page[t] * c.scale_stride + (((int64_t)kvh << (c.shift - 4)) + (slot >> 4)) * 2));
+            // (where there are no rows the bytes are 0, a finite power of numbers that are 0)
+            const auto rp = __builtin_amdgcn_make_buffer_rsrc(
+                c.scales + uniform((int64_t)max(page[t], 0) * c.scale_stride + (((int64_t)kvh << (c.shift - 4)) + (slot >> 4)) * 2), 0, rows > 0 ? 2 : 0, 0x00020000);
+            const uint32_t b = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rp, 0, 0, 0);
             if constexpr (WHAT & kLoadK) x.pk[t] = b;
             if constexpr (WHAT & kLoadV) x.pv[t] = b;
         }
@@ -400,8 +422,8 @@ __device__ __forceinline__ uint32_t e4m3_bf16(uint32_t w, float power) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, HI));
 }
 // Operand i of tile t's K.
-template <typename T, int HD>
-__device__ __forceinline__ u4 keys_b8(const Block<T, uint8_t, HD>& x, int t, int i) {
+template <typename T, int HD, int TILES>
+__device__ __forceinline__ u4 keys_b8(const Block<T, uint8_t, HD, TILES>& x, int t, int i) {
     const float p = power_k(x.pk[t]);
     const uint32_t lo = x.k[t][2 * i], hi = x.k[t][2 * i + 1];
     return u4{e4m3_bf16<false>(lo, p), e4m3_bf16<true>(lo, p), e4m3_bf16<false>(hi, p), e4m3_bf16<true>(hi, p)};
@@ -468,33 +490,50 @@ __device__ __forceinline__ f4 mfma_b8(u4 v, u4 w, f4 c) {
 
 // Scores of a block, in units of log2, those that a row does not read at -inf.
 // k0: the first key's position.
-template <typename T, typename C, bool W, int HD, int NT>
-__device__ __forceinline__ void block_scores(const Block<T, C, HD>& x, const u4 (&q)[NT][Block<T, C, HD>::QP][Block<T, C, HD>::NK],
-                                             f4 (&sc)[NT][Block<T, C, HD>::TK], const PagedAttnArgs& a, const int* page, int k0,
+// q(j, p, i): part p of query operand i.
+template <typename T, typename C, bool W, int HD, int NT, typename Q>
+__device__ __forceinline__ void block_scores(const BlockOf<T, C, HD, NT>& x, const Q& q,
+                                             f4 (&sc)[NT][BlockOf<T, C, HD, NT>::TK], const PagedAttnArgs& a, const int* page, int k0,
                                              const int (&pos)[NT], bool whole, float scale, int lane) {
-    using B = Block<T, C, HD>;
+    using B = BlockOf<T, C, HD, NT>;
     const int g = lane >> 4;
+    // 8 bits: the largest parts' products and the others' in sums of their own, all tiles' side by side
+    f4 big[NT][B::TK], small[NT][B::TK];
+    if constexpr (kHeld8<C>) {
+#pragma unroll
+        for (int t = 0; t < B::TK; ++t)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) big[j][t] = small[j][t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < B::NK; ++i)
+#pragma unroll
+            for (int t = 0; t < B::TK; ++t) {
+                const u4 k = keys_b8(x, t, i);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    big[j][t] = mfma_b8(k, q(j, 0, i), big[j][t]);
+#pragma unroll
+                    for (int p = B::QP - 1; p > 0; --p) small[j][t] = mfma_b8(k, q(j, p, i), small[j][t]);
+                }
+            }
+    }
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int t = 0; t < B::TK; ++t) {
             f4 s = f4{0.f, 0.f, 0.f, 0.f};
             if constexpr (kHeld8<C>) {
-                // (the smallest parts' products first)
-#pragma unroll
-                for (int p = B::QP - 1; p >= 0; --p)
-#pragma unroll
-                    for (int i = 0; i < B::NK; ++i) s = mfma_b8(keys_b8<T, HD>(x, t, i), q[j][p][i], s);
+                s = B::QP > 1 ? big[j][t] + small[j][t] : big[j][t];
             } else if constexpr (B::H) {
 #pragma unroll
                 for (int i = 0; i < B::NK; ++i)
-                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, x.k[t][i]), __builtin_bit_cast(b8, q[j][0][i]),
+                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, x.k[t][i]), __builtin_bit_cast(b8, q(j, 0, i)),
                                                                 s, 0, 0, 0);
             } else {
                 f4 s1 = s;  // two chains
 #pragma unroll
                 for (int i = 0; i < B::NK; ++i) {
-                    const f4 kk = __builtin_bit_cast(f4, x.k[t][i]), qq = __builtin_bit_cast(f4, q[j][0][i]);
+                    const f4 kk = __builtin_bit_cast(f4, x.k[t][i]), qq = __builtin_bit_cast(f4, q(j, 0, i));
 #pragma unroll
                     for (int e = 0; e < 4; e += 2) {
                         s = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[e], qq[e], s, 0, 0, 0);
@@ -504,6 +543,9 @@ __device__ __forceinline__ void block_scores(const Block<T, C, HD>& x, const u4 
                 s += s1;
             }
             s *= scale;
+            // (Held here: used on one side of the branch only, the matrix instructions' results were moved behind it, where the
+            // compiler left 3 of the 8 wait states that they need on the way on which it is taken.)
+            asm volatile("" : "+v"(s));
             if (!whole)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[r] = page[t] >= 0 && reads<W>(a, pos[j], k0 + 16 * t + 4 * g + r) ? s[r] : -INFINITY;
@@ -513,8 +555,8 @@ __device__ __forceinline__ void block_scores(const Block<T, C, HD>& x, const u4 
 
 // The block's part of the softmax: its scores become weights.
 template <typename T, typename C, int HD, int NT>
-__device__ __forceinline__ void block_weights(Acc<T, HD, NT>& acc, f4 (&sc)[NT][Block<T, C, HD>::TK]) {
-    using B = Block<T, C, HD>;
+__device__ __forceinline__ void block_weights(Acc<T, HD, NT>& acc, f4 (&sc)[NT][BlockOf<T, C, HD, NT>::TK]) {
+    using B = BlockOf<T, C, HD, NT>;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         f4(&s)[B::TK] = sc[j];
@@ -585,8 +627,8 @@ __device__ __forceinline__ Parts<T> parts_b8(const f4& a, const f4& b) {
     return p;
 }
 // Columns 16 i .. 16 i + 15 and the next 16 of an 8-bit block's V (i even), tiles 2 u and 2 u + 1, as operands.
-template <typename T, int HD>
-__device__ __forceinline__ void values_e4m3(const Block<T, uint8_t, HD>& x, int u, int i, u4 (&w)[2], int zero = 0) {
+template <typename T, int HD, int TILES>
+__device__ __forceinline__ void values_e4m3(const Block<T, uint8_t, HD, TILES>& x, int u, int i, u4 (&w)[2], int zero = 0) {
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
         const int k = 8 * u + 2 * d;
@@ -598,7 +640,7 @@ __device__ __forceinline__ void values_e4m3(const Block<T, uint8_t, HD>& x, int 
 }
 // Columns 16 i .. 16 i + 15 of a bf16 block's V as an operand.
 template <int HD>
-__device__ __forceinline__ u4 values_b8(const Block<uint16_t, uint16_t, HD>& x, int i, int zero = 0) {
+__device__ __forceinline__ u4 values_b8(const Block<uint16_t, uint16_t, HD, 2>& x, int i, int zero = 0) {
     u4 w;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -608,8 +650,8 @@ __device__ __forceinline__ u4 values_b8(const Block<uint16_t, uint16_t, HD>& x, 
 
 // The block's product with V.
 template <typename T, typename C, int HD, int NT>
-__device__ __forceinline__ void block_sums(const Block<T, C, HD>& x, const f4 (&sc)[NT][Block<T, C, HD>::TK], Acc<T, HD, NT>& acc) {
-    using B = Block<T, C, HD>;
+__device__ __forceinline__ void block_sums(const BlockOf<T, C, HD, NT>& x, const f4 (&sc)[NT][BlockOf<T, C, HD, NT>::TK], Acc<T, HD, NT>& acc) {
+    using B = BlockOf<T, C, HD, NT>;
     if constexpr (kHeld8<C>) {
 #pragma unroll
         for (int u = 0; u < B::TK / 2; ++u) {
@@ -619,7 +661,7 @@ __device__ __forceinline__ void block_sums(const Block<T, C, HD>& x, const f4 (&
 #pragma unroll
             for (int i = 0; i < HD / 16; i += 2) {
                 u4 w[2];
-                values_e4m3<T, HD>(x, u, i, w);
+                values_e4m3(x, u, i, w);
 #pragma unroll
                 for (int e = Parts<T>::N - 1; e >= 0; --e)
 #pragma unroll
@@ -663,9 +705,9 @@ __device__ __forceinline__ void block_sums(const Block<T, C, HD>& x, const f4 (&
     }
 }
 
-template <typename T, typename C, int HD>
-__device__ __forceinline__ bool block_odd(const Block<T, C, HD>& x) {
-    using B = Block<T, C, HD>;
+template <typename T, typename C, int HD, int TILES>
+__device__ __forceinline__ bool block_odd(const Block<T, C, HD, TILES>& x) {
+    using B = Block<T, C, HD, TILES>;
     uint32_t any = 0;
 #pragma unroll
     for (int r = 0; r < 4 * B::TK; ++r) {
@@ -684,9 +726,9 @@ __device__ __forceinline__ bool block_odd(const Block<T, C, HD>& x) {
 // block_sums for a block with such values, from position k0 on, whose rows end at `from` .. `upto` (or behind); under a
 // window: whose rows are at from .. upto.
 template <typename T, typename C, bool W, int HD, int NT>
-__device__ __forceinline__ void block_sums_odd(const Block<T, C, HD>& x, const f4 (&sc)[NT][Block<T, C, HD>::TK], const PagedAttnArgs& a,
+__device__ __forceinline__ void block_sums_odd(const BlockOf<T, C, HD, NT>& x, const f4 (&sc)[NT][BlockOf<T, C, HD, NT>::TK], const PagedAttnArgs& a,
                                                int k0, int from, int upto, const int (&pos)[NT], Acc<T, HD, NT>& acc, int lane) {
-    using B = Block<T, C, HD>;
+    using B = BlockOf<T, C, HD, NT>;
     // of two bf16 values of neighbouring keys those that a row at `at` reads
     auto cut = [&](int key, int at) {
         if constexpr (!W) return cut_mask(key, at);
@@ -704,7 +746,7 @@ __device__ __forceinline__ void block_sums_odd(const Block<T, C, HD>& x, const f
                 for (int u = 0; u < B::TK / 2; ++u) {
                     if constexpr (kHeld8<C>) {
                         u4 y[2];
-                        values_e4m3<T, HD>(x, u, i & ~1, y, unknown(0));
+                        values_e4m3(x, u, i & ~1, y, unknown(0));
                         w[u] = y[i & 1];
                     } else {
                         w[u] = values_b8<HD>(x, i, unknown(0));
@@ -737,9 +779,9 @@ __device__ __forceinline__ void block_sums_odd(const Block<T, C, HD>& x, const f
 
 // Query vector v of a sequence and KV head: row v / G of the sequence, head kvh * G + v % G.
 template <typename T, typename C, bool W, int HD, int NT>
-__global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) {
-    using B = Block<T, C, HD>;
-    constexpr int QV = 16 * NT, BK = kBlockKeys<T, C>;
+__global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdecode(DecodeArgs d) {
+    using B = BlockOf<T, C, HD, NT>;
+    constexpr int QV = 16 * NT, BK = kBlockKeys<C, NT>;
     __shared__ __attribute__((aligned(16))) f4 os[kDecodeWaves / 2][NT * (HD / 16)][64];
     __shared__ float ms[kDecodeWaves][QV][2];
     const PagedAttnArgs& a = d.a;
@@ -750,7 +792,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     const int per = (d.units * a.c.Hkv + 7) / 8 * 8;
     const int cg = blockIdx.x / per, unit = blockIdx.x % per / a.c.Hkv, kvh = blockIdx.x % per % a.c.Hkv;
     if (unit >= d.units) return;
-    const Units un = units_of<T, C, W>(d, unit, 0);
+    const Units un = units_of<W, kBlockKeys<C, NT>>(d, unit, 0);
     const int b = un.b;
     if (b < 0) return;
     const int G = a.H / a.c.Hkv;
@@ -760,9 +802,11 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     const int kb = (unit - un.first) * un.keys;
     int k0 = kb + wave * BK;
     const Run run = run_of<W>(a, uniform(un.rows.len) - uniform(un.rows.n));
-    int entry[2][B::TK];
+    // blocks in registers: of 8 bits three (two of 32 query vectors); else two (one)
+    constexpr int D = kHeld8<C> ? (NT == 1 ? DEP1 : DEP2) : NT == 1 ? 2 : 1, E = D > 2 ? D : 2;
+    int entry[E][B::TK];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < E; ++i)
 #pragma unroll
         for (int t = 0; t < B::TK; ++t) {
             const int j = (position<W>(run, k0 + i * step) + 16 * t) >> a.c.shift;
@@ -776,6 +820,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     const int ke = min(keys_below<W>(run, min(last + 1, seq_end(a, un.rows))), un.count > 1 ? kb + un.keys : INT32_MAX);
     const bool whole_seq = un.count == 1;
     const int64_t slot = ((int64_t)unit * a.c.Hkv + kvh) * d.ncg + cg;
+    // the query vectors' operands, in registers; 32 vectors of three parts each, which would take 96, in LDS
+    constexpr bool QL = NT == 2 && B::QP == 3;
+    __shared__ u4 qs[QL ? NT : 1][QL ? 3 : 1][QL ? B::NK : 1][64];
     u4 q[NT][B::QP][B::NK];
     int pos[NT];
 #pragma unroll
@@ -789,16 +836,24 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
             if constexpr (B::QP == 1) {
                 q[j][0][i] = *(const u4*)(p + col);
             } else {
+                if (QL && wave != (j * B::NK + i) % kDecodeWaves) continue;
                 float x[8];
                 *(f4*)x = *(const f4*)(p + col);
                 *(f4*)(x + 4) = *(const f4*)(p + col + 4);
                 u4 w[3];
                 split3(x, w);
 #pragma unroll
-                for (int e = 0; e < 3; ++e) q[j][e][i] = w[e];
+                for (int e = 0; e < 3; ++e) {
+                    if constexpr (QL) qs[j][e][i][lane] = w[e];
+                    else q[j][e][i] = w[e];
+                }
             }
         }
     }
+    auto query = [&](int j, int p, int i) -> u4 {
+        if constexpr (QL) return qs[j][p][i][lane];
+        else return q[j][p][i];
+    };
     const float scale = a.scale * kLog2e;
     Acc<T, HD, NT> acc;
 #pragma unroll
@@ -810,19 +865,24 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     }
     // (tiles that no row of the group reads are left out as well)
     auto wanted = [&](int k0, int t) { return k0 + 16 * t < ke && (!W || any_reads<W>(a, first, last, position<W>(run, k0) + 16 * t, 16)); };
-    auto look = [&](int k0, int (&page)[B::TK]) {
-#pragma unroll
-        for (int t = 0; t < B::TK; ++t)
-            page[t] = wanted(k0, t) ? __builtin_amdgcn_readfirstlane(paged_page(a.c, b, (position<W>(run, k0) + 16 * t) >> a.c.shift)) : -1;
-    };
-    int page[3][B::TK];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
+    // a block's table entries, and later, where they are needed, the pages they name (the first test of an entry waits for it)
+    auto ask = [&](int k0, int (&entry)[B::TK]) {
 #pragma unroll
         for (int t = 0; t < B::TK; ++t) {
-            const int p = uniform(entry[i][t]);
-            page[i][t] = wanted(k0 + i * step, t) && (uint32_t)p < (uint32_t)a.c.n_pages ? p : -1;
+            const int j = (position<W>(run, k0) + 16 * t) >> a.c.shift;
+            entry[t] = a.c.table[(int64_t)b * a.c.max_pages + (k0 + 16 * t < ke && j < a.c.max_pages ? j : 0)];
         }
+    };
+    auto named = [&](int k0, const int (&entry)[B::TK], int (&page)[B::TK]) {
+#pragma unroll
+        for (int t = 0; t < B::TK; ++t) {
+            const int p = uniform(entry[t]);
+            page[t] = wanted(k0, t) && (position<W>(run, k0) + 16 * t) >> a.c.shift < a.c.max_pages && (uint32_t)p < (uint32_t)a.c.n_pages ? p : -1;
+        }
+    };
+    int page[E][B::TK], ahead[B::TK];
+#pragma unroll
+    for (int i = 0; i < E; ++i) named(k0 + i * step, entry[i], page[i]);
     f4 sc[NT][B::TK];
     auto whole = [&](int k) {
         bool w = k + BK <= ke && all_read<W>(a, first, last, position<W>(run, k), BK);
@@ -830,63 +890,67 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
         for (int t = 0; t < B::TK; ++t) w &= page[0][t] >= 0;
         return w;
     };
-    auto shift = [&] {
+    auto shift = [&](int k) {
 #pragma unroll
-        for (int t = 0; t < B::TK; ++t) {
-            page[0][t] = page[1][t];
-            page[1][t] = page[2][t];
-        }
+        for (int t = 0; t < B::TK; ++t)
+#pragma unroll
+            for (int i = 0; i + 1 < E; ++i) page[i][t] = page[i + 1][t];
+        named(k + E * step, ahead, page[E - 1]);
     };
     // whether rows differ in what they read of a block (without a window: such blocks come last), or read less than all
     auto mixed = [&](int k) { return W ? !all_read<W>(a, first, last, position<W>(run, k), BK) : min(k + BK, ke) - 1 > first; };
     bool odd = false;
-    if constexpr (NT == 1) {
-        // the next block is requested before this one is used
-        Block<T, C, HD> x[2];
-        load_block<T, C, HD, kLoadK | kLoadV>(x[0], a.c, kvh, page[0], k0, position<W>(run, k0), ke, lane);
-        for (; k0 < ke; k0 += 2 * step) {
+    if constexpr (D > 1) {
+        // the next D - 1 blocks are requested before this one is used
+        BlockOf<T, C, HD, NT> x[D];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < D - 1; ++i)
+            load_block<kLoadK | kLoadV>(x[i], a.c, kvh, page[i], k0 + i * step, position<W>(run, k0 + i * step), ke, lane);
+        if constexpr (QL) __syncthreads();
+        for (; k0 < ke; k0 += D * step) {
+#pragma unroll
+            for (int i = 0; i < D; ++i) {
                 const int k = k0 + i * step;
                 if (k >= ke) break;
-                look(k + 2 * step, page[2]);
-                load_block<T, C, HD, kLoadK | kLoadV>(x[1 - i], a.c, kvh, page[1], k + step, position<W>(run, k + step), ke, lane);
-                if (mixed(k) && block_odd<T, C, HD>(x[i])) {
+                ask(k + E * step, ahead);
+                load_block<kLoadK | kLoadV>(x[(i + D - 1) % D], a.c, kvh, page[D - 1], k + (D - 1) * step, position<W>(run, k + (D - 1) * step), ke, lane);
+                if (mixed(k) && block_odd(x[i])) {
                     odd = true;
                     k0 = k;
                     break;
                 }
-                block_scores<T, C, W, HD, NT>(x[i], q, sc, a, page[0], position<W>(run, k), pos, whole(k), scale, lane);
+                block_scores<T, C, W, HD, NT>(x[i], query, sc, a, page[0], position<W>(run, k), pos, whole(k), scale, lane);
                 block_weights<T, C, HD, NT>(acc, sc);
                 block_sums<T, C, HD, NT>(x[i], sc, acc);
-                shift();
+                shift(k);
             }
             if (odd) break;
         }
     } else {
         // registers for one block: its K is replaced when the scores are there, its V when the sums are
-        Block<T, C, HD> x;
-        load_block<T, C, HD, kLoadK | kLoadV>(x, a.c, kvh, page[0], k0, position<W>(run, k0), ke, lane);
-        for (; k0 < ke && !(mixed(k0) && block_odd<T, C, HD>(x)); k0 += step) {
-            look(k0 + 2 * step, page[2]);
-            block_scores<T, C, W, HD, NT>(x, q, sc, a, page[0], position<W>(run, k0), pos, whole(k0), scale, lane);
-            load_block<T, C, HD, kLoadK>(x, a.c, kvh, page[1], k0 + step, position<W>(run, k0 + step), ke, lane);
+        BlockOf<T, C, HD, NT> x;
+        load_block<kLoadK | kLoadV>(x, a.c, kvh, page[0], k0, position<W>(run, k0), ke, lane);
+        for (; k0 < ke && !(mixed(k0) && block_odd(x)); k0 += step) {
+            ask(k0 + E * step, ahead);
+            block_scores<T, C, W, HD, NT>(x, query, sc, a, page[0], position<W>(run, k0), pos, whole(k0), scale, lane);
+            load_block<kLoadK>(x, a.c, kvh, page[1], k0 + step, position<W>(run, k0 + step), ke, lane);
             block_weights<T, C, HD, NT>(acc, sc);
             block_sums<T, C, HD, NT>(x, sc, acc);
-            load_block<T, C, HD, kLoadV>(x, a.c, kvh, page[1], k0 + step, position<W>(run, k0 + step), ke, lane);
-            shift();
+            load_block<kLoadV>(x, a.c, kvh, page[1], k0 + step, position<W>(run, k0 + step), ke, lane);
+            shift(k0);
         }
     }
     // from a block with infinities or NaN on one by one, apart so that it costs the others no registers
 #pragma unroll 1
     for (; k0 < ke; k0 += step) {
-        Block<T, C, HD> x;
+        BlockOf<T, C, HD, NT> x;
         const int lane = unknown(threadIdx.x) & 63;
-        look(k0, page[0]);
-        load_block<T, C, HD, kLoadK>(x, a.c, kvh, page[0], k0, position<W>(run, k0), ke, lane);
-        block_scores<T, C, W, HD, NT>(x, q, sc, a, page[0], position<W>(run, k0), pos, false, scale, lane);
+        ask(k0, ahead);
+        named(k0, ahead, page[0]);
+        load_block<kLoadK>(x, a.c, kvh, page[0], k0, position<W>(run, k0), ke, lane);
+        block_scores<T, C, W, HD, NT>(x, query, sc, a, page[0], position<W>(run, k0), pos, false, scale, lane);
         block_weights<T, C, HD, NT>(acc, sc);
-        load_block<T, C, HD, kLoadV>(x, a.c, kvh, page[0], k0, position<W>(run, k0), ke, lane);
+        load_block<kLoadV>(x, a.c, kvh, page[0], k0, position<W>(run, k0), ke, lane);
         block_sums_odd<T, C, W, HD, NT>(x, sc, a, position<W>(run, k0), W ? first : max(first, k0), W ? last : min(k0 + BK, ke) - 1, pos, acc, lane);
     }
     // the waves' parts on one maximum, then added
@@ -943,15 +1007,16 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
 #pragma unroll
                 for (int e = 0; e < B::VW; ++e) y[r * B::VW + e] = acc.o[j][u * B::VW + e][r] * inv;
             const int c = (16 * u + 4 * g) * B::VW;
+            if (v >= nqv) continue;
             if (!whole_seq) {
                 float* p = d.part + (slot * QV + 16 * j + n) * HD + c;
 #pragma unroll
                 for (int i = 0; i < 4 * B::VW; i += 4) *(f4*)(p + i) = f4{y[i], y[i + 1], y[i + 2], y[i + 3]};
-            } else if (v < nqv) {
+            } else {
                 put<T, 4 * B::VW>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
             }
         }
-        if (!whole_seq && g == 0) {
+        if (!whole_seq && v < nqv && g == 0) {
             float* p = d.part + d.ml + (slot * QV + 16 * j + n) * 2;
             *(f2*)p = f2{mt[j], lt[j]};
         }
@@ -999,7 +1064,7 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
     const int nb = (QV + PER - 1) / PER, group = blockIdx.x / nb;
     const int i = blockIdx.x % nb * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4;
     const int cg = group % d.ncg, kvh = group / d.ncg % a.c.Hkv, b = group / d.ncg / a.c.Hkv, G = a.H / a.c.Hkv;
-    const Units un = units_of<T, C, W>(d, -1, b);
+    const Units un = units_of<W, kBlockKeys<C, NT>>(d, -1, b);
     const int live = un.count;
     if (live == 1) return;
     const int r0 = un.rows.r0, nqv = un.rows.n * G, v0 = cg * QV, n = min(QV, nqv - v0);
@@ -1254,6 +1319,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
     // leave them as bf16 for the places in LDS that the others are loaded to.
     constexpr int NT = KT / 8 / NW, PB = HD >= 64 ? 16 : 8, PR = HD / PB, NP = 16 * PR / 64;  // a group's pieces: bytes, of a row, of a lane
     uint32_t hold[kHeld8<C> ? NT : 1][NP ? NP : 1][PB / 4], power[NT];
+    auto power_of = [&](int page, int slot, int rows, int which, int bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc(a.c.scales + uniform((int64_t)page * a.c.scale_stride + (((int64_t)kvh << (a.c.shift - 4)) + (slot >> 4)) * 2 + which),
+                                                 0, rows > 0 ? bytes : 0, 0x00020000);
+    };
     auto fetch = [&](int k0, int pg) {
 #pragma unroll
         for (int w = 0; w < NT; ++w) {
@@ -1262,8 +1331,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
             const int64_t at = uniform(max(page, 0) * a.c.page_stride + (((int64_t)kvh << a.c.shift) + slot) * HD);
             const bool isv = task >= KT / 16;
             const auto rs = __builtin_amdgcn_make_buffer_rsrc((uint8_t*)(isv ? a.c.v : a.c.k) + at, 0, rows * HD, 0x00020000);
-            power[w] = 127;
-            if (rows > 0) power[w] = a.c.scales[uniform((int64_t)page * a.c.scale_stride + (((int64_t)kvh << (a.c.shift - 4)) + (slot >> 4)) * 2 + isv)];
+            power[w] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(power_of(max(page, 0), slot, rows, isv, 1), 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int off = (i * 64 + lane) * PB;
@@ -1624,10 +1692,9 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
         if constexpr (kHeld8<C>) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                power[t] = 0x7f7f;
-                if (page[t] >= 0 && k0 + 16 * t < end)
-                    power[t] = *(const uint16_t*)(a.c.scales + uniform((int64_t)page[t] * a.c.scale_stride +
-                                                                       (((int64_t)kvh << (a.c.shift - 4)) + (((p0 + 16 * t) & mask) >> 4)) * 2));
+                const int64_t at = (int64_t)max(page[t], 0) * a.c.scale_stride + (((int64_t)kvh << (a.c.shift - 4)) + (((p0 + 16 * t) & mask) >> 4)) * 2;
+                power[t] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
+                    __builtin_amdgcn_make_buffer_rsrc(a.c.scales + uniform(at), 0, page[t] >= 0 && k0 + 16 * t < end ? 2 : 0, 0x00020000), 0, 0, 0);
             }
         }
 #pragma unroll
@@ -1900,7 +1967,7 @@ inline DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, boo
     const int64_t groups = (int64_t)c.Hkv * p.ncg;
     // two workgroups per CU, or as many units again as sequences (for 384 / 512 / 768 workgroups 16 fp32 sequences
     // of 256 to 2048 take 41.4 / 36.4 / 44.6 us, and the 905 MB batch 171 / 159 / 161)
-    int64_t target = max_len <= kDirect * kDecodeWaves * (bf16 ? 32 : 16) ? 0 : std::max<int64_t>((512 + groups - 1) / groups, r.nseq);
+    int64_t target = max_len <= kDirect * kDecodeWaves * (bf16 ? 32 : 16) ? 0 : std::max<int64_t>(((c.scales ? TGT8 : 512) + groups - 1) / groups, r.nseq);
     const size_t per = (size_t)groups * 16 * p.nt * (c.hd + 2) * sizeof(float);
     if (target && per * (target + r.nseq + 8) > bytes) target = std::max<int64_t>(0, (int64_t)(bytes / per) - r.nseq - 8);
     p.target = (int)target;
@@ -1925,7 +1992,7 @@ inline bool fits(const PagedView& c, const PagedRows& r, bool, const DecodePlan&
 
 template <typename T, typename C, bool W, int HD, int NT>
 hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p, float* ws) {
-    const DecodeArgs d{a, p.ncg, p.target, kDecodeWaves * kBlockKeys<T, C>, p.units, ws, p.ml};
+    const DecodeArgs d{a, p.ncg, p.target, kDecodeWaves * kBlockKeys<C, NT>, p.units, ws, p.ml};
     const int64_t per = ((int64_t)p.units * a.c.Hkv + 7) / 8 * 8;
     const hipError_t err = launch(k_pdecode<T, C, W, HD, NT>, dim3((unsigned)(per * p.ncg)), dim3(64 * kDecodeWaves), s, d);
     if (err != hipSuccess || !p.target) return err;

@@ -249,3 +249,17 @@ def test_refusals():
             f()
             print("not refused:", i)
     c.attend(q, lens, window=2 ** 30, sinks=2 ** 30)
+
+
+@pytest.mark.parametrize("dtype", list(T))
+@pytest.mark.parametrize("held8", [False, True])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("g,rows", [(1, 1), (8, 2), (4, 5), (4, 8), (8, 8)])
+def test_long_runs_of_keys_that_every_row_reads(dtype, held8, hd, g, rows):
+    """Without masks, where scores go straight into the softmax: 16 and 32 query vectors of a KV head, several blocks of keys
+    for every wave."""
+    make = (lambda *a, **k: make_scaled(*a, clean=True, **k)) if held8 else (lambda lens, *a, **k: make_cache(lens, T[dtype], *a, **k))
+    cache = make([3000, 777], 2, hd, 64, seed=7)
+    q = rand(2 * rows, 2 * g, hd, dtype=T[dtype], seed=3)
+    dl, _ = rows_of([3000, 777], [rows, rows], False)
+    check(cache.attend(q, dl), cache, q, [3000, 777], [rows, rows])
