@@ -9,7 +9,7 @@ import os
 import numpy as np
 import torch
 
-from .build import SO
+from .build import SO, TORCH_SO
 
 P = ctypes.c_void_p
 
@@ -87,6 +87,15 @@ class PagedRows(ctypes.Structure):
 
 
 _lib = None
+
+
+def load_torch_paged():
+    """The binding of the paged calls to torch tensors (built in-tree); raises if it is missing."""
+    load()
+    if not os.path.exists(TORCH_SO):
+        raise RuntimeError(f"{TORCH_SO} is not built; run paper_2511_09844_amd.build() first")
+    from . import _torch_paged
+    return _torch_paged
 
 
 def load():

@@ -10,7 +10,7 @@ size_t paged_attn_bytes(const PagedView& c, const PagedRows& r, int H, bool bf16
         const PromptPlan p = prompt_plan(c, r, H, bf16, max_len, SIZE_MAX);
         return fits(c, r, bf16, p) ? std::max<size_t>(p.bytes, 256) : 0;
     }
-    const DecodePlan p = decode_plan(c, r, H, bf16, max_len, SIZE_MAX);
+    const DecodePlan p = decode_plan(c, r, H, bf16, max_len, SIZE_MAX, c.scales || window);
     return fits(c, r, bf16, p) ? std::max<size_t>(p.bytes, 256) : 0;
 }
 

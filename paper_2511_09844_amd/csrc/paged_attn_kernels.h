@@ -58,8 +58,8 @@ constexpr bool kHeld8 = sizeof(C) == 1;
 #ifndef LB8
 #define LB8 2
 #endif
-#ifndef TGT8
-#define TGT8 512
+#ifndef SUB
+#define SUB 2
 #endif
 #ifndef KT8
 #define KT8 2
@@ -224,14 +224,18 @@ __device__ __forceinline__ float inverse(const PagedAttnArgs& a, int b, float su
     return sum > 0.f ? inv : pos < first ? 0.f : NAN;
 }
 
+// Waves of a workgroup: with 8 the one-token calls of 16 fp32 sequences take 42.5 us, not 36.5, and blocks of eight
+// rows 57, not 49 (larger units, and one more join of the waves' sums).
+constexpr int kDecodeWaves = 4;
+
 // The keys a workgroup of k_pdecode takes at a time, 16 or 32 per wave.
 template <typename C, int NT>
 constexpr int kTiles = kHeld8<C> ? (NT == 1 ? kTiles8 : 2) : sizeof(C) == 2 ? 2 : 1;  // of 16 keys
 template <typename C, int NT>
 constexpr int kBlockKeys = 16 * kTiles<C, NT>;
-// Waves of a workgroup: with 8 the one-token calls of 16 fp32 sequences take 42.5 us, not 36.5, and blocks of eight
-// rows 57, not 49 (larger units, and one more join of the waves' sums).
-constexpr int kDecodeWaves = 4;
+// A unit's keys are a multiple of this many.
+template <typename C, bool W, int NT>
+constexpr int kUnitKeys = kHeld8<C> || W ? kBlockKeys<C, NT> : kDecodeWaves * kBlockKeys<C, NT>;
 
 struct DecodeArgs {
     PagedAttnArgs a;
@@ -266,9 +270,8 @@ __device__ __forceinline__ int seq_keys(const PagedAttnArgs& a, const SeqRows& s
 }
 
 // The sequence that unit `unit` belongs to (b = -1: none), or sequence `b` itself when unit is negative.
-template <bool W, int BK>
+template <bool W, int STEP>
 __device__ __forceinline__ Units units_of(const DecodeArgs& d, int unit, int b) {
-    constexpr int step = kDecodeWaves * BK;
     const PagedAttnArgs& a = d.a;
     Units u;
     if (!d.target) {
@@ -286,7 +289,7 @@ __device__ __forceinline__ Units units_of(const DecodeArgs& d, int unit, int b) 
     total = wave_sum_dpp(total);
     // (rounded up past what the sum may have lost)
     const float want = fmaxf(total / (float)d.target * 1.00001f, (float)d.min_keys);
-    u.keys = want < 1.0e9f ? ((int)want + step) / step * step : 1 << 30;
+    u.keys = want < 1.0e9f ? ((int)want + STEP) / STEP * STEP : 1 << 30;
     u.b = -1;
     int at = 0;
     for (int b0 = 0; b0 < nseq; b0 += 64) {
@@ -792,7 +795,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdec
     const int per = (d.units * a.c.Hkv + 7) / 8 * 8;
     const int cg = blockIdx.x / per, unit = blockIdx.x % per / a.c.Hkv, kvh = blockIdx.x % per % a.c.Hkv;
     if (unit >= d.units) return;
-    const Units un = units_of<W, kBlockKeys<C, NT>>(d, unit, 0);
+    const Units un = units_of<W, kUnitKeys<C, W, NT>>(d, unit, 0);
     const int b = un.b;
     if (b < 0) return;
     const int G = a.H / a.c.Hkv;
@@ -1064,7 +1067,7 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
     const int nb = (QV + PER - 1) / PER, group = blockIdx.x / nb;
     const int i = blockIdx.x % nb * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4;
     const int cg = group % d.ncg, kvh = group / d.ncg % a.c.Hkv, b = group / d.ncg / a.c.Hkv, G = a.H / a.c.Hkv;
-    const Units un = units_of<W, kBlockKeys<C, NT>>(d, -1, b);
+    const Units un = units_of<W, kUnitKeys<C, W, NT>>(d, -1, b);
     const int live = un.count;
     if (live == 1) return;
     const int r0 = un.rows.r0, nqv = un.rows.n * G, v0 = cg * QV, n = min(QV, nqv - v0);
@@ -1958,7 +1961,7 @@ struct DecodePlan {
 };
 
 // bytes: room for partials.
-inline DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes) {
+inline DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes, bool grain = false) {
     DecodePlan p;
     const int qv = std::min<int64_t>((int64_t)r.max_rows * (H / c.Hkv), 1 << 20);
     // (blocks of 32 query vectors as two groups that read the keys once each: 62 us, not 49)
@@ -1967,7 +1970,7 @@ inline DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, boo
     const int64_t groups = (int64_t)c.Hkv * p.ncg;
     // two workgroups per CU, or as many units again as sequences (for 384 / 512 / 768 workgroups 16 fp32 sequences
     // of 256 to 2048 take 41.4 / 36.4 / 44.6 us, and the 905 MB batch 171 / 159 / 161)
-    int64_t target = max_len <= kDirect * kDecodeWaves * (bf16 ? 32 : 16) ? 0 : std::max<int64_t>(((c.scales ? TGT8 : 512) + groups - 1) / groups, r.nseq);
+    int64_t target = max_len <= kDirect * kDecodeWaves * (bf16 ? 32 : 16) ? 0 : std::max<int64_t>((512 + groups - 1) / groups - (grain ? r.nseq * SUB / 4 : 0), r.nseq);
     const size_t per = (size_t)groups * 16 * p.nt * (c.hd + 2) * sizeof(float);
     if (target && per * (target + r.nseq + 8) > bytes) target = std::max<int64_t>(0, (int64_t)(bytes / per) - r.nseq - 8);
     p.target = (int)target;
@@ -2004,7 +2007,7 @@ template <typename T, typename C, bool W, int HD>
 hipError_t attn(hipStream_t s, const PagedAttnArgs& a, int64_t max_len, float* ws, size_t bytes) {
     max_len = keys_expected(a.r, max_len, a.window, a.sinks);
     if (many_rows(a.c, a.r, a.H, sizeof(T) == 2)) return prompt<T, C, W, HD>(s, a, prompt_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, bytes), ws);
-    const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, bytes);
+    const DecodePlan p = decode_plan(a.c, a.r, a.H, sizeof(T) == 2, max_len, bytes, kHeld8<C> || W);
     return p.nt == 1 ? run_decode<T, C, W, HD, 1>(s, a, p, ws) : run_decode<T, C, W, HD, 2>(s, a, p, ws);
 }
 template <typename T, typename C, bool W>

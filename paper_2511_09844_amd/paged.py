@@ -1,4 +1,6 @@
-"""Paged K/V caches of include/sd2.h on torch tensors: argument checks and marshalling only.
+"""Paged K/V caches of include/sd2.h on torch tensors: argument checks and marshalling only.  A call whose arguments are
+plain cases of what it takes goes through csrc/torch_paged.cpp in one step; any other comes back from there, untouched, to
+the checks here.
 
     cache = PagedCache.empty(n_pages=512, page_size=64, n_layers=32, n_kv_heads=8, head_dim=128,
                              max_seqs=16, max_pages=64)
@@ -34,6 +36,7 @@ MOST_POSITIONS = 1 << 30
 # the current stream of a device, as HIP's handle (torch's own shortcut to it where there is one: a
 # microsecond less per call)
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _need(ok, msg):
@@ -96,6 +99,12 @@ class PagedCache:
         if self.held8:
             self._kv = {t: [B.PagedScaled(kv, scales.data_ptr() + l * record, n_layers * record) for l, kv in enumerate(kvs)]
                         for t, kvs in self._kv.items()}
+        self._quick = B.load_torch_paged()
+        views = [(type(self._kv[t][0]) * n_layers)(*self._kv[t]) if t in self._kv else None for t in (torch.float32, torch.bfloat16)]
+        self._cache = self._quick.cache(
+            self._index, n_layers, hd, n_kv, self.max_seqs, self.max_pages, page, int(self.held8),
+            *(0 if v is None else ctypes.addressof(v) for v in views), ctypes.addressof(pages), self._unused.data_ptr(),
+            self._pages_ws, self._scale)
 
     @classmethod
     def empty(cls, n_pages, page_size, n_layers, n_kv_heads, head_dim, max_seqs, max_pages, dtype=torch.bfloat16,
@@ -162,6 +171,10 @@ class PagedCache:
     def _workspace(self, nbytes):
         return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
+    def _plain(self):
+        """Whether a call may go the short way: on the current device, and where no tensor carries a tangent."""
+        return _device() == self._index and getattr(forward_ad, "_current_level", 0) < 0
+
     def _call(self, fn, *args):
         """A C call on the current stream of the cache's device, which is the current one meanwhile."""
         if torch.cuda.current_device() == self._index:
@@ -177,6 +190,8 @@ class PagedCache:
         """Write rows k, v [rows][n_kv_heads][head_dim] to their positions (sd2_paged_append): those of
         sequence b are the last ones of its lens[b] positions, rows row_off[b] .. row_off[b + 1] - 1, or
         without row_off an equal number for every sequence."""
+        if self._plain() and self._quick.append(self._cache, _stream_of(self._index), k, v, lens, layer, row_off, max_rows):
+            return
         ks, vs = self._packed(k, "k"), self._packed(v, "v")
         kv = self._layer(layer, k)
         _need(k.dtype == v.dtype, "k and v: one type")
@@ -191,6 +206,11 @@ class PagedCache:
         unless given; max_rows, max_len: the most rows and the largest length, where they are known (they
         decide how the work is split).  With a window a row reads the last `window` positions up to its own and the
         first `sinks` ones (sd2_paged_attn_window); caches of 8 bits: sd2_paged_attn_scaled."""
+        if self._plain():
+            res = self._quick.attend(self._cache, _stream_of(self._index), q, lens, layer, row_off, max_rows, max_len, scale, out,
+                                     window, sinks)
+            if res is not None:
+                return res
         qs = self._packed(q, "q")
         kv = self._layer(layer, q)
         heads = q.shape[1]
@@ -235,6 +255,10 @@ class PagedCache:
     def reserve(self, first, last, keep=None):
         """Make positions first[b] .. last[b] - 1 writable (sd2_pages_reserve); returns granted, int32
         per sequence: last[b], or where the first page begins that could not be had."""
+        if self._plain():
+            granted = self._quick.reserve(self._cache, _stream_of(self._index), first, last, keep)
+            if granted is not None:
+                return granted
         n = self._seqs("first, last, keep", first, last, *(() if keep is None else (keep,)))
         granted = torch.empty_like(last)
         ws = self._workspace(self._pages_ws)
@@ -245,6 +269,8 @@ class PagedCache:
     def fork(self, src, dst):
         """Sequence dst[i] gives up its pages and takes those of src[i], shared (sd2_pages_fork; lists of
         ints)."""
+        if self._plain() and self._quick.fork(self._cache, _stream_of(self._index), src, dst):
+            return
         src, dst = list(src), list(dst)
         _need(len(src) == len(dst), "fork: as many src as dst")
         _need(all(0 <= b < self.max_seqs for b in src + dst), f"fork: the table has {self.max_seqs} sequences")
@@ -261,6 +287,8 @@ class PagedCache:
     def slide(self, lens, window, sinks=0):
         """Sequences 0 .. len(lens) - 1 give up the pages that, under this window, no row from position lens[b] on
         reads (sd2_pages_slide; a negative length: none)."""
+        if self._plain() and self._quick.slide(self._cache, _stream_of(self._index), lens, window, sinks):
+            return
         self._window(window, sinks)
         n = self._seqs("lens", lens)
         self._call(self.lib.sd2_pages_slide, ctypes.byref(self._pages), n, lens.data_ptr(), window, sinks)
