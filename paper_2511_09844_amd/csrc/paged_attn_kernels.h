@@ -49,22 +49,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 // which are three bf16 numbers each there, exactly too (8 of 24 bits in each).  W: whether there is a window.
 template <typename C>
 constexpr bool kHeld8 = sizeof(C) == 1;
-#ifndef DEP1
-#define DEP1 3
-#endif
-#ifndef DEP2
-#define DEP2 2
-#endif
-#ifndef LB8
-#define LB8 2
-#endif
-#ifndef SUB
-#define SUB 2
-#endif
-#ifndef KT8
-#define KT8 2
-#endif
-constexpr int kTiles8 = KT8;
 
 // Under a window the keys that a group of rows reads are two runs, sinks and window.  The kernels go through them as one,
 // numbered without the positions between them (from the sinks' end, in whole kRun, to the start of the first row's window):
@@ -229,13 +213,13 @@ __device__ __forceinline__ float inverse(const PagedAttnArgs& a, int b, float su
 constexpr int kDecodeWaves = 4;
 
 // The keys a workgroup of k_pdecode takes at a time, 16 or 32 per wave.
-template <typename C, int NT>
-constexpr int kTiles = kHeld8<C> ? (NT == 1 ? kTiles8 : 2) : sizeof(C) == 2 ? 2 : 1;  // of 16 keys
-template <typename C, int NT>
-constexpr int kBlockKeys = 16 * kTiles<C, NT>;
+template <typename C>
+constexpr int kTiles = sizeof(C) == 4 ? 1 : 2;  // of 16 keys
+template <typename C>
+constexpr int kBlockKeys = 16 * kTiles<C>;
 // A unit's keys are a multiple of this many.
-template <typename C, bool W, int NT>
-constexpr int kUnitKeys = kHeld8<C> || W ? kBlockKeys<C, NT> : kDecodeWaves * kBlockKeys<C, NT>;
+template <typename C, bool W>
+constexpr int kUnitKeys = kHeld8<C> || W ? kBlockKeys<C> : kDecodeWaves * kBlockKeys<C>;
 
 struct DecodeArgs {
     PagedAttnArgs a;
@@ -343,8 +327,8 @@ struct Block<T, uint8_t, HD, TILES> {
     uint32_t pk[TK], pv[TK];  // the tile's powers, k's and v's bytes, as they came with K and with V
 };
 
-template <typename T, typename C, int HD, int NT>
-using BlockOf = Block<T, C, HD, kTiles<C, NT>>;
+template <typename T, typename C, int HD>
+using BlockOf = Block<T, C, HD, kTiles<C>>;
 
 // Which of a block's operands.
 enum { kLoadK = 1, kLoadV = 2 };
@@ -495,10 +479,10 @@ __device__ __forceinline__ f4 mfma_b8(u4 v, u4 w, f4 c) {
 // k0: the first key's position.
 // q(j, p, i): part p of query operand i.
 template <typename T, typename C, bool W, int HD, int NT, typename Q>
-__device__ __forceinline__ void block_scores(const BlockOf<T, C, HD, NT>& x, const Q& q,
-                                             f4 (&sc)[NT][BlockOf<T, C, HD, NT>::TK], const PagedAttnArgs& a, const int* page, int k0,
+__device__ __forceinline__ void block_scores(const BlockOf<T, C, HD>& x, const Q& q,
+                                             f4 (&sc)[NT][BlockOf<T, C, HD>::TK], const PagedAttnArgs& a, const int* page, int k0,
                                              const int (&pos)[NT], bool whole, float scale, int lane) {
-    using B = BlockOf<T, C, HD, NT>;
+    using B = BlockOf<T, C, HD>;
     const int g = lane >> 4;
     // 8 bits: the largest parts' products and the others' in sums of their own, all tiles' side by side
     f4 big[NT][B::TK], small[NT][B::TK];
@@ -558,8 +542,8 @@ __device__ __forceinline__ void block_scores(const BlockOf<T, C, HD, NT>& x, con
 
 // The block's part of the softmax: its scores become weights.
 template <typename T, typename C, int HD, int NT>
-__device__ __forceinline__ void block_weights(Acc<T, HD, NT>& acc, f4 (&sc)[NT][BlockOf<T, C, HD, NT>::TK]) {
-    using B = BlockOf<T, C, HD, NT>;
+__device__ __forceinline__ void block_weights(Acc<T, HD, NT>& acc, f4 (&sc)[NT][BlockOf<T, C, HD>::TK]) {
+    using B = BlockOf<T, C, HD>;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         f4(&s)[B::TK] = sc[j];
@@ -653,8 +637,8 @@ __device__ __forceinline__ u4 values_b8(const Block<uint16_t, uint16_t, HD, 2>& 
 
 // The block's product with V.
 template <typename T, typename C, int HD, int NT>
-__device__ __forceinline__ void block_sums(const BlockOf<T, C, HD, NT>& x, const f4 (&sc)[NT][BlockOf<T, C, HD, NT>::TK], Acc<T, HD, NT>& acc) {
-    using B = BlockOf<T, C, HD, NT>;
+__device__ __forceinline__ void block_sums(const BlockOf<T, C, HD>& x, const f4 (&sc)[NT][BlockOf<T, C, HD>::TK], Acc<T, HD, NT>& acc) {
+    using B = BlockOf<T, C, HD>;
     if constexpr (kHeld8<C>) {
 #pragma unroll
         for (int u = 0; u < B::TK / 2; ++u) {
@@ -729,9 +713,9 @@ __device__ __forceinline__ bool block_odd(const Block<T, C, HD, TILES>& x) {
 // block_sums for a block with such values, from position k0 on, whose rows end at `from` .. `upto` (or behind); under a
 // window: whose rows are at from .. upto.
 template <typename T, typename C, bool W, int HD, int NT>
-__device__ __forceinline__ void block_sums_odd(const BlockOf<T, C, HD, NT>& x, const f4 (&sc)[NT][BlockOf<T, C, HD, NT>::TK], const PagedAttnArgs& a,
+__device__ __forceinline__ void block_sums_odd(const BlockOf<T, C, HD>& x, const f4 (&sc)[NT][BlockOf<T, C, HD>::TK], const PagedAttnArgs& a,
                                                int k0, int from, int upto, const int (&pos)[NT], Acc<T, HD, NT>& acc, int lane) {
-    using B = BlockOf<T, C, HD, NT>;
+    using B = BlockOf<T, C, HD>;
     // of two bf16 values of neighbouring keys those that a row at `at` reads
     auto cut = [&](int key, int at) {
         if constexpr (!W) return cut_mask(key, at);
@@ -782,10 +766,15 @@ __device__ __forceinline__ void block_sums_odd(const BlockOf<T, C, HD, NT>& x, c
 
 // Query vector v of a sequence and KV head: row v / G of the sequence, head kvh * G + v % G.
 template <typename T, typename C, bool W, int HD, int NT>
-__global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdecode(DecodeArgs d) {
-    using B = BlockOf<T, C, HD, NT>;
-    constexpr int QV = 16 * NT, BK = kBlockKeys<C, NT>;
-    __shared__ __attribute__((aligned(16))) f4 os[kDecodeWaves / 2][NT * (HD / 16)][64];
+__global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) {
+    using B = BlockOf<T, C, HD>;
+    constexpr int QV = 16 * NT, BK = kBlockKeys<C>;
+    // Whether every wave joins a quarter of the columns (below).
+    constexpr bool QUARTERS = kHeld8<C> || W;
+    // the query vectors' operands in registers; 32 vectors of three parts each, which would take 96, in LDS
+    constexpr bool QL = NT == 2 && B::QP == 3;
+    constexpr int NI = NT * (HD / 16), OS = (QUARTERS ? kDecodeWaves : kDecodeWaves / 2) * NI * 64, QS = QL ? NT * 3 * B::NK * 64 : 0;
+    __shared__ __attribute__((aligned(16))) f4 lds[OS > QS ? OS : QS];  // the operands, then the waves' sums
     __shared__ float ms[kDecodeWaves][QV][2];
     const PagedAttnArgs& a = d.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -795,7 +784,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdec
     const int per = (d.units * a.c.Hkv + 7) / 8 * 8;
     const int cg = blockIdx.x / per, unit = blockIdx.x % per / a.c.Hkv, kvh = blockIdx.x % per % a.c.Hkv;
     if (unit >= d.units) return;
-    const Units un = units_of<W, kUnitKeys<C, W, NT>>(d, unit, 0);
+    const Units un = units_of<W, kUnitKeys<C, W>>(d, unit, 0);
     const int b = un.b;
     if (b < 0) return;
     const int G = a.H / a.c.Hkv;
@@ -805,8 +794,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdec
     const int kb = (unit - un.first) * un.keys;
     int k0 = kb + wave * BK;
     const Run run = run_of<W>(a, uniform(un.rows.len) - uniform(un.rows.n));
-    // blocks in registers: of 8 bits three (two of 32 query vectors); else two (one)
-    constexpr int D = kHeld8<C> ? (NT == 1 ? DEP1 : DEP2) : NT == 1 ? 2 : 1, E = D > 2 ? D : 2;
+    // Blocks in registers: two, or one of 32 query vectors, unless it is of 8 bits (three of those, for 16 query vectors: a
+    // token of 16 sequences of 256 to 2048 17.9 us, not 17.0, and two long ones 90.3, not 89.3).
+    constexpr int D = kHeld8<C> || NT == 1 ? 2 : 1, E = 2;
     int entry[E][B::TK];
 #pragma unroll
     for (int i = 0; i < E; ++i)
@@ -823,9 +813,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdec
     const int ke = min(keys_below<W>(run, min(last + 1, seq_end(a, un.rows))), un.count > 1 ? kb + un.keys : INT32_MAX);
     const bool whole_seq = un.count == 1;
     const int64_t slot = ((int64_t)unit * a.c.Hkv + kvh) * d.ncg + cg;
-    // the query vectors' operands, in registers; 32 vectors of three parts each, which would take 96, in LDS
-    constexpr bool QL = NT == 2 && B::QP == 3;
-    __shared__ u4 qs[QL ? NT : 1][QL ? 3 : 1][QL ? B::NK : 1][64];
+    auto shared_q = [&](int j, int p, int i) -> u4& { return ((u4*)lds)[((j * 3 + p) * B::NK + i) * 64 + lane]; };
     u4 q[NT][B::QP][B::NK];
     int pos[NT];
 #pragma unroll
@@ -847,14 +835,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdec
                 split3(x, w);
 #pragma unroll
                 for (int e = 0; e < 3; ++e) {
-                    if constexpr (QL) qs[j][e][i][lane] = w[e];
+                    if constexpr (QL) shared_q(j, e, i) = w[e];
                     else q[j][e][i] = w[e];
                 }
             }
         }
     }
     auto query = [&](int j, int p, int i) -> u4 {
-        if constexpr (QL) return qs[j][p][i][lane];
+        if constexpr (QL) return shared_q(j, p, i);
         else return q[j][p][i];
     };
     const float scale = a.scale * kLog2e;
@@ -905,7 +893,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdec
     bool odd = false;
     if constexpr (D > 1) {
         // the next D - 1 blocks are requested before this one is used
-        BlockOf<T, C, HD, NT> x[D];
+        BlockOf<T, C, HD> x[D];
 #pragma unroll
         for (int i = 0; i < D - 1; ++i)
             load_block<kLoadK | kLoadV>(x[i], a.c, kvh, page[i], k0 + i * step, position<W>(run, k0 + i * step), ke, lane);
@@ -931,7 +919,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdec
         }
     } else {
         // registers for one block: its K is replaced when the scores are there, its V when the sums are
-        BlockOf<T, C, HD, NT> x;
+        BlockOf<T, C, HD> x;
         load_block<kLoadK | kLoadV>(x, a.c, kvh, page[0], k0, position<W>(run, k0), ke, lane);
         for (; k0 < ke && !(mixed(k0) && block_odd(x)); k0 += step) {
             ask(k0 + E * step, ahead);
@@ -946,7 +934,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdec
     // from a block with infinities or NaN on one by one, apart so that it costs the others no registers
 #pragma unroll 1
     for (; k0 < ke; k0 += step) {
-        BlockOf<T, C, HD, NT> x;
+        BlockOf<T, C, HD> x;
         const int lane = unknown(threadIdx.x) & 63;
         ask(k0, ahead);
         named(k0, ahead, page[0]);
@@ -956,7 +944,71 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kHeld8<C> ? LB8 : 2) void k_pdec
         load_block<kLoadV>(x, a.c, kvh, page[0], k0, position<W>(run, k0), ke, lane);
         block_sums_odd<T, C, W, HD, NT>(x, sc, a, position<W>(run, k0), W ? first : max(first, k0), W ? last : min(k0 + BK, ke) - 1, pos, acc, lane);
     }
-    // the waves' parts on one maximum, then added
+    // The waves' parts on one maximum, added.  By quarters: every wave takes the columns of one r of its four, all waves' parts
+    // of them, and writes those.
+    if constexpr (QUARTERS) {
+        if constexpr (QL) __syncthreads();  // (nobody reads operands any more)
+        float* const os = (float*)lds;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            acc.l[j] = col_sum(acc.l[j]);
+            if (g == 0) {
+                ms[wave][16 * j + n][0] = acc.m[j];
+                ms[wave][16 * j + n][1] = acc.l[j];
+            }
+#pragma unroll
+            for (int i = 0; i < HD / 16; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) os[((wave * 4 + r) * NI + j * (HD / 16) + i) * 64 + lane] = acc.o[j][i][r];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            float m = -INFINITY, l = 0.f, f[kDecodeWaves];
+#pragma unroll
+            for (int w = 0; w < kDecodeWaves; ++w) m = fmaxf(m, ms[w][16 * j + n][0]);
+            const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int w = 0; w < kDecodeWaves; ++w) {
+                f[w] = __builtin_amdgcn_exp2f(ms[w][16 * j + n][0] - base);
+                l += ms[w][16 * j + n][1] * f[w];
+            }
+            const int v = v0 + 16 * j + n;
+            const float inv = !whole_seq ? 1.f : inverse<W>(a, b, l, pos[j], last);
+#pragma unroll
+            for (int u = 0; u < B::VU; ++u) {
+                float y[B::VW];
+#pragma unroll
+                for (int e = 0; e < B::VW; ++e) {
+                    const float* p = os + (wave * NI + j * (HD / 16) + u * B::VW + e) * 64 + lane;
+                    y[e] = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kDecodeWaves; ++w) y[e] += p[w * 4 * NI * 64] * f[w];
+                    y[e] *= inv;
+                }
+                const int c = (16 * u + 4 * g + wave) * B::VW;
+                if (v >= nqv) continue;
+                if (!whole_seq) {
+                    float* p = d.part + (slot * QV + 16 * j + n) * HD + c;
+                    if constexpr (B::VW >= 4) {
+#pragma unroll
+                        for (int i = 0; i < B::VW; i += 4) *(f4*)(p + i) = f4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+                    } else {
+                        *(f2*)p = f2{y[0], y[1]};
+                    }
+                } else if constexpr (B::VW >= 4) {
+                    put<T, B::VW>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
+                } else {
+                    T* p = (T*)a.out + (r0 + v / G) * a.out_stride + (kvh * G + v % G) * HD + c;
+                    if constexpr (sizeof(T) == 2) *(uint32_t*)p = pack_bf16(y[0], y[1]);
+                    else *(f2*)p = f2{y[0], y[1]};
+                }
+            }
+            if (!whole_seq && v < nqv && g == 0 && wave == j) *(f2*)(d.part + d.ml + (slot * QV + 16 * j + n) * 2) = f2{m, l};
+        }
+        return;
+    }
+    f4(*const os)[NI][64] = (f4(*)[NI][64])lds;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         acc.l[j] = col_sum(acc.l[j]);
@@ -1067,7 +1119,7 @@ __global__ __launch_bounds__(256) void k_pjoin(DecodeArgs d) {
     const int nb = (QV + PER - 1) / PER, group = blockIdx.x / nb;
     const int i = blockIdx.x % nb * PER + threadIdx.x / (HD / 4), c = threadIdx.x % (HD / 4) * 4;
     const int cg = group % d.ncg, kvh = group / d.ncg % a.c.Hkv, b = group / d.ncg / a.c.Hkv, G = a.H / a.c.Hkv;
-    const Units un = units_of<W, kUnitKeys<C, W, NT>>(d, -1, b);
+    const Units un = units_of<W, kUnitKeys<C, W>>(d, -1, b);
     const int live = un.count;
     if (live == 1) return;
     const int r0 = un.rows.r0, nqv = un.rows.n * G, v0 = cg * QV, n = min(QV, nqv - v0);
@@ -1960,8 +2012,9 @@ struct DecodePlan {
     size_t bytes;
 };
 
-// bytes: room for partials.
-inline DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes, bool grain = false) {
+// bytes: room for partials.  fine: units of whole blocks, not workgroup steps; with half a unit of each sequence that is
+// not full the workgroups are then those that the CUs hold at once (8 bits, 16 sequences: 17.0 us, and 21.6 without that).
+inline DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes, bool fine = false) {
     DecodePlan p;
     const int qv = std::min<int64_t>((int64_t)r.max_rows * (H / c.Hkv), 1 << 20);
     // (blocks of 32 query vectors as two groups that read the keys once each: 62 us, not 49)
@@ -1970,7 +2023,7 @@ inline DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, boo
     const int64_t groups = (int64_t)c.Hkv * p.ncg;
     // two workgroups per CU, or as many units again as sequences (for 384 / 512 / 768 workgroups 16 fp32 sequences
     // of 256 to 2048 take 41.4 / 36.4 / 44.6 us, and the 905 MB batch 171 / 159 / 161)
-    int64_t target = max_len <= kDirect * kDecodeWaves * (bf16 ? 32 : 16) ? 0 : std::max<int64_t>((512 + groups - 1) / groups - (grain ? r.nseq * SUB / 4 : 0), r.nseq);
+    int64_t target = max_len <= kDirect * kDecodeWaves * (bf16 ? 32 : 16) ? 0 : std::max<int64_t>((512 + groups - 1) / groups - (fine ? r.nseq / 2 : 0), r.nseq);
     const size_t per = (size_t)groups * 16 * p.nt * (c.hd + 2) * sizeof(float);
     if (target && per * (target + r.nseq + 8) > bytes) target = std::max<int64_t>(0, (int64_t)(bytes / per) - r.nseq - 8);
     p.target = (int)target;
@@ -1995,7 +2048,7 @@ inline bool fits(const PagedView& c, const PagedRows& r, bool, const DecodePlan&
 
 template <typename T, typename C, bool W, int HD, int NT>
 hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p, float* ws) {
-    const DecodeArgs d{a, p.ncg, p.target, kDecodeWaves * kBlockKeys<C, NT>, p.units, ws, p.ml};
+    const DecodeArgs d{a, p.ncg, p.target, kDecodeWaves * kBlockKeys<C>, p.units, ws, p.ml};
     const int64_t per = ((int64_t)p.units * a.c.Hkv + 7) / 8 * 8;
     const hipError_t err = launch(k_pdecode<T, C, W, HD, NT>, dim3((unsigned)(per * p.ncg)), dim3(64 * kDecodeWaves), s, d);
     if (err != hipSuccess || !p.target) return err;
