@@ -1279,7 +1279,6 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
     constexpr int NW = kPromptWaves, KT = prompt_keys(HD), NB = KT / 32, NS = HD / 16, NC = HD / 32, CH = HD / 8;
     constexpr int QV = 32 * NW, RB = HD * 2;
     __shared__ __attribute__((aligned(1024))) char ks[2][KT * RB], vs[2][KT * RB];
-    __shared__ __attribute__((aligned(1024))) char raw[kHeld8<C> ? 2 * KT * HD : 1];
     const PagedAttnArgs& a = d.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, g = lane >> 5;
@@ -1371,49 +1370,53 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
             }
         }
     };
-    // Of 8 bits: the same groups as they lie, into the wave's part of `raw` (16 rows one behind the other); from there the wave
-    // takes them as bf16 to where the others are loaded to (in registers meanwhile, they took 8 to 44 of those to scratch, and
-    // 24 prompts of 1 to 2001 positions 400 us).
-    constexpr int TASKS = KT / 8 / NW, GB = 16 * HD;  // groups of a wave; bytes of one
-    uint32_t power[TASKS];
+    // Of 8 bits: the same groups through registers, a lane 16 (head dim 32: 8) neighbouring numbers of a row at a time, which
+    // leave them as bf16 for the places in LDS that the others are loaded to.  (Half of them at a time, 24 prompts of 1 to 2001
+    // positions take 385 us, not 371; through LDS as they lie, 407; taken from there a quarter a turn, 421.)
+    constexpr int NT = KT / 8 / NW, PB = HD >= 64 ? 16 : 8, PR = HD / PB, NP = 16 * PR / 64;  // a group's pieces: bytes, of a row, of a lane
+    uint32_t hold[kHeld8<C> ? NT : 1][NP ? NP : 1][PB / 4];
+    uint32_t power[NT];
     auto fetch = [&](int k0, int pg) {
 #pragma unroll
-        for (int w = 0; w < TASKS; ++w) {
+        for (int w = 0; w < NT; ++w) {
             const int task = wave + w * NW, grp = task % (KT / 16), key = k0 + 16 * grp, page = __builtin_amdgcn_readlane(pg, grp);
             const int rows = uniform(page < 0 ? 0 : max(min(end - key, 16), 0)), slot = position<W>(run, key) & mask;
-            const int64_t at = max(page, 0) * a.c.page_stride + (((int64_t)kvh << a.c.shift) + slot) * HD;
+            const int64_t at = uniform(max(page, 0) * a.c.page_stride + (((int64_t)kvh << a.c.shift) + slot) * HD);
             const bool isv = task >= KT / 16;
-            const int64_t base = uniform((int64_t)((uint8_t*)(isv ? a.c.v : a.c.k) + at));
-            const u4 rs = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffff, (uint32_t)(rows * HD), 0x00020000};
-            typedef __attribute__((address_space(3))) char* lds;
-            const uint32_t to = uniform((int)(uint32_t)(uintptr_t)(lds)(raw + task * GB));
+            const auto rs = __builtin_amdgcn_make_buffer_rsrc((uint8_t*)(isv ? a.c.v : a.c.k) + at, 0, rows * HD, 0x00020000);
+            power[w] = 0;
+            if (rows > 0) power[w] = a.c.scales[uniform((int64_t)page * a.c.scale_stride + (((int64_t)kvh << (a.c.shift - 4)) + (slot >> 4)) * 2 + isv)];
 #pragma unroll
-            for (int i = 0; i < (GB + 1023) / 1024; ++i)
-                if (GB >= 1024 || lane < GB / 16)
-                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                                 :: "s"(to + i * 1024), "v"(i * 1024 + lane * 16), "s"(rs) : "memory");
-            const auto rp = __builtin_amdgcn_make_buffer_rsrc(
-                a.c.scales + uniform((int64_t)max(page, 0) * a.c.scale_stride + (((int64_t)kvh << (a.c.shift - 4)) + (slot >> 4)) * 2 + isv), 0,
-                rows > 0 ? 1 : 0, 0x00020000);
-            power[w] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rp, 0, 0, 0);
+            for (int i = 0; i < NP; ++i) {
+                const int off = (i * 64 + lane) * PB;
+                if constexpr (PB == 16) {
+                    const u4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) hold[w][i][e] = x[e];
+                } else {
+                    const u2 x = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0);
+                    hold[w][i][0] = x[0];
+                    hold[w][i][1] = x[1];
+                }
+            }
         }
     };
     auto settle_in = [&](int buf) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int w = 0; w < TASKS; ++w) {
+        for (int w = 0; w < NT; ++w) {
             const int task = wave + w * NW, grp = task % (KT / 16);
             const bool isv = task >= KT / 16;
             char* const to = (isv ? vs[buf] : ks[buf]) + grp * 16 * RB;
-            const char* const from = raw + task * GB;
-            const float p = __uint_as_float(power[w] << 23);
-            // a lane 8 numbers of a row at a time: one unit of 16 bytes
+            const float p = power_k(power[w]);
 #pragma unroll
-            for (int i = 0; i < GB / 512; ++i) {
-                const int row = (i * 64 + lane) / CH, u = lane % CH, turn = (isv ? 4 * ((row & 3) / RL) : row / RL) & (CH - 1);
-                const u2 x = *(const u2*)(from + (i * 64 + lane) * 8);
-                *(u4*)(to + row * RB + ((u ^ turn) * 16)) =
-                    u4{e4m3_bf16<false>(x[0], p), e4m3_bf16<true>(x[0], p), e4m3_bf16<false>(x[1], p), e4m3_bf16<true>(x[1], p)};
+            for (int i = 0; i < NP; ++i) {
+                const int row = (i * 64 + lane) / PR, piece = (i * 64 + lane) % PR, turn = (isv ? 4 * ((row & 3) / RL) : row / RL) & (CH - 1);
+#pragma unroll
+                for (int e = 0; e < PB / 8; ++e) {
+                    const uint32_t x = hold[w][i][2 * e], y = hold[w][i][2 * e + 1];
+                    *(u4*)(to + row * RB + (((piece * (PB / 8) + e) ^ turn) * 16)) =
+                        u4{e4m3_bf16<false>(x, p), e4m3_bf16<true>(x, p), e4m3_bf16<false>(y, p), e4m3_bf16<true>(y, p)};
+                }
             }
         }
     };
