@@ -1689,13 +1689,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
 // reaches 154), 32 query vectors per wave and tiles of 32 keys, row by row in LDS
 // (rows of K four words apart from whole bank rounds).  A lane reads a row of K, or HD / 32 neighbouring
 // columns of its keys of V, at a time.
-// Four e4m3 numbers times a power of two.
-__device__ __forceinline__ f4 e4m3_f32(uint32_t w, float power) {
-    const f2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, power, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, power, true);
-    return f4{lo[0], lo[1], hi[0], hi[1]};
-}
-
-template <typename C, bool W, int HD>
+template <bool W, int HD>
 __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
     constexpr int KT = 32, QV = 128, C4 = HD / 4, KL = HD + 4, VW = HD / 32, NU = KT * C4 / 256;
     __shared__ __attribute__((aligned(16))) float ks[2][KT * KL], vs[2][KT * HD];
@@ -1732,8 +1726,7 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
     const int mask = (1 << a.c.shift) - 1;
-    std::conditional_t<kHeld8<C>, uint32_t, u4> st[2][NU];
-    uint32_t power[2];  // (8 bits) of the two groups of 16 keys, k's and v's
+    u4 st[2][NU];
     auto look = [&](int k0, int (&page)[2]) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -1743,43 +1736,23 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
     // unit i of a thread: row i * 1024 / HD + tid / C4, whose group of 16 keys is the same for a wave
     auto load = [&](int k0, const int (&page)[2]) {
         const int p0 = position<W>(run, k0);
-        if constexpr (kHeld8<C>) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int64_t at = (int64_t)max(page[t], 0) * a.c.scale_stride + (((int64_t)kvh << (a.c.shift - 4)) + (((p0 + 16 * t) & mask) >> 4)) * 2;
-                power[t] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
-                    __builtin_amdgcn_make_buffer_rsrc(a.c.scales + uniform(at), 0, page[t] >= 0 && k0 + 16 * t < end ? 2 : 0, 0x00020000), 0, 0, 0);
-            }
-        }
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
             const int t = HD == 32 ? wave >> 1 : i * (1024 / HD) / 16, key = k0 + 16 * t;
             const int pg = HD == 32 ? (t ? page[1] : page[0]) : page[t];
             const int rows = uniform(pg < 0 ? 0 : max(min(end - key, 16), 0));
             const int64_t at = uniform(max(pg, 0) * a.c.page_stride + (((int64_t)kvh << a.c.shift) + ((p0 + 16 * t) & mask)) * HD);
-            const int off = ((i * (1024 / HD) + tid / C4) % 16 * HD + tid % C4 * 4) * (int)sizeof(C);
-            if constexpr (kHeld8<C>) {
-                st[0][i] = __builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc((C*)a.c.k + at, 0, rows * HD, 0x00020000), off, 0, 0);
-                st[1][i] = __builtin_amdgcn_raw_buffer_load_b32(__builtin_amdgcn_make_buffer_rsrc((C*)a.c.v + at, 0, rows * HD, 0x00020000), off, 0, 0);
-                continue;
-            } else {
+            const int off = ((i * (1024 / HD) + tid / C4) % 16 * HD + tid % C4 * 4) * 4;
             st[0][i] = __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((float*)a.c.k + at, 0, rows * HD * 4, 0x00020000), off, 0, 0);
             st[1][i] = __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((float*)a.c.v + at, 0, rows * HD * 4, 0x00020000), off, 0, 0);
-            }
         }
     };
     auto store = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
             const int row = i * (1024 / HD) + tid / C4, x = tid % C4 * 4;
-            if constexpr (kHeld8<C>) {
-                const uint32_t w = HD == 32 ? (wave >> 1 ? power[1] : power[0]) : power[i * (1024 / HD) / 16];
-                *(f4*)(ks[buf] + row * KL + x) = e4m3_f32(st[0][i], power_k(w));
-                *(f4*)(vs[buf] + row * HD + x) = e4m3_f32(st[1][i], power_v(w));
-            } else {
-                *(u4*)(ks[buf] + row * KL + x) = st[0][i];
-                *(u4*)(vs[buf] + row * HD + x) = st[1][i];
-            }
+            *(u4*)(ks[buf] + row * KL + x) = st[0][i];
+            *(u4*)(vs[buf] + row * HD + x) = st[1][i];
         }
     };
     const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
@@ -1917,6 +1890,252 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
     if (sp.live > 1 && g == 0) *(f2*)(d.part + d.ml + at * 2) = f2{m, sum};
 }
 
+// fp32 rows over a cache of 8 bits: bf16 matrix instructions, which its values enter exactly, as q and the weights do in
+// three parts each, so that there are three for one of k_pprompt_bf16; the tiles, spans and careful pass of k_pprompt_f32, whose
+// instructions would take five times as long.  K and V lie in LDS as there in bf16.
+template <bool W, int HD>
+__global__ __launch_bounds__(256, 2) void k_pprompt_split(PromptArgs d) {
+    constexpr int KT = 32, QV = 128, NS = HD / 16, NC = HD / 32, CH = HD / 8, RB = HD * 2, RL = 16 / CH, PB = HD / 8;
+    __shared__ __attribute__((aligned(1024))) char ks[2][KT * RB], vs[2][KT * RB];
+    const PagedAttnArgs& a = d.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 31, g = lane >> 5;
+    const int G = a.H / a.c.Hkv;
+    const int kvh = blockIdx.x % a.c.Hkv, span = blockIdx.x / a.c.Hkv % d.nspan, tile = blockIdx.x / a.c.Hkv / d.nspan;
+    const Tile tl = prompt_tile<QV>(a.r, G, tile);
+    const int b = uniform(tl.b), v0 = uniform(tl.v0), r0 = uniform(tl.rows.r0), nrows = uniform(tl.rows.n);
+    if (b < 0) return;
+    const int nqv = nrows * G;
+    if (v0 >= nqv) return;
+    const int at0 = uniform(tl.rows.len) - nrows;
+    const int wv = v0 + 32 * wave;
+    const int first = at0 + v0 / G, last = at0 + min(v0 + QV - 1, nqv - 1) / G;  // of the tile's rows
+    const Run run = run_of<W>(a, first);
+    const Span sp = prompt_span(keys_below<W>(run, max(min(last + 1, (int64_t)a.c.max_pages << a.c.shift), 0)), d.nspan, span_keys<W>(d, KT, QV / G + 1, tl.rows), span);
+    if (span >= sp.live) return;
+    const int end = sp.upto;
+    const int wfirst = at0 + wv / G, wlast = at0 + min(wv + 31, nqv - 1) / G, wend = wv < nqv ? min(end, keys_below<W>(run, wlast + 1)) : 0;
+    const float c = a.scale * kLog2e;
+    const int v = wv + n, vc = min(v, nqv - 1), pos = at0 + vc / G;
+    u4 q[NS][3];
+    {
+        const float* p = (const float*)a.q + (r0 + vc / G) * a.q_stride + (kvh * G + vc % G) * HD + 8 * g;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            float x[8];
+            *(f4*)x = *(const f4*)(p + 16 * s) * c;
+            *(f4*)(x + 4) = *(const f4*)(p + 16 * s + 4) * c;
+            split3(x, q[s]);
+        }
+    }
+    f16v o[NC];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    const int mask = (1 << a.c.shift) - 1;
+    auto look = [&](int k0, int (&page)[2]) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            page[t] = k0 + 16 * t < end && (!W || any_reads<W>(a, first, last, position<W>(run, k0) + 16 * t, 16)) ?
+                          __builtin_amdgcn_readfirstlane(paged_page(a.c, b, (position<W>(run, k0) + 16 * t) >> a.c.shift)) : -1;
+    };
+    // a thread PB neighbouring numbers of row tid / 8, whose group of 16 keys is the wave's
+    uint32_t st[2][HD == 128 ? 4 : HD / 32], power = 0;
+    auto load = [&](int k0, const int (&page)[2]) {
+        const int t = wave >> 1, pg = t ? page[1] : page[0], key = k0 + 16 * t, slot = (position<W>(run, k0) + 16 * t) & mask;
+        const int rows = uniform(pg < 0 ? 0 : max(min(end - key, 16), 0));
+        const int64_t at = uniform(max(pg, 0) * a.c.page_stride + (((int64_t)kvh << a.c.shift) + slot) * HD);
+        power = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
+            __builtin_amdgcn_make_buffer_rsrc(a.c.scales + uniform((int64_t)max(pg, 0) * a.c.scale_stride + (((int64_t)kvh << (a.c.shift - 4)) + (slot >> 4)) * 2),
+                                              0, rows > 0 ? 2 : 0, 0x00020000), 0, 0, 0);
+        const int off = (tid / 8 % 16) * HD + tid % 8 * PB;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            const auto rs = __builtin_amdgcn_make_buffer_rsrc((uint8_t*)(kv ? a.c.v : a.c.k) + at, 0, rows * HD, 0x00020000);
+            if constexpr (PB == 16) {
+                const u4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st[kv][e] = x[e];
+            } else if constexpr (PB == 8) {
+                const u2 x = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0);
+                st[kv][0] = x[0];
+                st[kv][1] = x[1];
+            } else {
+                st[kv][0] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0);
+            }
+        }
+    };
+    // (16-byte unit u of a row at the place that k_pprompt_bf16 has it)
+    auto store = [&](int buf) {
+        const int row = tid / 8, piece = tid % 8;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            char* const to = (kv ? vs[buf] : ks[buf]) + row * RB;
+            const int turn = (kv ? 4 * ((row & 3) / RL) : row / RL) & (CH - 1);
+            const float p = kv ? power_v(power) : power_k(power);
+            if constexpr (PB == 4) {
+                *(u2*)(to + (((piece / 2) ^ turn) * 16) + piece % 2 * 8) = u2{e4m3_bf16<false>(st[kv][0], p), e4m3_bf16<true>(st[kv][0], p)};
+            } else {
+#pragma unroll
+                for (int e = 0; e < PB / 8; ++e) {
+                    const uint32_t x = st[kv][2 * e], y = st[kv][2 * e + 1];
+                    *(u4*)(to + (((piece * (PB / 8) + e) ^ turn) * 16)) =
+                        u4{e4m3_bf16<false>(x, p), e4m3_bf16<true>(x, p), e4m3_bf16<false>(y, p), e4m3_bf16<true>(y, p)};
+                }
+            }
+        }
+    };
+    int ka[NS], va[NC];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) ka[i] = n * RB + (((2 * i + g) ^ (n / RL & (CH - 1))) * 16);
+    const int vk = (lane & 15) / 4;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+        va[i] = (4 * g + vk) * RB + (((4 * i + (lane >> 4 & 1) * 2 + (lane & 3) / 2) ^ (4 * (vk / RL) & (CH - 1))) * 16) + (lane & 1) * 8;
+    typedef short h4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) h4* ldsv;
+    // V's values of 16 keys for columns 32 i ..
+    auto values = [&](const char* vf, int u, int i) {
+        const char* p = vf + va[i] + 16 * u * RB;
+        const u2 lo = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldsv)p));
+        const u2 hi = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldsv)(p + 8 * RB)));
+        return u4{lo[0], lo[1], hi[0], hi[1]};
+    };
+    auto mfma = [](u4 x, u4 y, f16v z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, x), __builtin_bit_cast(b8, y), z, 0, 0, 0); };
+    const int t0 = sp.from / KT, nt = (end + KT - 1) / KT;
+    int todo = INT32_MAX;  // (as in k_pprompt_f32)
+    auto pass = [&](auto careful, int from) {
+        constexpr bool kCareful = decltype(careful)::value;
+        int pg[2], nx[2];
+        look(from * KT, pg);
+        look((from + 1) * KT, nx);
+        load(from * KT, pg);
+        store(from & 1);
+        for (int t = from; t < nt; ++t) {
+            __syncthreads();
+            const int k0 = t * KT, p0 = position<W>(run, k0);
+            const bool all = all_read<W>(a, wfirst, wlast, p0, 32), whole = all && pg[0] >= 0 && pg[1] >= 0;
+            const bool have[2] = {pg[0] >= 0, pg[1] >= 0};
+            if (t + 1 < nt) {
+                pg[0] = nx[0];
+                pg[1] = nx[1];
+                load(k0 + KT, pg);
+                look(k0 + 2 * KT, nx);
+            }
+            const char *kf = ks[t & 1], *vf = vs[t & 1];
+            if (!kCareful && k0 < wend && !all && t < todo) {
+                uint32_t any = 0;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) {
+                        const u4 x = values(vf, u, i);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) any |= odd_bits<uint16_t>(x[e]);
+                    }
+                if (any_odd<uint16_t>(any)) todo = t;
+            }
+            if (k0 < wend && (kCareful ? t >= todo : t < todo)) {
+                f16v s, s1;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = s1[r] = 0.f;
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                    const u4 x = *(const u4*)(kf + ka[i]);
+                    s1 = mfma(x, q[i][2], s1);
+                    s = mfma(x, q[i][0], s);
+                    s1 = mfma(x, q[i][1], s1);
+                }
+                s += s1;
+                asm volatile("" : "+v"(s));  // (as in block_scores)
+                if (!whole)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int key = 8 * (r / 4) + 4 * g + r % 4;
+                        s[r] = reads<W>(a, pos, p0 + key) && have[r / 8] ? s[r] : -INFINITY;
+                    }
+                float mx = s[0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+                mx = half_max(mx);
+                if (__any(mx > m + kLazy)) {
+                    const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+                    m = mn;
+                    l *= f;
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) o[i] *= f;
+                }
+                const float base = m == -INFINITY ? 0.f : m;
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = __builtin_amdgcn_exp2f(s[r] - base);
+                    sum += s[r];
+                }
+                l += sum;
+                u4 w[2][3];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float x[8] = {s[8 * u], s[8 * u + 1], s[8 * u + 2], s[8 * u + 3], s[8 * u + 4], s[8 * u + 5], s[8 * u + 6], s[8 * u + 7]};
+                    split3(x, w[u]);
+                }
+                if constexpr (!kCareful) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int i = 0; i < NC; ++i) {
+                            const u4 x = values(vf, u, i);
+#pragma unroll
+                            for (int e = 2; e >= 0; --e) o[i] = mfma(x, w[u][e], o[i]);
+                        }
+                } else {
+                    const int upto = W ? wlast : min(k0 + 32, end) - 1;
+#pragma unroll 1
+                    for (int at = W ? wfirst : max(wfirst, k0); at <= upto; ++at)
+#pragma unroll
+                        for (int i = 0; i < NC; ++i) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            const int key = unknown(p0 + 4 * g);
+                            f16v z = {};
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                u4 x = values(vf, u, i);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const int j = key + 16 * u + 8 * (e / 2) + e % 2 * 2;
+                                    x[e] &= (reads<W>(a, at, j) ? 0xffffu : 0u) | (reads<W>(a, at, j + 1) ? 0xffff0000u : 0u);
+                                }
+#pragma unroll
+                                for (int e = 2; e >= 0; --e) z = mfma(x, w[u][e], z);
+                            }
+                            const bool mine = (W ? pos : min(pos, upto)) == at;
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) o[i][r] += mine ? z[r] : 0.f;
+                        }
+                }
+            }
+            if (t + 1 < nt) store((t + 1) & 1);
+        }
+    };
+    pass(std::false_type{}, t0);
+    if (__syncthreads_or(todo != INT32_MAX)) pass(std::true_type{}, W ? t0 : max(t0, first / KT));
+    const float sum = half_sum(l), inv = sp.live > 1 ? 1.f : inverse<W>(a, b, sum, pos, wlast);
+    if (v >= nqv) return;
+    const int64_t at = (((int64_t)tile * a.c.Hkv + kvh) * d.nspan + span) * QV + wv - v0 + n;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int col = 32 * i + 2 * r + 4 * g;
+            const float y[4] = {o[i][r] * inv, o[i][r + 1] * inv, o[i][r + 2] * inv, o[i][r + 3] * inv};
+            if (sp.live > 1) *(f4*)(d.part + at * HD + col) = f4{y[0], y[1], y[2], y[3]};
+            else put<float, 4>(a, r0 + v / G, (kvh * G + v % G) * HD + col, y);
+        }
+    if (sp.live > 1 && g == 0) *(f2*)(d.part + d.ml + at * 2) = f2{m, sum};
+}
+
 // The spans of k_pprompt's tiles joined: a thread per query vector and 4 columns.
 template <typename T, bool W, int HD, int QV, int KT>
 __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs d) {
@@ -1987,7 +2206,8 @@ hipError_t prompt(hipStream_t s, const PagedAttnArgs& a, const PromptPlan& p, fl
     const PromptArgs d{a, (int)p.tiles, p.nspan, p.least, ws, p.ml};
     hipError_t err;
     if constexpr (sizeof(T) == 2) err = launch(k_pprompt_bf16<C, W, HD>, dim3((unsigned)(groups * p.nspan)), dim3(64 * kPromptWaves), s, d);
-    else err = launch(k_pprompt_f32<C, W, HD>, dim3((unsigned)(groups * p.nspan)), dim3(256), s, d);
+    else if constexpr (kHeld8<C>) err = launch(k_pprompt_split<W, HD>, dim3((unsigned)(groups * p.nspan)), dim3(256), s, d);
+    else err = launch(k_pprompt_f32<W, HD>, dim3((unsigned)(groups * p.nspan)), dim3(256), s, d);
     if (err != hipSuccess || p.nspan == 1) return err;
     return launch(k_prompt_join<T, W, HD, kPromptQv<T>, sizeof(T) == 2 ? prompt_keys(HD) : 32>, dim3((unsigned)(groups * nj)), dim3(256), s, d);
 }
