@@ -765,17 +765,17 @@ __device__ __forceinline__ void block_sums_odd(const BlockOf<T, C, HD>& x, const
 }
 
 // Query vector v of a sequence and KV head: row v / G of the sequence, head kvh * G + v % G.
-template <typename T, typename C, bool W, int HD, int NT>
-__global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) {
+template <typename T, typename C, bool W, int HD, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_pdecode(DecodeArgs d) {
     using B = BlockOf<T, C, HD>;
     constexpr int QV = 16 * NT, BK = kBlockKeys<C>;
     // Whether every wave joins a quarter of the columns (below).
     constexpr bool QUARTERS = kHeld8<C> || W;
     // the query vectors' operands in registers; 32 vectors of three parts each, which would take 96, in LDS
     constexpr bool QL = NT == 2 && B::QP == 3;
-    constexpr int NI = NT * (HD / 16), OS = (QUARTERS ? kDecodeWaves : kDecodeWaves / 2) * NI * 64, QS = QL ? NT * 3 * B::NK * 64 : 0;
+    constexpr int NI = NT * (HD / 16), OS = (QUARTERS ? NW : NW / 2) * NI * 64, QS = QL ? NT * 3 * B::NK * 64 : 0;
     __shared__ __attribute__((aligned(16))) f4 lds[OS > QS ? OS : QS];  // the operands, then the waves' sums
-    __shared__ float ms[kDecodeWaves][QV][2];
+    __shared__ float ms[NW][QV][2];
     const PagedAttnArgs& a = d.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
@@ -790,7 +790,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     const int G = a.H / a.c.Hkv;
     // the first two blocks' table entries, which need no length (a sequence that is one unit has been asked
     // for nothing else yet, and one round trip to memory is saved)
-    constexpr int step = kDecodeWaves * BK;
+    constexpr int step = NW * BK;
     const int kb = (unit - un.first) * un.keys;
     int k0 = kb + wave * BK;
     const Run run = run_of<W>(a, uniform(un.rows.len) - uniform(un.rows.n));
@@ -827,7 +827,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
             if constexpr (B::QP == 1) {
                 q[j][0][i] = *(const u4*)(p + col);
             } else {
-                if (QL && wave != (j * B::NK + i) % kDecodeWaves) continue;
+                if (QL && wave != (j * B::NK + i) % NW) continue;
                 float x[8];
                 *(f4*)x = *(const f4*)(p + col);
                 *(f4*)(x + 4) = *(const f4*)(p + col + 4);
@@ -945,7 +945,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
         block_sums_odd<T, C, W, HD, NT>(x, sc, a, position<W>(run, k0), W ? first : max(first, k0), W ? last : min(k0 + BK, ke) - 1, pos, acc, lane);
     }
     // The waves' parts on one maximum, added.  By quarters: every wave takes the columns of one r of its four, all waves' parts
-    // of them, and writes those.
+    // of them, and writes those (of eight waves: one of two query vectors' or half of them).
     if constexpr (QUARTERS) {
         if constexpr (QL) __syncthreads();  // (nobody reads operands any more)
         float* const os = (float*)lds;
@@ -962,14 +962,17 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
                 for (int r = 0; r < 4; ++r) os[((wave * 4 + r) * NI + j * (HD / 16) + i) * 64 + lane] = acc.o[j][i][r];
         }
         __syncthreads();
+        constexpr int HALF = NW == 8 && NT == 1 ? 2 : 1, N = B::VW / HALF;  // columns of a wave
+        const int r = wave & 3, h = HALF == 2 ? wave >> 2 : 0;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            float m = -INFINITY, l = 0.f, f[kDecodeWaves];
+            if (NW == 8 && NT == 2 && wave >> 2 != j) continue;
+            float m = -INFINITY, l = 0.f, f[NW];
 #pragma unroll
-            for (int w = 0; w < kDecodeWaves; ++w) m = fmaxf(m, ms[w][16 * j + n][0]);
+            for (int w = 0; w < NW; ++w) m = fmaxf(m, ms[w][16 * j + n][0]);
             const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-            for (int w = 0; w < kDecodeWaves; ++w) {
+            for (int w = 0; w < NW; ++w) {
                 f[w] = __builtin_amdgcn_exp2f(ms[w][16 * j + n][0] - base);
                 l += ms[w][16 * j + n][1] * f[w];
             }
@@ -977,34 +980,38 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
             const float inv = !whole_seq ? 1.f : inverse<W>(a, b, l, pos[j], last);
 #pragma unroll
             for (int u = 0; u < B::VU; ++u) {
-                float y[B::VW];
+                float y[N];
 #pragma unroll
-                for (int e = 0; e < B::VW; ++e) {
-                    const float* p = os + (wave * NI + j * (HD / 16) + u * B::VW + e) * 64 + lane;
+                for (int e = 0; e < N; ++e) {
+                    const float* p = os + (r * NI + j * (HD / 16) + u * B::VW + h * N + e) * 64 + lane;
                     y[e] = 0.f;
 #pragma unroll
-                    for (int w = 0; w < kDecodeWaves; ++w) y[e] += p[w * 4 * NI * 64] * f[w];
+                    for (int w = 0; w < NW; ++w) y[e] += p[w * 4 * NI * 64] * f[w];
                     y[e] *= inv;
                 }
-                const int c = (16 * u + 4 * g + wave) * B::VW;
+                const int c = (16 * u + 4 * g + r) * B::VW + h * N;
                 if (v >= nqv) continue;
                 if (!whole_seq) {
                     float* p = d.part + (slot * QV + 16 * j + n) * HD + c;
-                    if constexpr (B::VW >= 4) {
+                    if constexpr (N >= 4) {
 #pragma unroll
-                        for (int i = 0; i < B::VW; i += 4) *(f4*)(p + i) = f4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+                        for (int i = 0; i < N; i += 4) *(f4*)(p + i) = f4{y[i], y[i + 1], y[i + 2], y[i + 3]};
                     } else {
-                        *(f2*)p = f2{y[0], y[1]};
+#pragma unroll
+                        for (int i = 0; i < N; ++i) p[i] = y[i];
                     }
-                } else if constexpr (B::VW >= 4) {
-                    put<T, B::VW>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
+                } else if constexpr (N >= 4) {
+                    put<T, N>(a, r0 + v / G, (kvh * G + v % G) * HD + c, y);
                 } else {
                     T* p = (T*)a.out + (r0 + v / G) * a.out_stride + (kvh * G + v % G) * HD + c;
-                    if constexpr (sizeof(T) == 2) *(uint32_t*)p = pack_bf16(y[0], y[1]);
-                    else *(f2*)p = f2{y[0], y[1]};
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        if constexpr (sizeof(T) == 2) p[i] = (uint16_t)pack_bf16(y[i], 0.f);
+                        else p[i] = y[i];
+                    }
                 }
             }
-            if (!whole_seq && v < nqv && g == 0 && wave == j) *(f2*)(d.part + d.ml + (slot * QV + 16 * j + n) * 2) = f2{m, l};
+            if (!whole_seq && v < nqv && g == 0 && wave == (NW == 8 && NT == 2 ? 4 * j : j)) *(f2*)(d.part + d.ml + (slot * QV + 16 * j + n) * 2) = f2{m, l};
         }
         return;
     }
@@ -1023,18 +1030,18 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void k_pdecode(DecodeArgs d) 
     for (int j = 0; j < NT; ++j) {
         float m = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kDecodeWaves; ++w) m = fmaxf(m, ms[w][16 * j + n][0]);
+        for (int w = 0; w < NW; ++w) m = fmaxf(m, ms[w][16 * j + n][0]);
         mt[j] = m;
         const float base = m == -INFINITY ? 0.f : m;
         lt[j] = 0.f;
 #pragma unroll
-        for (int w = 0; w < kDecodeWaves; ++w) lt[j] += ms[w][16 * j + n][1] * __builtin_amdgcn_exp2f(ms[w][16 * j + n][0] - base);
+        for (int w = 0; w < NW; ++w) lt[j] += ms[w][16 * j + n][1] * __builtin_amdgcn_exp2f(ms[w][16 * j + n][0] - base);
         const float f = __builtin_amdgcn_exp2f(acc.m[j] - base);
 #pragma unroll
         for (int i = 0; i < HD / 16; ++i) acc.o[j][i] *= f;
     }
 #pragma unroll
-    for (int half = kDecodeWaves / 2; half > 0; half /= 2) {
+    for (int half = NW / 2; half > 0; half /= 2) {
         if (wave >= half && wave < 2 * half)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
@@ -2227,6 +2234,7 @@ constexpr int kDirect = 6;
 
 struct DecodePlan {
     int nt, ncg, target, units;
+    bool wide;   // eight waves
     int64_t ml;  // floats of the sums
     size_t bytes;
 };
@@ -2242,7 +2250,14 @@ inline DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, boo
     const int64_t groups = (int64_t)c.Hkv * p.ncg;
     // two workgroups per CU, or as many units again as sequences (for 384 / 512 / 768 workgroups 16 fp32 sequences
     // of 256 to 2048 take 41.4 / 36.4 / 44.6 us, and the 905 MB batch 171 / 159 / 161)
-    int64_t target = max_len <= kDirect * kDecodeWaves * (bf16 ? 32 : 16) ? 0 : std::max<int64_t>((512 + groups - 1) / groups - (fine ? r.nseq / 2 : 0), r.nseq);
+    const int bk = bf16 || c.scales ? 32 : 16;
+    // fine: eight waves and one unit for a sequence, where four waves do not take its keys at once, there is a workgroup for
+    // each CU at most, and the keys are few (us with four waves, or in units, and with eight; 8 bits, 8 KV heads): one
+    // sequence of 517, head dim 64, 7.6 and 6.5, of 1500 9.7 and 10.4; head dim 128, 700 10.1 and 9.6, 1000 10.6 and 11.0; 16
+    // sequences of 1200 16.4 and 13.4; bf16 under a window, one of 517, head dim 64, 7.8 and 7.3, 700 8.7 and 9.2
+    const int64_t whole = r.nseq * groups, key_bytes = (int64_t)c.hd * (c.scales ? 1 : bf16 ? 2 : 4);
+    p.wide = fine && whole <= 256 && max_len > kDecodeWaves * bk && max_len <= kDirect * 8 * bk && (whole >= 64 || max_len * key_bytes <= 88 << 10);
+    int64_t target = p.wide || max_len <= kDirect * kDecodeWaves * bk ? 0 : std::max<int64_t>((512 + groups - 1) / groups - (fine ? r.nseq / 2 : 0), r.nseq);
     const size_t per = (size_t)groups * 16 * p.nt * (c.hd + 2) * sizeof(float);
     if (target && per * (target + r.nseq + 8) > bytes) target = std::max<int64_t>(0, (int64_t)(bytes / per) - r.nseq - 8);
     p.target = (int)target;
@@ -2269,7 +2284,10 @@ template <typename T, typename C, bool W, int HD, int NT>
 hipError_t run_decode(hipStream_t s, const PagedAttnArgs& a, const DecodePlan& p, float* ws) {
     const DecodeArgs d{a, p.ncg, p.target, kDecodeWaves * kBlockKeys<C>, p.units, ws, p.ml};
     const int64_t per = ((int64_t)p.units * a.c.Hkv + 7) / 8 * 8;
-    const hipError_t err = launch(k_pdecode<T, C, W, HD, NT>, dim3((unsigned)(per * p.ncg)), dim3(64 * kDecodeWaves), s, d);
+    const dim3 grid((unsigned)(per * p.ncg));
+    if constexpr (kHeld8<C> || W)
+        if (p.wide) return launch(k_pdecode<T, C, W, HD, NT, 8>, grid, dim3(64 * 8), s, d);
+    const hipError_t err = launch(k_pdecode<T, C, W, HD, NT, kDecodeWaves>, grid, dim3(64 * kDecodeWaves), s, d);
     if (err != hipSuccess || !p.target) return err;
     constexpr int nb = join_blocks(HD, NT);
     return launch(k_pjoin<T, C, W, HD, NT>, dim3((unsigned)(a.r.nseq * a.c.Hkv * p.ncg * nb)), dim3(256), s, d);
