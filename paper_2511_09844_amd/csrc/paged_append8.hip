@@ -8,7 +8,12 @@
 //
 // A wave has a unit: up to 16 rows of one sequence that share a block, and one KV head.  It loads their k and v (a lane 8
 // neighbouring values of 64 / (hd / 8) rows at a time), takes the largest magnitudes over the wave, and writes the
-// numbers, 8 bytes a lane, rows of a block one behind the other.
+// numbers, 8 bytes a lane, rows of a block one behind the other.  Where all magnitudes are finite and a power reaches them, a
+// value costs half an instruction for its magnitude (bf16) and half a one to convert; others are looked at one by one.
+//
+// Bound by the bytes and, for single rows, by a launch and two to three round trips: 36764 bf16 rows of 8 heads of 128
+// (226 MB read and written) 54 us, 4.2 TB/s; one fp32 row of each of 16 sequences 4.1 us.  A wave for k and one for v took
+// 78 and 71 us; five workgroups a CU instead of four 54, six (to scratch) 63; groups of 32 or 64 rows 55.
 #include <algorithm>
 
 #include "device_common.h"

@@ -21,6 +21,15 @@
 // its join, one of a bf16 batch of 905 MB 165 (5.5 TB/s), eight rows of 16 fp32 sequences 50 (155 MB, and
 // 16 us of fp32 matrix instructions that overlap with the loads in part); one short sequence is
 // bound by round trips to memory in a row, 7.1 us.  Prompts are bound by the matrix cores, see k_pprompt_bf16.
+//
+// The same kernels read caches of 8 bits, whose numbers become bf16 operands on their way (two of them an instruction, the
+// power of two with it), and windows.  8 bits: two sequences of 90001 and 131071 positions (453 MB) take 90 us (5.0
+// TB/s), one token of 16 fp32 sequences (38 MB) 17.0, eight rows of them 24.1, one short sequence 6.2: half of the
+// second and third is what starts and ends a call (lengths, table, first block; the waves' sums, the join), which fewer
+// bytes do not shorten.  A window of 2048 of 16 sequences of up to 20000 (131 MB of bf16) takes 31.4 us.
+//
+// Matrix instructions' results are used in the same stretch of code, before any branch: behind one the compiler
+// has left too few wait states (see block_scores), which changed results.
 #pragma once
 #include <math.h>
 
@@ -118,6 +127,15 @@ __device__ __forceinline__ int wave_total(int v) {
     v = dpp_add<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
     v = dpp_add<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
     return __builtin_amdgcn_readlane(v, 63);
+}
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int wave_upto(int v) {
+    v = dpp_add<0x111, 0xf>(v);  // row_shr:1
+    v = dpp_add<0x112, 0xf>(v);  // row_shr:2
+    v = dpp_add<0x114, 0xf>(v);  // row_shr:4
+    v = dpp_add<0x118, 0xf>(v);  // row_shr:8
+    v = dpp_add<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
+    return dpp_add<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
 }
 // Maximum over a wave of values that are not negative.
 template <int CTRL, int ROWS>
@@ -279,12 +297,7 @@ __device__ __forceinline__ Units units_of(const DecodeArgs& d, int unit, int b) 
     for (int b0 = 0; b0 < nseq; b0 += 64) {
         if (b0) mine = b0 + lane < nseq ? seq_rows(a.r, b0 + lane) : SeqRows{};
         const int cnt = b0 + lane < nseq ? max((seq_keys<W>(a, mine) + (u.keys - 1)) / u.keys, 1) : 0;
-        int inc = cnt;
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            const int y = __shfl_up(inc, o, 64);
-            if (lane >= o) inc += y;
-        }
+        const int inc = wave_upto(cnt);
         const uint64_t here = unit < 0 ? (b >= b0 && b < b0 + 64 ? (uint64_t)1 << (b - b0) : 0) : __ballot(unit < at + inc);
         if (here) {
             const int l = __builtin_ctzll(here);
