@@ -457,7 +457,8 @@ sd2_status sd2_paged_append_scaled(const sd2_paged_scaled* kv, const sd2_paged_r
 
 /*
  * sd2_paged_attn_window over such a cache (window 0: sd2_paged_attn), for q and out of kv->kv.dtype.  The cache's values enter
- * both products exactly; q, sums and softmax are as there.
+ * both products exactly; bf16: q, sums and softmax are as there; fp32: q and the softmax's weights enter as three bf16
+ * numbers each, which together hold their 24 bits, and all sums are in fp32.
  */
 size_t sd2_paged_attn_scaled_workspace_bytes(const sd2_paged_scaled* kv, const sd2_paged_rows* rows, int32_t n_heads,
                                        int32_t max_len, int32_t window, int32_t sinks);

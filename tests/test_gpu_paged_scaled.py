@@ -163,9 +163,11 @@ def test_scores_far_apart_and_scales_at_their_ends(dtype):
             check(cache.attend(q, dl, scale=scale), cache, q, [800], [rows], scale=scale)
 
 
-def test_pages_take_their_scales_along():
+# records of the scales of 12, 16 and 2048 bytes
+@pytest.mark.parametrize("hkv,page", [(3, 32), (4, 32), (64, 256)])
+def test_pages_take_their_scales_along(hkv, page):
     """Forks, copies on writing, trims and compactions of a small pool against a list model."""
-    page, hkv, layers = 32, 3, 2
+    layers = 2
     from paper_2511_09844_amd.paged import PagedCache
     cache = PagedCache.empty(14, page, layers, hkv, 32, 4, 5, dtype=torch.float8_e4m3fn)
     model = PageModel(14, page, 4, 5)
