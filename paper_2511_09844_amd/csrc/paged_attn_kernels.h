@@ -230,7 +230,7 @@ __device__ __forceinline__ float inverse(const PagedAttnArgs& a, int b, float su
 // rows 57, not 49 (larger units, and one more join of the waves' sums).
 constexpr int kDecodeWaves = 4;
 
-// The keys a workgroup of k_pdecode takes at a time, 16 or 32 per wave.
+// The keys a wave of k_pdecode takes at a time, in tiles of 16: 32, or 16 of fp32.
 template <typename C>
 constexpr int kTiles = sizeof(C) == 4 ? 1 : 2;  // of 16 keys
 template <typename C>
@@ -802,7 +802,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_pdecode(DecodeArgs d) {
     if (b < 0) return;
     const int G = a.H / a.c.Hkv;
     // the first two blocks' table entries, which need no length (a sequence that is one unit has been asked
-    // for nothing else yet, and one round trip to memory is saved)
+    // for nothing else yet, and one round trip to memory is saved); under a window the length says where they are
     constexpr int step = NW * BK;
     const int kb = (unit - un.first) * un.keys;
     int k0 = kb + wave * BK;
