@@ -1,6 +1,8 @@
 // The paged calls on torch tensors that are as they should be (paged.py): the checks, the arguments and the call in one
 // step, 0.5 us of host time where Python takes 5 to 9 beside the launch.  Any argument that is not a plain case of what
-// the call documents, and any refusal, gives None, and paged.py's own checks say what is wrong.
+// the call documents, and any refusal (SD2_ERR_INVALID_ARG, which comes before anything is enqueued), gives None, and
+// paged.py's own checks say what is wrong.  A call that failed otherwise is not to be made again, as it may have enqueued a
+// part of its work (sd2_pages_reserve: the tables, but not the copies that they ask for): its error is raised here.
 //
 // These calls are bound by the host otherwise: one row of each of 16 sequences is appended in 4.4 us on the GPU.
 #include <Python.h>
@@ -106,6 +108,24 @@ at::Tensor bytes(size_t n, const at::Tensor& like) {
 #define NONE_IF(cond) \
     if (cond) Py_RETURN_NONE
 
+// What a call that was made gives: result (a new reference, made before the call: nothing may throw behind it), None where it
+// was refused, else the exception that binding.check makes of its status.
+PyObject* ended(sd2_status rc, const char* call, PyObject* result) {
+    if (rc == SD2_OK) return result;
+    Py_DECREF(result);
+    NONE_IF(rc == SD2_ERR_INVALID_ARG);
+    if (PyObject* binding = PyImport_ImportModule("paper_2511_09844_amd.binding")) {
+        Py_XDECREF(PyObject_CallMethod(binding, "check", "iOs", (int)rc, Py_None, call));
+        Py_DECREF(binding);
+    }
+    if (!PyErr_Occurred()) PyErr_Format(PyExc_RuntimeError, "%s: status %d", call, (int)rc);
+    return nullptr;
+}
+PyObject* new_true() {
+    Py_INCREF(Py_True);
+    return Py_True;
+}
+
 // cache(device, n_layers, hd, hkv, max_seqs, max_pages, page_size, held8, kv of fp32 rows, of bf16 rows (addresses or 0),
 // pages (address), unused workspace, workspace bytes of pages, scale)
 PyObject* make_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -154,8 +174,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return c->held8 ? sd2_paged_append_scaled(&c->scaled[k.dtype][layer], &r, kp, k.stride, vp, v.stride, reinterpret_cast<void*>(stream))
                         : sd2_paged_append(&c->kv[k.dtype][layer], &r, kp, k.stride, vp, v.stride, reinterpret_cast<void*>(stream));
     });
-    NONE_IF(rc != SD2_OK);
-    Py_RETURN_TRUE;
+    return ended(rc, c->held8 ? "sd2_paged_append_scaled" : "sd2_paged_append", new_true());
 }
 
 // attend(cache, stream, q, lens, layer, row_off, max_rows, max_len, scale, out, window, sinks): out, or None
@@ -195,16 +214,15 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const void* qp = q.t->data_ptr();
     void* op = out.data_ptr();
+    PyObject* result = a[9];
+    if (result == Py_None) result = THPVariable_Wrap(std::move(out));
+    else Py_INCREF(result);
+    if (!result) return nullptr;
     const sd2_status rc = unlocked([&] {
         return sc ? sd2_paged_attn_scaled(sc, &r, qp, q.stride, op, o.stride, heads, scale, max_len, window, sinks, w, need, reinterpret_cast<void*>(stream))
                   : sd2_paged_attn_window(kv, &r, qp, q.stride, op, o.stride, heads, scale, max_len, window, sinks, w, need, reinterpret_cast<void*>(stream));
     });
-    NONE_IF(rc != SD2_OK);
-    if (a[9] != Py_None) {
-        Py_INCREF(a[9]);
-        return a[9];
-    }
-    return THPVariable_Wrap(std::move(out));
+    return ended(rc, sc ? "sd2_paged_attn_scaled" : window ? "sd2_paged_attn_window" : "sd2_paged_attn", result);
 }
 
 // A list, tuple or range of sequences of the table.
@@ -235,8 +253,8 @@ PyObject* fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int64_t stream;
     std::vector<int32_t> src, dst;
     NONE_IF(!int_of(a[1], 0, INT64_MAX, stream) || !seqs_of(a[2], *c, src) || !seqs_of(a[3], *c, dst) || src.size() != dst.size() || src.empty());
-    NONE_IF(unlocked([&] { return sd2_pages_fork(&c->pages, src.size(), src.data(), dst.data(), reinterpret_cast<void*>(stream)); }) != SD2_OK);
-    Py_RETURN_TRUE;
+    const sd2_status rc = unlocked([&] { return sd2_pages_fork(&c->pages, src.size(), src.data(), dst.data(), reinterpret_cast<void*>(stream)); });
+    return ended(rc, "sd2_pages_fork", new_true());
 }
 
 // slide(cache, stream, lens, window, sinks): True, or None
@@ -250,8 +268,8 @@ PyObject* slide(PyObject*, PyObject* const* a, Py_ssize_t n) {
     NONE_IF(!int_of(a[3], 1, 1 << 30, window) || !int_of(a[4], 0, 1 << 30, sinks));
     const int32_t* p = static_cast<const int32_t*>(lens->data_ptr());
     const int32_t m = lens->numel();
-    NONE_IF(unlocked([&] { return sd2_pages_slide(&c->pages, m, p, window, sinks, reinterpret_cast<void*>(stream)); }) != SD2_OK);
-    Py_RETURN_TRUE;
+    const sd2_status rc = unlocked([&] { return sd2_pages_slide(&c->pages, m, p, window, sinks, reinterpret_cast<void*>(stream)); });
+    return ended(rc, "sd2_pages_slide", new_true());
 }
 
 // reserve(cache, stream, first, last, keep): granted, or None
@@ -269,16 +287,20 @@ PyObject* reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t *f = ints(first), *l = ints(last), *k = ints(keep);
     int32_t* g = static_cast<int32_t*>(granted.data_ptr());
     void* w = ws.data_ptr();
-    NONE_IF(unlocked([&] { return sd2_pages_reserve(&c->pages, m, f, l, k, g, w, c->pages_ws, reinterpret_cast<void*>(stream)); }) != SD2_OK);
-    return THPVariable_Wrap(std::move(granted));
+    PyObject* result = THPVariable_Wrap(std::move(granted));
+    if (!result) return nullptr;
+    const sd2_status rc = unlocked([&] { return sd2_pages_reserve(&c->pages, m, f, l, k, g, w, c->pages_ws, reinterpret_cast<void*>(stream)); });
+    return ended(rc, "sd2_pages_reserve", result);
 }
 
-// What torch throws (an allocation that fails, say) comes again, as its own exception, from the call that paged.py makes then.
+// What torch throws (an allocation that fails, say: all of it before the library's call) comes again, as its own exception, from
+// the call that paged.py makes then.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     try {
         return F(self, a, n);
     } catch (const std::exception&) {
+        PyErr_Clear();
         Py_RETURN_NONE;
     }
 }
