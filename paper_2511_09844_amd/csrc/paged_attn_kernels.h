@@ -28,8 +28,10 @@
 // second and third is what starts and ends a call (lengths, table, first block; the waves' sums, the join), which fewer
 // bytes do not shorten.  A window of 2048 of 16 sequences of up to 20000 (131 MB of bf16) takes 31.4 us.
 //
-// Matrix instructions' results are used in the same stretch of code, before any branch: behind one the compiler
-// has left too few wait states (see block_scores), which changed results.
+// Behind a branch the compiler has left too few wait states before the use of a matrix instruction's result, which
+// changed results (see block_scores).  Scores that only one side of a branch masks are held in front of it.  Those of
+// k_pprompt_bf16 are used a turn later, behind a barrier and the loop's branches: at least 16 wait states on any way as
+// built, of the 12 that they need.  tests/test_wait_states.py walks every way of every kernel that was built.
 #pragma once
 #include <math.h>
 
@@ -1830,6 +1832,7 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
                     }
                 }
                 s += s1;
+                asm volatile("" : "+v"(s));  // (as in block_scores)
                 if (!whole)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
