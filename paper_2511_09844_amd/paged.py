@@ -204,7 +204,8 @@ class PagedCache:
         """Causal attention of rows q [rows][heads][head_dim] over their sequences' pages
         (sd2_paged_attn), rows and positions as in append; returns out, like q.  scale: 1 / sqrt(head_dim)
         unless given; max_rows, max_len: the most rows and the largest length, where they are known (they
-        decide how the work is split).  With a window a row reads the last `window` positions up to its own and the
+        decide how the work is split, and max_rows how bf16 rows' weights are rounded; with row_off it is all rows
+        unless given).  With a window a row reads the last `window` positions up to its own and the
         first `sinks` ones (sd2_paged_attn_window); caches of 8 bits: sd2_paged_attn_scaled."""
         if self._plain():
             res = self._quick.attend(self._cache, _stream_of(self._index), q, lens, layer, row_off, max_rows, max_len, scale, out,
