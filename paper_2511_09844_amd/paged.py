@@ -23,6 +23,7 @@ current stream of that device.
 """
 import ctypes
 import math
+import warnings
 
 import torch
 from torch.autograd import forward_ad
@@ -99,7 +100,12 @@ class PagedCache:
         if self.held8:
             self._kv = {t: [B.PagedScaled(kv, scales.data_ptr() + l * record, n_layers * record) for l, kv in enumerate(kvs)]
                         for t, kvs in self._kv.items()}
-        self._quick = B.load_torch_paged()
+        try:
+            self._quick = B.load_torch_paged()
+        except (RuntimeError, ImportError) as e:  # (libsd2.so is there: the same calls, in more steps)
+            warnings.warn(f"{e}; until then each call takes 5 to 9 us more of the host", RuntimeWarning, stacklevel=2)
+            self._quick = None
+            return
         views = [(type(self._kv[t][0]) * n_layers)(*self._kv[t]) if t in self._kv else None for t in (torch.float32, torch.bfloat16)]
         self._cache = self._quick.cache(
             self._index, n_layers, hd, n_kv, self.max_seqs, self.max_pages, page, int(self.held8),
@@ -172,8 +178,8 @@ class PagedCache:
         return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
     def _plain(self):
-        """Whether a call may go the short way: on the current device, and where no tensor carries a tangent."""
-        return _device() == self._index and getattr(forward_ad, "_current_level", 0) < 0
+        """Whether a call may go the short way: if there is one, on the current device, and where no tensor carries a tangent."""
+        return self._quick is not None and _device() == self._index and getattr(forward_ad, "_current_level", 0) < 0
 
     def _call(self, fn, *args):
         """A C call on the current stream of the cache's device, which is the current one meanwhile."""

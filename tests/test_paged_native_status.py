@@ -2,7 +2,9 @@
 enqueued goes back to paged.py's own checks, any other failure is raised at once and the call not made again (a copy that failed
 behind the tables' rewrite would find nothing left to copy).
 
-In a process of its own, without a GPU: tensors of one aligned block of host memory that claim to be on device 0, and a
+Without the binding's library the same calls go through paged.py alone.
+
+In processes of their own, without a GPU: tensors of one aligned block of host memory that claim to be on device 0, and a
 library whose calls only count themselves and give the status that they are told to."""
 import os
 import subprocess
@@ -17,7 +19,7 @@ CALLS = ["sd2_paged_append", "sd2_paged_append_scaled", "sd2_paged_attn_window",
 STUB = ("#include <stddef.h>\nint calls, status;\n" + "".join(f"int {c}() {{ calls++; return status; }}\n" for c in CALLS)
         + "".join(f"size_t {c}_workspace_bytes() {{ return 256; }}\n" for c in CALLS if "attn" in c))
 
-PROGRAM = r'''
+SETUP = r'''
 import ctypes, sys
 stub = ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)  # its symbols come before those of libsd2.so
 import torch
@@ -46,23 +48,13 @@ torch.empty_like = lambda t, **kw: claimed(tuple(t.shape), t.dtype)
 torch.cuda._lazy_init, torch.cuda.current_device = (lambda: None), (lambda: 0)
 paged._device, paged._stream_of = (lambda: 0), (lambda i: 0)
 i32 = torch.int32
-caches = {}
-for held in (torch.float32, torch.float8_e4m3fn):
+
+
+def cache_of(held):
     pool = (4, 1, 2, 16, 32)
     scales = claimed((4, 1, 2, 1, 2), torch.float8_e8m0fnu) if held == paged.HELD8 else None
-    caches[held] = c = paged.PagedCache(claimed(pool, held), claimed(pool, held), claimed((3, 4), i32), claimed((4,), i32), scales)
+    return paged.PagedCache(claimed(pool, held), claimed(pool, held), claimed((3, 4), i32), claimed((4,), i32), scales)
 
-    class Again:  # paged.py's own way to the library
-        def __init__(self, lib):
-            self.real = lib
-
-        def __getattr__(self, name):
-            return again if name in CALLS + ["sd2_paged_attn"] else getattr(self.real, name)
-
-    def again(*args):
-        raise AssertionError("called again")
-    c.lib = Again(c.lib)
-CALLS = sys.argv[2].split(",")
 
 q, kv, lens = claimed((3, 2, 32), torch.float32), claimed((3, 2, 32), torch.float32), claimed((3,), i32)
 at += 1 << 16
@@ -75,6 +67,24 @@ ways = {
     "slide": ("sd2_pages_slide", lambda c: c.slide(lens, 5)),
     "reserve": ("sd2_pages_reserve", lambda c: c.reserve(lens, lens)),
 }
+'''
+
+STATUS = r'''
+CALLS = sys.argv[2].split(",")
+caches = {}
+for held in (torch.float32, torch.float8_e4m3fn):
+    caches[held] = c = cache_of(held)
+
+    class Again:  # paged.py's own way to the library
+        def __init__(self, lib):
+            self.real = lib
+
+        def __getattr__(self, name):
+            return again if name in CALLS + ["sd2_paged_attn"] else getattr(self.real, name)
+
+    def again(*args):
+        raise AssertionError("called again")
+    c.lib = Again(c.lib)
 for held, c in caches.items():
     for name, (what, call) in ways.items():
         calls.value, status.value = 0, 0
@@ -100,12 +110,39 @@ print("every status")
 '''
 
 
-def test_a_failed_call_is_raised_and_not_made_again(tmp_path):
+MISSING = r'''
+import warnings
+B.TORCH_SO = sys.argv[1] + ".missing"
+for held in (torch.float32, torch.float8_e4m3fn):
+    with warnings.catch_warnings(record=True) as told:
+        warnings.simplefilter("always")
+        c = cache_of(held)
+    assert [w.category for w in told] == [RuntimeWarning] and "not built" in str(told[0].message), told
+    for name, (what, call) in ways.items():
+        try:  # as far as the library, which finds no device
+            call(c)
+            raise SystemExit(f"{held} {name}: no call")
+        except B.Sd2Error as e:
+            assert what in str(e), e
+print("every call")
+'''
+
+
+def run(program, tmp_path):
     from paper_2511_09844_amd import binding
     binding.load_torch_paged()
     stub = tmp_path / "libstub.so"
     (tmp_path / "stub.c").write_text(STUB)
     subprocess.check_call(["gcc", "-shared", "-fPIC", "-o", str(stub), str(tmp_path / "stub.c")])
-    res = subprocess.run([sys.executable, "-c", PROGRAM, str(stub), ",".join(CALLS)], capture_output=True, text=True,
-                         env=dict(os.environ, PYTHONPATH=ROOT), timeout=300)
-    assert res.returncode == 0 and "every status" in res.stdout, res.stdout[-2000:] + res.stderr[-4000:]
+    res = subprocess.run([sys.executable, "-c", SETUP + program, str(stub), ",".join(CALLS)], capture_output=True, text=True,
+                         env=dict(os.environ, PYTHONPATH=ROOT, HIP_VISIBLE_DEVICES=""), timeout=300)
+    assert res.returncode == 0, res.stdout[-2000:] + res.stderr[-4000:]
+    return res.stdout
+
+
+def test_a_failed_call_is_raised_and_not_made_again(tmp_path):
+    assert "every status" in run(STATUS, tmp_path)
+
+
+def test_without_the_binding_calls_go_the_long_way(tmp_path):
+    assert "every call" in run(MISSING, tmp_path)
