@@ -450,7 +450,8 @@ typedef struct {
  * x / 2^e (ties to even, at most 448 in magnitude); an infinity or NaN becomes NaN.  Positions of the 16 behind the
  * last new row are not written (and count for nothing until they are).  One sequence's rows of 16 positions are
  * best brought in one call: what they are rounded to does not depend on it, except below 2^(e - 6), where numbers
- * that were rounded before e grew are rounded twice.
+ * that were rounded before e grew are rounded twice.  e falls only when the first of the 16 positions is written: rows that
+ * are written over from behind it (drafts that were rejected) leave it where they raised it, and the rows before them rounded.
  */
 sd2_status sd2_paged_append_scaled(const sd2_paged_scaled* kv, const sd2_paged_rows* rows, const void* k, int64_t k_stride,
                              const void* v, int64_t v_stride, void* hip_stream);

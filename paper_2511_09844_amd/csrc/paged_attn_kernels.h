@@ -24,9 +24,9 @@
 //
 // The same kernels read caches of 8 bits, whose numbers become bf16 operands on their way (two of them an instruction, the
 // power of two with it), and windows.  8 bits: two sequences of 90001 and 131071 positions (453 MB) take 90 us (5.0
-// TB/s), one token of 16 fp32 sequences (38 MB) 17.0, eight rows of them 24.1, one short sequence 6.2: half of the
+// TB/s), one token of 16 fp32 sequences (38 MB) 16.6, eight rows of them 23.7, one short sequence 6.3: half of the
 // second and third is what starts and ends a call (lengths, table, first block; the waves' sums, the join), which fewer
-// bytes do not shorten.  A window of 2048 of 16 sequences of up to 20000 (131 MB of bf16) takes 31.4 us.
+// bytes do not shorten.  A window of 2048 of 16 sequences of up to 20000 (131 MB of bf16) takes 31.0 us.
 //
 // Behind a branch the compiler has left too few wait states before the use of a matrix instruction's result, which
 // changed results (see block_scores).  Scores that only one side of a branch masks are held in front of it.  Those of
@@ -810,7 +810,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_pdecode(DecodeArgs d) {
     int k0 = kb + wave * BK;
     const Run run = run_of<W>(a, uniform(un.rows.len) - uniform(un.rows.n));
     // Blocks in registers: two, or one of 32 query vectors, unless it is of 8 bits (three of those, for 16 query vectors: a
-    // token of 16 sequences of 256 to 2048 17.9 us, not 17.0, and two long ones 90.3, not 89.3).
+    // token of 16 sequences of 256 to 2048 17.7 us, not 16.6, one of 517 6.7, not 6.3, and two long ones 90.4 and 90.2).
     constexpr int D = kHeld8<C> || NT == 1 ? 2 : 1, E = 2;
     int entry[E][B::TK];
 #pragma unroll
@@ -1393,8 +1393,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, HD == 32 ? 4 : 2) void k_pprompt
         }
     };
     // Of 8 bits: the same groups through registers, a lane 16 (head dim 32: 8) neighbouring numbers of a row at a time, which
-    // leave them as bf16 for the places in LDS that the others are loaded to.  (Half of them at a time, 24 prompts of 1 to 2001
-    // positions take 385 us, not 371; through LDS as they lie, 407; taken from there a quarter a turn, 421.)
+    // leave them as bf16 for the places in LDS that the others are loaded to.  (24 prompts of 1 to
+    // 2001 positions took 371 us this way, 385 with half of them at a time, 407 through LDS as they lie and 421 taken from
+    // there a quarter a turn, one after the other on one box.)  Registers for them go to scratch: 30 of head dim 32 (22 under a
+    // window), 7 of head dim 128 under a window.
     constexpr int NT = KT / 8 / NW, PB = HD >= 64 ? 16 : 8, PR = HD / PB, NP = 16 * PR / 64;  // a group's pieces: bytes, of a row, of a lane
     uint32_t hold[kHeld8<C> ? NT : 1][NP ? NP : 1][PB / 4];
     uint32_t power[NT];
@@ -1915,7 +1917,8 @@ __global__ __launch_bounds__(256, 2) void k_pprompt_f32(PromptArgs d) {
 
 // fp32 rows over a cache of 8 bits: bf16 matrix instructions, which its values enter exactly, as q and the weights do in
 // three parts each, so that there are three for one of k_pprompt_bf16; the tiles, spans and careful pass of k_pprompt_f32, whose
-// instructions would take five times as long.  K and V lie in LDS as there in bf16.
+// instructions would take five times as long.  K and V lie in LDS as there in bf16.  2000 positions of 32/8 heads of 128 take 162
+// to 175 us; head dim 128 has 7 registers in scratch, 12 under a window.
 template <bool W, int HD>
 __global__ __launch_bounds__(256, 2) void k_pprompt_split(PromptArgs d) {
     constexpr int KT = 32, QV = 128, NS = HD / 16, NC = HD / 32, CH = HD / 8, RB = HD * 2, RL = 16 / CH, PB = HD / 8;
@@ -2240,6 +2243,9 @@ hipError_t prompt(hipStream_t s, const PagedAttnArgs& a, const PromptPlan& p, fl
 // 128, 16 sequences of 2000 positions / one of 20000, us in k_pdecode and in k_pprompt:
 //   bf16:  48: 49 and 49 / 32 and 36    68: 75 and 51 / 37 and 38    132: 82 and 61 / 50 and 46
 //   fp32: 128: 184 and 195 / 112 and 130    192: 239 and 310 / 212 and 203    224: 306 and 319 / 252 and 207
+// and over 8 bits, where both kernels' instructions are bf16 ones:
+//   bf16:  48: 37 and 48 / 26 and 36    68: 46 and 50 / 39 and 38    96: 46 and 53 / 42 and 40    132: 67 and 61 / 55 and 47
+//   fp32: 132: 85 and 103 / 69 and 73   192: 87 and 111 / 79 and 79   224: 108 and 115 / 94 and 84   256: 110 and 123 / 73 and 88
 inline bool many_rows(const PagedView& c, const PagedRows& r, int H, bool bf16) {
     return (int64_t)r.max_rows * (H / c.Hkv) > (bf16 ? 64 : 192);
 }
@@ -2256,7 +2262,8 @@ struct DecodePlan {
 };
 
 // bytes: room for partials.  fine: units of whole blocks, not workgroup steps; with half a unit of each sequence that is
-// not full the workgroups are then those that the CUs hold at once (8 bits, 16 sequences: 17.0 us, and 21.6 without that).
+// not full the workgroups are then those that the CUs hold at once (one token of 16 sequences, 8 bits: 16.6 us, and 19.2
+// without that; under a window 31.0 and 37.0; eight rows 23.7 and 28.3).
 inline DecodePlan decode_plan(const PagedView& c, const PagedRows& r, int H, bool bf16, int64_t max_len, size_t bytes, bool fine = false) {
     DecodePlan p;
     const int qv = std::min<int64_t>((int64_t)r.max_rows * (H / c.Hkv), 1 << 20);
